@@ -240,10 +240,10 @@ def _own_scan(state):
 def _own_logprob(state):
     import paper_2105_14088_amd as cc
     args = (state["logits"], state["tokens"], state["mask"], state["placed"], state["scale"])
-    logprob, lse = cc.cc_token_logprob(*args)
+    logprob, rows = cc.cc_token_logprob(*args)
     if "grad" not in state:
         return [logprob]
-    return [logprob, cc.cc_token_logprob_backward(*args, lse, state["grad"], grad_scale=state["grad_scale"])]
+    return [logprob, cc.cc_token_logprob_backward(*args, rows, state["grad"], grad_scale=state["grad_scale"])]
 
 
 def _own_policy(state):
