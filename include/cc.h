@@ -8,7 +8,8 @@
  *     batches of candidate orders;
  *   - runs many independent searches: best-improvement 2-opt over the ring, pair-swap descent under the
  *     halving-doubling model, and simulated annealing for both (Section 4.3);
- *   - builds the cost matrix from latency probes (Section 4.2).
+ *   - builds the cost matrix from latency probes (Section 4.2);
+ *   - computes the parts of a learned policy over orders that matrix products do not cover (the order model, below).
  *
  * Conventions
  *   - Every buffer pointer is a DEVICE pointer owned by the caller unless stated otherwise.  The
@@ -29,7 +30,8 @@
  *     values are exact for the matrix they see; the max-hop and directed searches score true costs
  *     of the orders they produce; the annealing calls run a fixed number of steps.
  *     cc_validate_matrix checks the matrix contract.
- *   - All arithmetic is exact integer; costs are returned as int64.
+ *   - All arithmetic on costs is exact integer; costs are returned as int64.  Only the order-model calls (cc_embed and
+ *     below) compute in floating point.
  *   - Kernel choice never changes a result.  Each search call picks, from N, the objective and the size of
  *     the matrix entries, either a kernel specialised for that case or a general kernel that serves every
  *     case.  The environment variable CC_FORCE_PATH=general (read at every call) pins the general kernels:
@@ -383,6 +385,166 @@ int cc_cost_matrix_from_probes(const int32_t* samples, int32_t N, int32_t K, int
  * CC_ERR_NOT_SYMMETRIC.  Allocates and frees four bytes of device memory.
  */
 int cc_validate_matrix(const int32_t* cost_matrix, int32_t N, int32_t require_symmetric, void* stream);
+
+/*
+ * The order model.  Section 4.3 searches orders by permuting them; where a cost model has a batch call and no search of
+ * its own (BCube, double binary tree), orders can be proposed by a policy that learns from the batch calls' costs.  An order is a
+ * sequence of tokens: nodes are the vocabulary, rank t is position t, and a node that is placed is not placed again.  The
+ * calls below are the parts of such a policy that matrix products do not cover, forward and backward: a table of vectors
+ * looked up by node, a recurrence that carries what has been placed, log-probabilities of the orders' nodes, and
+ * the losses.  They serve sequences over any vocabulary alike.
+ *   - Elements are of one of the types below; computation is in 32-bit floating point or wider, each result is rounded once.
+ *   - Strides are in elements.  The innermost dimension is contiguous; a matrix or row may start at any element.
+ *   - Results do not depend on timing: the same call gives the same bits.
+ *   - Outputs must not overlap inputs, except where a call says so.
+ *   - The calls only enqueue kernels (no allocation, no memset): they can be captured into a graph.
+ *   - Workspaces: device memory, 256-byte aligned, at least the size that the matching *_workspace_bytes gives (else
+ *     CC_ERR_WORKSPACE; a size of 0 needs none), contents undefined before and after.
+ *   - Sizes: at most 2^24 elements in a row, fewer than 2^30 rows of a table and tokens of a list, fewer than 2^31 positions
+ *     (sequences times length), fewer than 2^32 channels (sequences times elements); else CC_ERR_INVALID_ARG.
+ */
+typedef enum {
+    CC_F32 = 0,
+    CC_F16 = 1,
+    CC_BF16 = 2
+} cc_dtype;
+
+/*
+ * Embedding lookup with scaling (the nodes of an order, Section 4.3's r_i, as vectors): out[i] = scale * table[ids[i]].
+ *   table   [V, D], rows table_stride apart;  ids int32 [n];  out [n, D], rows out_stride apart, the table's type.
+ * An id outside [0, V) is no token (padding, or the place before an order's first rank): its row is zero.
+ */
+int cc_embed(const void* table, int32_t dtype, int64_t V, int64_t D, int64_t table_stride, const int32_t* ids, int64_t n,
+             float scale, void* out, int64_t out_stride, void* stream);
+
+/*
+ * Its gradient: grad_table[v] = scale * (sum of grad[i] over the i with ids[i] = v), added up in 32 bits in the order of i
+ * (Section 4.3 scores many orders over the same nodes: every node has as many rows to add as there are orders).
+ *   grad        [n, D], rows grad_stride apart, of type dtype
+ *   grad_table  [V, D], rows grad_table_stride apart, of type grad_dtype: CC_F32 or dtype.  Written in full; with
+ *               accumulate != 0 the sums are added to what is there, and rows of ids that do not occur are left alone.
+ * Workspace: cc_embed_workspace_bytes(V, D, n).
+ */
+size_t cc_embed_workspace_bytes(int64_t V, int64_t D, int64_t n);
+int cc_embed_backward(const void* grad, int32_t dtype, int64_t n, int64_t D, int64_t grad_stride, const int32_t* ids, int64_t V,
+                      float scale, void* grad_table, int32_t grad_dtype, int64_t grad_table_stride, int32_t accumulate,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* The forward pass of the recurrence keeps the state before every CC_SCAN_CHUNK positions for the backward pass. */
+#define CC_SCAN_CHUNK 16
+
+/*
+ * Gated linear recurrence over the positions of B sequences, every channel by itself (what Section 4.3's search has placed
+ * so far, as a state):
+ *     keep = sigmoid(gate),  h_t = keep_t * h_{t-1} + (1 - keep_t) * x_t
+ *   x, gate    [B, T, D] of type dtype, strides as given (two halves of one matrix, for instance)
+ *   lengths    int32 [B] or NULL (all T).  Positions from a sequence's length on are not read and give h = 0.
+ *   h0         fp32 [B, D] or NULL (zero): the state before the first position
+ *   h          [B, T, D] of type dtype
+ *   last       fp32 [B, D] or NULL: the state after the last position that counts (h0 where there is none).  May be h0 itself:
+ *              with T = 1 the call is one step of sampling.
+ *   states     fp32 [B, ceil(T / CC_SCAN_CHUNK), D] or NULL: kept for the backward pass
+ * Workspace: cc_gated_scan_workspace_bytes(B, T, D), which may be 0.
+ */
+size_t cc_gated_scan_workspace_bytes(int64_t B, int64_t T, int64_t D);
+int cc_gated_scan(const void* x, int64_t x_stride_b, int64_t x_stride_t, const void* gate, int64_t gate_stride_b,
+                  int64_t gate_stride_t, int32_t dtype, int64_t B, int64_t T, int64_t D, const int32_t* lengths, const float* h0,
+                  void* h, int64_t h_stride_b, int64_t h_stride_t, float* last, float* states, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient (Section 4.3's search has none; the policy that stands in for it is trained by one).  x, gate, lengths
+ * and states are the forward call's.
+ *   grad_h     [B, T, D] of type dtype; positions from a sequence's length on are not read
+ *   grad_last  fp32 [B, D] or NULL (zero): the gradient of `last`
+ *   grad_x, grad_gate  [B, T, D] of type dtype, zero from a sequence's length on
+ *   grad_h0    fp32 [B, D] or NULL; may be grad_last itself
+ */
+int cc_gated_scan_backward(const void* x, int64_t x_stride_b, int64_t x_stride_t, const void* gate, int64_t gate_stride_b,
+                           int64_t gate_stride_t, int32_t dtype, int64_t B, int64_t T, int64_t D, const int32_t* lengths,
+                           const float* states, const void* grad_h, int64_t grad_h_stride_b, int64_t grad_h_stride_t,
+                           const float* grad_last, void* grad_x, int64_t grad_x_stride_b, int64_t grad_x_stride_t,
+                           void* grad_gate, int64_t grad_gate_stride_b, int64_t grad_gate_stride_t, float* grad_h0,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Log-probabilities of tokens: with z = scale * logits[b, t, :],
+ *     logprob[b, t] = z[tokens[b, t]] - log sum over the candidates j of exp(z_j)
+ *   logits     [B, T, V] of type dtype;  2^-64 <= scale <= 2^64 (an inverse temperature)
+ *   tokens     int32 [B, T]
+ *   mask       bytes [B, T] or NULL (all ones).  A position counts if its byte is not 0 and its token lies in [0, V); the
+ *              others' logits are not read, their log-probability is 0 and their gradient zero.
+ *   placed     0: every j is a candidate.  Otherwise V and T are at most CC_MAX_N (else CC_ERR_UNSUPPORTED_N) and the nodes
+ *              that the order has at an earlier position, masked or not, are no candidates (an order is a permutation,
+ *              Section 4.3): their logits have no effect, whatever they are, and no gradient.  A position's own token is
+ *              always a candidate.
+ *   logprob    fp32 [B, T]
+ *   rows       fp32 [B, T, 2], 8-byte aligned, or NULL: what the backward call needs of each row
+ * Where every candidate's logit is minus infinity the log-probability is minus infinity and the gradient zero.
+ */
+int cc_token_logprob(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t,
+                     const int32_t* tokens, const uint8_t* mask, int32_t placed, float scale, float* logprob, float* rows,
+                     void* stream);
+
+/*
+ * Its gradient, for a loss of the caller's own over the orders that Section 4.3's search compares:
+ *     grad_logits[b, t, j] = grad_scale * scale * grad_logprob[b, t] * ([j = token] - p_j)
+ * The first arguments and rows are the forward call's; grad_logprob is fp32 [B, T].  grad_logits [B, T, V] of type dtype may be
+ * the logits' own memory (same strides).
+ */
+int cc_token_logprob_backward(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b,
+                              int64_t stride_t, const int32_t* tokens, const uint8_t* mask, int32_t placed, float scale,
+                              const float* rows, const float* grad_logprob, float grad_scale, void* grad_logits,
+                              int64_t grad_stride_b, int64_t grad_stride_t, void* stream);
+
+/* How the positions' losses are averaged. */
+typedef enum {
+    CC_MEAN_TOKENS = 0,          /* over all positions that count */
+    CC_MEAN_ORDERS = 1           /* over each order's positions that count, then over the orders that have any */
+} cc_mean;
+
+/* Workspace of cc_policy_loss and cc_preference_loss. */
+size_t cc_token_workspace_bytes(int64_t B, int64_t T);
+
+/*
+ * Clipped policy loss with a divergence term, and its gradient in the same pass.  An order that costs less than the others
+ * (Section 4.1's models) has a positive advantage, and the policy that proposed it is moved towards it, but not far beyond what it
+ * was when it did.  With lp the log-probability of cc_token_logprob (whose arguments these calls share),
+ *     r = exp(lp - old_logprob),  gain = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *     kl = exp(ref_logprob - lp) - (ref_logprob - lp) - 1
+ *     loss = mean of (kl_coef * kl - gain)
+ *   old_logprob   fp32 [B, T]: when the orders were drawn
+ *   ref_logprob   fp32 [B, T] or NULL (no divergence term): under the policy to stay near to
+ *   advantage     fp32 [B], or [B, T] with advantage_per_token != 0
+ *   mean          cc_mean
+ *   grad_scale    multiplies the gradient (a loss scale, or the gradient of a loss that this one is a part of)
+ *   stats         fp32 [3]: loss, mean of kl, share of positions whose gain is clipped (averaged alike)
+ *   logprob       fp32 [B, T]
+ *   grad_logits   [B, T, V] of type dtype, or NULL (no gradient); may be the logits' own memory (same strides)
+ * Positions that do not count have no part in anything; with none at all stats and gradient are zero.
+ */
+int cc_policy_loss(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t,
+                   const int32_t* tokens, const uint8_t* mask, int32_t placed, float scale, const float* old_logprob,
+                   const float* ref_logprob, const float* advantage, int32_t advantage_per_token, float clip_low,
+                   float clip_high, float kl_coef, int32_t mean, float grad_scale, float* stats, float* logprob,
+                   void* grad_logits, int64_t grad_stride_b, int64_t grad_stride_t, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/*
+ * Preference loss over pairs of sequences, and its gradient: sequence i, the cheaper order (Section 4.1's models say which),
+ * is preferred to sequence B/2 + i.  B is even.  With lp as above and sums over the positions that count,
+ *     margin_i = beta * ((sum lp - sum ref_logprob) of i - (the same) of B/2 + i)
+ *     loss = mean over pairs of (1 - label_smoothing) * softplus(-margin) + label_smoothing * softplus(margin)
+ *   ref_logprob  fp32 [B, T] or NULL (zero);  0 <= label_smoothing <= 1
+ *   loss         fp32 [1];  margin fp32 [B/2];  logprob fp32 [B, T]
+ *   grad_logits, grad_scale, workspace as for cc_policy_loss.
+ * The sums are held in 64 bits.  With no pairs the loss is zero.
+ */
+int cc_preference_loss(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t,
+                       const int32_t* tokens, const uint8_t* mask, int32_t placed, float scale, const float* ref_logprob,
+                       float beta, float label_smoothing, float grad_scale, float* loss, float* margin, float* logprob,
+                       void* grad_logits, int64_t grad_stride_b, int64_t grad_stride_t, void* workspace,
+                       size_t workspace_bytes, void* stream);
 
 /* Static, human-readable text for a cc_status value (host pointer, never freed). */
 const char* cc_status_string(int status);

@@ -27,6 +27,9 @@ EXPORTS = ["cc_ring_cost_batch", "cc_ring_cost_batch_u8", "cc_ring_cost_batch_u1
            "cc_2opt_workspace_bytes", "cc_local_search", "cc_local_search_ex", "cc_best_of_restarts", "cc_rd_swap_search", "cc_rd_swap_search_ex",
            "cc_rd_swap_workspace_bytes", "cc_sa_search", "cc_sa_search_ex", "cc_sa_workspace_bytes", "cc_sa_rd_search",
            "cc_sa_rd_search_ex", "cc_init_tours", "cc_cost_matrix_from_probes", "cc_validate_matrix",
+           "cc_embed", "cc_embed_workspace_bytes", "cc_embed_backward", "cc_gated_scan", "cc_gated_scan_workspace_bytes",
+           "cc_gated_scan_backward", "cc_token_logprob", "cc_token_logprob_backward", "cc_token_workspace_bytes", "cc_policy_loss",
+           "cc_preference_loss",
            "cc_status_string", "cc_last_hip_error", "cc_version"]
 
 
@@ -107,6 +110,31 @@ def lib() -> ctypes.CDLL:
         L.cc_cost_matrix_from_probes.argtypes = [p, i32, i32, i32, i32, p, p]
         L.cc_validate_matrix.restype = ctypes.c_int
         L.cc_validate_matrix.argtypes = [p, i32, i32, p]
+        f = ctypes.c_float
+        L.cc_embed.restype = ctypes.c_int
+        L.cc_embed.argtypes = [p, i32, i64, i64, i64, p, i64, f, p, i64, p]
+        L.cc_embed_workspace_bytes.restype = sz
+        L.cc_embed_workspace_bytes.argtypes = [i64, i64, i64]
+        L.cc_embed_backward.restype = ctypes.c_int
+        L.cc_embed_backward.argtypes = [p, i32, i64, i64, i64, p, i64, f, p, i32, i64, i32, p, sz, p]
+        L.cc_gated_scan_workspace_bytes.restype = sz
+        L.cc_gated_scan_workspace_bytes.argtypes = [i64, i64, i64]
+        L.cc_gated_scan.restype = ctypes.c_int
+        L.cc_gated_scan.argtypes = [p, i64, i64, p, i64, i64, i32, i64, i64, i64, p, p, p, i64, i64, p, p, p, sz, p]
+        L.cc_gated_scan_backward.restype = ctypes.c_int
+        L.cc_gated_scan_backward.argtypes = [p, i64, i64, p, i64, i64, i32, i64, i64, i64, p, p, p, i64, i64, p, p, i64, i64, p, i64,
+                                             i64, p, p, sz, p]
+        logits = [p, i32, i64, i64, i64, i64, i64, p, p, i32, f]
+        L.cc_token_logprob.restype = ctypes.c_int
+        L.cc_token_logprob.argtypes = logits + [p, p, p]
+        L.cc_token_logprob_backward.restype = ctypes.c_int
+        L.cc_token_logprob_backward.argtypes = logits + [p, p, f, p, i64, i64, p]
+        L.cc_token_workspace_bytes.restype = sz
+        L.cc_token_workspace_bytes.argtypes = [i64, i64]
+        L.cc_policy_loss.restype = ctypes.c_int
+        L.cc_policy_loss.argtypes = logits + [p, p, p, i32, f, f, f, i32, f, p, p, p, i64, i64, p, sz, p]
+        L.cc_preference_loss.restype = ctypes.c_int
+        L.cc_preference_loss.argtypes = logits + [p, f, f, f, p, p, p, p, i64, i64, p, sz, p]
         L.cc_status_string.restype = ctypes.c_char_p
         L.cc_status_string.argtypes = [ctypes.c_int]
         L.cc_last_hip_error.restype = ctypes.c_int

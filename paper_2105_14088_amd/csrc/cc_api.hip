@@ -12,10 +12,8 @@ namespace {
 
 thread_local int g_last_hip_error = 0;
 
-int hip_fail(hipError_t e) {
-    g_last_hip_error = (int)e;
-    return CC_ERR_HIP;
-}
+using cc::hip_fail;
+using cc::poison_lds_if_asked;
 
 #define CC_HIP(expr)                                  \
     do {                                              \
@@ -62,16 +60,6 @@ __global__ __launch_bounds__(1024) void lds_poison_kernel() {
     for (int i = threadIdx.x; i < kLdsBytesPerCu / 4; i += 1024) p[i] = 0x7f7f7f7fu;
 }
 
-hipError_t poison_lds_if_asked(hipStream_t s) {
-    const char* v = getenv("CC_LDS_POISON");
-    if (!v || v[0] != '1') return hipSuccess;
-    hipError_t e = hipFuncSetAttribute((const void*)lds_poison_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       kLdsBytesPerCu);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(lds_poison_kernel, dim3(2048), dim3(1024), kLdsBytesPerCu, s);
-    return hipGetLastError();
-}
-
 // Device memory of cc_2opt_search_noalloc: one array per GPU, part of the code object, there from the moment the
 // library is loaded on a device until the process ends.  In host code the name `scratch` is only a handle for
 // hipGetSymbolAddress; the array's memory is reached through the per-device pointer that call returns.
@@ -98,6 +86,21 @@ int static_scratch(void** out) {
 }
 
 }  // namespace
+
+int cc::hip_fail(hipError_t e) {
+    g_last_hip_error = (int)e;
+    return CC_ERR_HIP;
+}
+
+hipError_t cc::poison_lds_if_asked(hipStream_t s) {
+    const char* v = getenv("CC_LDS_POISON");
+    if (!v || v[0] != '1') return hipSuccess;
+    hipError_t e = hipFuncSetAttribute((const void*)lds_poison_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       kLdsBytesPerCu);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(lds_poison_kernel, dim3(2048), dim3(1024), kLdsBytesPerCu, s);
+    return hipGetLastError();
+}
 
 extern "C" {
 

@@ -12,6 +12,10 @@ namespace cc {
 // the same bit for bit, only the time differs.
 bool force_general_path();
 
+// What the ABI files share: the calling thread's last HIP error, and the debug aid of cc.h (CC_LDS_POISON).
+int hip_fail(hipError_t e);
+hipError_t poison_lds_if_asked(hipStream_t s);
+
 hipError_t launch_ring_cost_batch(const int32_t* c, int N, bool is_max, const int32_t* perms, int64_t B,
                                   int64_t* out, hipStream_t s);
 hipError_t launch_ring_cost_batch_u8(const int32_t* c, int N, bool is_max, const uint8_t* perms, int64_t B,
@@ -134,5 +138,67 @@ hipError_t launch_rdswap(const int32_t* c, int N, int restarts, uint64_t seed, b
                          int64_t* costs, int32_t* moves, int32_t* flags, uint16_t* mat16, hipStream_t s);
 hipError_t launch_best_restart(const int64_t* costs, const int32_t* tours, int N, int restarts, int32_t* best_perm,
                                int64_t* best_cost, int32_t* best_restart, hipStream_t s);
+
+// ---- The order model (cc_model_api.hip checks; cc_embed.hip, cc_scan.hip, cc_token.hip compute).  Element types: cc.h, cc_dtype.
+constexpr int kF32 = 0, kF16 = 1, kBF16 = 2;
+
+struct EmbedCall {
+    const void* table;            // lookup only
+    void* grad_table;             // gradient only
+    const int32_t* ids;
+    void* out;                    // lookup: the rows written; gradient: the rows' gradients, read
+    int dtype, grad_dtype, accumulate;
+    int64_t V, D, n, table_stride, out_stride;
+    float scale;
+    void* workspace;
+};
+size_t embed_workspace_bytes(int64_t V, int64_t D, int64_t n);
+hipError_t launch_embed(const EmbedCall& c, hipStream_t s);
+hipError_t launch_embed_backward(const EmbedCall& c, hipStream_t s);
+
+constexpr int kScanChunk = 16;    // cc.h: CC_SCAN_CHUNK
+struct Strided {
+    void* p;
+    int64_t b, t;                 // elements from one sequence to the next, from one position to the next
+};
+struct ScanCall {
+    Strided x, gate;
+    int dtype;
+    int64_t B, T, D;
+    const int32_t* lengths;
+    const float* h0;              // forward
+    Strided h;                    // forward: h, backward: its gradient
+    float* last;                  // forward: written; backward: the gradient of the last state, read (or null)
+    float* states;                // [B, chunks, D]; forward: written (or null), backward: read
+    Strided grad_x, grad_gate;    // backward
+    float* grad_h0;               // backward, or null
+    void* workspace;
+};
+size_t scan_workspace_bytes(int64_t B, int64_t T, int64_t D);
+hipError_t launch_scan(const ScanCall& c, hipStream_t s);
+hipError_t launch_scan_backward(const ScanCall& c, hipStream_t s);
+
+enum TokenKind { kTokenForward, kTokenBackward, kTokenPolicy, kTokenPreference };
+struct TokenCall {
+    const void* logits;
+    void* grad;                   // or null
+    int dtype;
+    int64_t B, T, V, stride_b, stride_t, grad_stride_b, grad_stride_t;
+    const int32_t* tokens;
+    const uint8_t* mask;          // or null
+    bool placed;
+    float scale, grad_scale;
+    float* logprob;
+    float* rows;                  // [B, T, 2] row statistics, or null
+    const float* slope;           // backward: the gradient of logprob
+    const float *old, *ref, *advantage;
+    bool advantage_per_token, mean_of_orders;
+    float clip_low, clip_high, kl_coef, beta, smoothing;
+    float* stats;                 // policy: [3]; preference: [1]
+    float* margin;
+    void* workspace;
+};
+size_t token_workspace_bytes(int64_t B, int64_t T);
+hipError_t launch_token(TokenKind kind, const TokenCall& c, hipStream_t s);
 
 }  // namespace cc

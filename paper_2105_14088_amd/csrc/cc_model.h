@@ -1,0 +1,101 @@
+// Device-side helpers of the order-model kernels (cc_embed.hip, cc_scan.hip, cc_token.hip): element types, vectors of
+// elements at any element's address, reductions over groups of lanes.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ccm {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLn2 = 0.693147180559945309417;
+
+// Element types in memory; every computation is in float.  Conversion to 16 bits rounds to nearest, ties to even.
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(_Float16 v) { return (float)v; }
+__device__ __forceinline__ float widen(__bf16 v) { return __builtin_bit_cast(float, (uint32_t)__builtin_bit_cast(uint16_t, v) << 16); }
+template <class S>
+__device__ __forceinline__ S narrow(float v) { return (S)v; }
+
+// N elements that lie together.  Their address need only be a multiple of the element's size: gfx950 loads and stores
+// 16 bytes from any such address in one instruction, so a row of odd length needs no peeling.
+template <class S, int N>
+struct Pack {
+    S v[N];
+};
+template <int N, class S>
+__device__ __forceinline__ Pack<S, N> load_pack(const S* p) {
+    Pack<S, N> r;
+    __builtin_memcpy(&r, p, sizeof(r));
+    return r;
+}
+template <int N, class S>
+__device__ __forceinline__ void store_pack(S* p, const Pack<S, N>& r) { __builtin_memcpy(p, &r, sizeof(r)); }
+// The first `have` of N elements; the others read as zero, and are not written.
+template <int N, class S>
+__device__ __forceinline__ Pack<S, N> load_some(const S* p, int have) {
+    if (have >= N) return load_pack<N>(p);
+    Pack<S, N> r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.v[i] = i < have ? p[i] : (S)0.0f;
+    return r;
+}
+template <int N, class S>
+__device__ __forceinline__ void store_some(S* p, const Pack<S, N>& r, int have) {
+    if (have >= N) {
+        store_pack(p, r);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < have) p[i] = r.v[i];
+}
+
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// The value of the lane that differs in one bit of its number (1, 2, 4, 8), once the lanes below that bit agree.
+template <int BIT>
+__device__ __forceinline__ float other_lane(float v) {
+    constexpr int ctrl = BIT == 1 ? 0xB1 : BIT == 2 ? 0x4E : BIT == 4 ? 0x141 : 0x140;   // quad_perm, half mirror, mirror
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, 0xf, 0xf, true));
+}
+struct MaxOp {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct SumOp {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+// Over each aligned group of G lanes; every lane ends with its group's result.  All 64 lanes are active.
+template <int G, class Op>
+__device__ __forceinline__ float group_reduce(float v, Op op) {
+    if constexpr (G > 1) v = op(v, other_lane<1>(v));
+    if constexpr (G > 2) v = op(v, other_lane<2>(v));
+    if constexpr (G > 4) v = op(v, other_lane<4>(v));
+    if constexpr (G > 8) v = op(v, other_lane<8>(v));
+    if constexpr (G > 16) {
+        // exchanges the odd rows of 16 lanes of one register with the even rows of the other
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+        v = op(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+    }
+    if constexpr (G > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+        v = op(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+    }
+    return v;
+}
+template <int G>
+__device__ __forceinline__ float group_max(float v) { return group_reduce<G>(v, MaxOp()); }
+template <int G>
+__device__ __forceinline__ float group_sum(float v) { return group_reduce<G>(v, SumOp()); }
+
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+    return v;
+}
+__device__ __forceinline__ int wave_sum_i32(int v) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+    return v;
+}
+
+}  // namespace ccm

@@ -1,0 +1,702 @@
+// Log-probabilities of tokens and the losses on them (cc.h: cc_token_logprob, cc_token_logprob_backward, cc_policy_loss,
+// cc_preference_loss).
+//
+// For a row of V logits l_j, its candidates j, m the largest of their logits, k the row's token:
+//   e_j = exp(scale * (l_j - m)),  rest = sum over j != k of e_j,  total = rest + e_k
+//   logprob = scale * (l_k - m) - log(total),  p_j = e_j / total,  1 - p_k = rest / total
+//   d loss / d logits_j = scale * slope * ([j = k] - p_j),  slope = d loss / d logprob
+// rest is summed without the token's own term, so that 1 - p_k keeps its relative precision for a token that is all but
+// certain, and the log-probability is then -log1p(rest / e_k).  Logits are subtracted before they are scaled: equal ones
+// of any size then have equal terms.
+//
+// `placed` leaves out the nodes that an earlier position of the order has: a workgroup first writes for every node the
+// earliest position that has it, and a logit is a candidate if that position is not before its own.
+//
+// All of this reads a row once and writes a row at most: the kernels are bound by memory, so rows are read in vectors of
+// 16 bytes whatever their alignment, and every lane reduces what it holds before lanes are reduced.
+//   rows of up to 1024 logits: kept in the registers of a group of 1 to 64 lanes; loss and gradient in the same pass.
+//   longer rows: a workgroup per row.
+#include <hip/hip_runtime.h>
+
+#include "cc_internal.h"
+#include "cc_model.h"
+
+namespace cc {
+namespace {
+
+using namespace ccm;
+
+constexpr int kShortRow = 1024;       // cc.h: CC_MAX_N, the longest row with nodes left out
+constexpr int kThreads = 256;
+constexpr float kInf = __builtin_inff();
+
+struct Args {
+    const void* logits;
+    void* grad;
+    int64_t B, T, sb, st, gsb, gst;
+    int V;
+    const int32_t* tokens;
+    const uint8_t* mask;
+    float scale, grad_scale;
+    float scale2, scale2_rest;        // scale * log2(e) as a float, and what that leaves out
+    float lowest;                     // a difference of logits from which on a term is 0
+    float* logprob;
+    float2* rows;                     // {m, rest}
+    double* gaps;                     // logprob - ref in 64 bits, for the margins
+    const float* slope;
+    int slope_per_token;              // else one per order
+    const float *old_lp, *ref, *advantage;
+    int advantage_per_token, mean_of_orders;
+    float clip_low, clip_high, kl_coef;
+    const int* counts;                // positions that count, per order
+    const int2* parts;                // {positions, orders with any} per workgroup of the counting kernel
+    int part_count;
+    double* partial;                  // [workgroups][3]
+    int row_slots, order_slots;       // short rows: a workgroup's rows of an order, and orders
+    int chunks;                       // workgroups per order
+    int64_t units;                    // workgroups that have rows
+};
+
+// A launch's first dimension holds fewer than 2^32 threads: workgroups beyond kAcross go to the second.
+constexpr int64_t kAcross = 1 << 20;
+__device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * kAcross + blockIdx.x; }
+dim3 grid_of(int64_t units) {
+    return units <= kAcross ? dim3((unsigned)units) : dim3((unsigned)kAcross, (unsigned)((units + kAcross - 1) / kAcross));
+}
+
+// Row statistics of a row and its token, in the form that loss and gradient need.
+struct Row {
+    float m, rest, own, total;        // own: e_k
+    double logprob;
+};
+
+// m, rest and the token's logit make the row's log-probability, in 64 bits: sums of log-probabilities are compared with
+// sums of others, and 2^-24 of each term's size would be what is left of a difference.
+__device__ __forceinline__ Row finish_row(float m, float rest, float token_logit, float scale) {
+    Row r;
+    r.m = m;
+    r.rest = rest;
+    const double d = (double)scale * ((double)token_logit - (double)m);
+    r.own = exp_fast((float)d);
+    if (m == -kInf) {                 // no candidate at all: nothing is probable and nothing has a gradient
+        r.own = 0.0f;
+        r.total = 1.0f;
+        r.rest = 0.0f;
+        r.logprob = -(double)kInf;
+        return r;
+    }
+    r.total = rest + r.own;
+    if (rest < r.own) {
+        r.logprob = -(double)log1pf(rest / r.own);
+    } else {
+        r.logprob = d - log((double)r.total);
+    }
+    return r;
+}
+
+// exp(scale * x) for a difference x of two logits.  With the rest of the scale: what its rounding leaves out would make every term
+// of every row too small or every term too large, and sums of log-probabilities would show it.  Below `lowest` the result is 0; a
+// NaN stays one.
+__device__ __forceinline__ float term(const Args& a, float x) {
+    x = __builtin_elementwise_maximum(x, a.lowest);
+    return __builtin_amdgcn_exp2f(fmaf(x, a.scale2, x * a.scale2_rest));
+}
+
+// What a policy row adds to the loss, the divergence and the clipped share, and its slope.
+struct PolicyTerms {
+    float loss, kl, clipped, slope;
+};
+// What it needs of its position beside the logits.
+struct PolicyInputs {
+    float old_lp, ref, advantage;
+    int order_count;
+};
+__device__ __forceinline__ PolicyInputs policy_inputs(const Args& a, int64_t at, int64_t order) {
+    PolicyInputs r;
+    r.old_lp = a.old_lp[at];
+    r.ref = a.ref ? a.ref[at] : 0.0f;
+    r.advantage = a.advantage[a.advantage_per_token ? at : order];
+    r.order_count = a.mean_of_orders ? a.counts[order] : 1;
+    return r;
+}
+__device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, const PolicyInputs& in) {
+    PolicyTerms r;
+    const float ratio = expf((float)(lp - (double)in.old_lp));
+    const float free_gain = ratio * in.advantage, held = fminf(fmaxf(ratio, 1.0f - a.clip_low), 1.0f + a.clip_high) * in.advantage;
+    const bool clipped = held < free_gain;
+    r.clipped = clipped ? 1.0f : 0.0f;
+    r.loss = -(clipped ? held : free_gain);
+    r.slope = clipped ? 0.0f : -free_gain;
+    r.kl = 0.0f;
+    if (a.ref) {
+        const float away = (float)((double)in.ref - lp), grown = expm1f(away);
+        r.kl = grown - away;
+        r.loss += a.kl_coef * r.kl;
+        r.slope -= a.kl_coef * grown;
+    }
+    return r;
+}
+
+// Positions and orders that count, from the counting kernel's parts.  Every lane of the workgroup ends with them.
+template <int THREADS>
+__device__ __forceinline__ int2 all_counts(const Args& a, int* lds) {
+    int2 sum = {0, 0};
+    for (int i = threadIdx.x; i < a.part_count; i += THREADS) {
+        const int2 p = a.parts[i];
+        sum.x += p.x;
+        sum.y += p.y;
+    }
+    sum.x = wave_sum_i32(sum.x);
+    sum.y = wave_sum_i32(sum.y);
+    if ((threadIdx.x & 63) == 0) {
+        lds[(threadIdx.x >> 6) * 2] = sum.x;
+        lds[(threadIdx.x >> 6) * 2 + 1] = sum.y;
+    }
+    __syncthreads();
+    sum = {0, 0};
+    for (int w = 0; w < THREADS / 64; ++w) {
+        sum.x += lds[2 * w];
+        sum.y += lds[2 * w + 1];
+    }
+    return sum;
+}
+__device__ __forceinline__ float weight_of(const Args& a, const int2& all, int order_count) {
+    if (!a.mean_of_orders) return all.x > 0 ? 1.0f / (float)all.x : 0.0f;
+    return order_count > 0 ? 1.0f / ((float)order_count * (float)all.y) : 0.0f;
+}
+
+__device__ __forceinline__ bool counts_here(const Args& a, int64_t at, int token) {
+    return (uint32_t)token < (uint32_t)a.V && (!a.mask || a.mask[at] != 0);
+}
+
+// A workgroup's three sums, added in one order.
+template <int THREADS>
+__device__ __forceinline__ void store_partial(double* out, double s0, double s1, double s2, double* lds) {
+    s0 = wave_sum_f64(s0);
+    s1 = wave_sum_f64(s1);
+    s2 = wave_sum_f64(s2);
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+        lds[wave * 3] = s0;
+        lds[wave * 3 + 1] = s1;
+        lds[wave * 3 + 2] = s2;
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double s = 0.0;
+        for (int w = 0; w < THREADS / 64; ++w) s += lds[w * 3 + threadIdx.x];
+        out[threadIdx.x] = s;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ short rows
+
+// G lanes per row, K vectors of VEC logits per lane.  A workgroup has order_slots orders, row_slots rows of each.
+//
+// A lane's vector starts at element j0; one that would end beyond the row is moved back to end with it.  It then repeats elements of
+// the lane before it: these are left out of the sum, and their gradient is written twice, with the same value.  Every
+// lane so has a whole vector to load and store.
+//
+// The next row is loaded before the present one is reduced.
+template <class S, int VEC, int K>
+struct RowLoad {
+    Pack<S, VEC> p[K];
+    float token_logit;
+    float2 saved;
+    float slope;
+    PolicyInputs in;
+    int64_t order, at;
+    int k, t, o;
+    bool real, valid;
+};
+
+template <class S, int VEC, int G, int K, int KIND, bool PLACED>
+__global__ __launch_bounds__(kThreads) void short_rows_kernel(Args a) {
+    constexpr int GROUPS = kThreads / G;
+    extern __shared__ int first_at[];                 // PLACED: [order_slots][stride] earliest position of each node
+    __shared__ int count_lds[2 * kThreads / 64];
+    __shared__ double sum_lds[3 * kThreads / 64];
+    const int group = threadIdx.x / G, lane = threadIdx.x % G, V = a.V;
+    const int stride = (V + 7) & ~7;
+    const int64_t unit = workgroup();
+    if (unit >= a.units) return;
+    const int64_t first_order = a.order_slots > 1 ? unit * a.order_slots : unit / a.chunks;
+    const int first_row = a.order_slots > 1 ? 0 : (int)(unit - first_order * a.chunks) * a.row_slots;
+    const int orders = (int)min((int64_t)a.order_slots, a.B - first_order);
+    const int rows = (int)min((int64_t)a.row_slots, a.T - first_row);
+    if (PLACED) {
+        for (int i = threadIdx.x; i < orders * stride; i += kThreads) first_at[i] = 0x7fffffff;
+        __syncthreads();
+        const int upto = first_row + rows - 1;        // positions before the last row's
+        for (int i = threadIdx.x; i < orders * upto; i += kThreads) {
+            const int o = i / upto, t = i - o * upto;
+            const int k = a.tokens[(first_order + o) * a.T + t];
+            if ((uint32_t)k < (uint32_t)V) atomicMin(&first_at[o * stride + k], t);
+        }
+        __syncthreads();
+    }
+    int2 all = {0, 0};
+    if (KIND == kTokenPolicy) all = all_counts<kThreads>(a, count_lds);
+    double sum_loss = 0.0, sum_kl = 0.0, sum_clipped = 0.0;
+    const int slots = orders * rows;
+    const auto load = [&](int slot) {
+        RowLoad<S, VEC, K> r = {};
+        r.real = slot < slots;
+        r.o = r.real ? slot / rows : 0;
+        r.t = r.real ? first_row + slot - r.o * rows : 0;
+        r.order = first_order + r.o;
+        r.at = r.order * a.T + r.t;
+        r.k = r.real ? a.tokens[r.at] : -1;
+        r.valid = r.real && counts_here(a, r.at, r.k);
+        if (r.valid) {
+            const S* const row = (const S*)a.logits + r.order * a.sb + (int64_t)r.t * a.st;
+#pragma unroll
+            for (int c = 0; c < K; ++c) r.p[c] = load_pack<VEC>(row + min((c * G + lane) * VEC, V - VEC));
+            r.token_logit = widen(row[r.k]);
+            if (KIND == kTokenPolicy) r.in = policy_inputs(a, r.at, r.order);
+            if (KIND == kTokenBackward) {
+                r.saved = a.rows[r.at];
+                r.slope = a.slope[a.slope_per_token ? r.at : r.order];
+            }
+        }
+        return r;
+    };
+    RowLoad<S, VEC, K> next = load(group);
+    for (int base = 0; base < slots; base += GROUPS) {
+        const RowLoad<S, VEC, K> now = next;
+        if (base + GROUPS < slots) next = load(base + GROUPS + group);
+        float z[K * VEC];
+        // what is no candidate becomes minus infinity, before it is looked at
+#pragma unroll
+        for (int c = 0; c < K; ++c) {
+            const int j0 = min((c * G + lane) * VEC, V - VEC);
+            int first[VEC];
+            if (PLACED) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) first[i] = first_at[now.o * stride + j0 + i];
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                z[c * VEC + i] = widen(now.p[c].v[i]);
+                if (PLACED) z[c * VEC + i] = (int)(j0 + i == now.k) | (int)(first[i] >= now.t) ? z[c * VEC + i] : -kInf;
+            }
+        }
+        float m = now.saved.x, rest = now.saved.y;
+        if (KIND != kTokenBackward) {
+            m = -kInf;
+#pragma unroll
+            for (int e = 0; e < K * VEC; ++e) m = fmaxf(m, z[e]);
+            m = group_max<G>(m);
+        }
+        const float low = m == -kInf ? 0.0f : m;
+#pragma unroll
+        for (int e = 0; e < K * VEC; ++e) z[e] = term(a, z[e] - low);
+        if (KIND != kTokenBackward) {
+            rest = 0.0f;
+#pragma unroll
+            for (int c = 0; c < K; ++c) {
+                const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) rest += (int)(j0 + i >= j) & (int)(j0 + i != now.k) ? z[c * VEC + i] : 0.0f;
+            }
+            rest = group_sum<G>(rest);
+        }
+        const Row r = finish_row(m, rest, now.token_logit, a.scale);
+        float slope = now.slope;
+        if (KIND == kTokenPolicy && now.valid) {
+            const PolicyTerms p = policy_terms(a, r.logprob, now.in);
+            const float w = weight_of(a, all, now.in.order_count);
+            slope = w * p.slope;
+            if (lane == 0) {
+                sum_loss += (double)w * p.loss;
+                sum_kl += (double)w * p.kl;
+                sum_clipped += (double)w * p.clipped;
+            }
+        }
+        if (KIND != kTokenBackward && now.real && lane == 0) {
+            a.logprob[now.at] = now.valid ? (float)r.logprob : 0.0f;
+            if (a.rows) a.rows[now.at] = now.valid ? make_float2(r.m, r.rest) : make_float2(0.0f, 0.0f);
+            if (a.gaps) a.gaps[now.at] = now.valid ? r.logprob - (a.ref ? (double)a.ref[now.at] : 0.0) : 0.0;
+        }
+        if (KIND == kTokenForward || !a.grad || !now.real) continue;
+        const float pull = now.valid ? slope * a.scale * a.grad_scale / r.total : 0.0f;
+        S* const out = (S*)a.grad + now.order * a.gsb + (int64_t)now.t * a.gst;
+#pragma unroll
+        for (int c = 0; c < K; ++c) {
+            const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
+            if (j >= V) continue;
+            Pack<S, VEC> p;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float e = j0 + i == now.k ? r.rest : -z[c * VEC + i];
+                p.v[i] = narrow<S>((int)now.valid & (int)(e != 0.0f) ? pull * e : 0.0f);
+            }
+            store_pack(out + j0, p);
+        }
+    }
+    if (KIND == kTokenPolicy) store_partial<kThreads>(a.partial + unit * 3, sum_loss, sum_kl, sum_clipped, sum_lds);
+}
+
+// ------------------------------------------------------------------------------------------------------- long rows
+
+// A workgroup per row, which is read twice: once for its maximum and sum, kept as a running pair in each lane, once for
+// the gradient.
+constexpr int kLongThreads = 512;
+template <class S, int KIND>
+__global__ __launch_bounds__(kLongThreads) void long_rows_kernel(Args a) {
+    constexpr int VEC = 16 / sizeof(S), WAVES = kLongThreads / 64;
+    __shared__ float wave_m[WAVES], wave_rest[WAVES];
+    __shared__ int count_lds[2 * WAVES];
+    const int V = a.V;
+    const int64_t at = workgroup();
+    if (at >= a.B * a.T) return;
+    const int64_t order = at / a.T, t = at - order * a.T;
+    const int k = a.tokens[at];
+    const bool valid = counts_here(a, at, k);
+    const S* const row = (const S*)a.logits + order * a.sb + t * a.st;
+    S* const out = (S*)a.grad + order * a.gsb + t * a.gst;
+    if (!valid) {
+        if (KIND != kTokenBackward && threadIdx.x == 0) {
+            a.logprob[at] = 0.0f;
+            if (a.rows) a.rows[at] = make_float2(0.0f, 0.0f);
+            if (a.gaps) a.gaps[at] = 0.0;
+        }
+        if (KIND == kTokenPolicy && threadIdx.x < 3) a.partial[at * 3 + threadIdx.x] = 0.0;
+        if (KIND == kTokenForward || !a.grad) return;
+        Pack<S, VEC> p;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) p.v[i] = (S)0.0f;
+        for (int j = threadIdx.x * VEC; j < V; j += kLongThreads * VEC) store_some<VEC>(out + j, p, V - j);
+        return;
+    }
+    const float token_logit = widen(row[k]);
+    int2 all = {0, 0};
+    if (KIND == kTokenPolicy) all = all_counts<kLongThreads>(a, count_lds);
+    float m = -kInf, rest = 0.0f;
+    if (KIND == kTokenBackward) {
+        const float2 saved = a.rows[at];
+        m = saved.x;
+        rest = saved.y;
+        __syncthreads();              // the gradient may take the logits' place: the token's has been read by all
+    } else {
+#pragma unroll 4
+        for (int j = threadIdx.x * VEC; j < V; j += kLongThreads * VEC) {
+            const Pack<S, VEC> p = load_some<VEC>(row + j, V - j);
+            float z[VEC], top = m;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                z[i] = j + i < V ? widen(p.v[i]) : -kInf;
+                top = fmaxf(top, z[i]);
+            }
+            const float low = top == -kInf ? 0.0f : top;
+            rest *= term(a, m - low);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float e = term(a, z[i] - low);
+                rest += j + i == k ? 0.0f : e;
+            }
+            m = top;
+        }
+        const float lane_m = m;
+        m = group_max<64>(m);
+        float low = m == -kInf ? 0.0f : m;
+        rest = group_sum<64>(rest * term(a, lane_m - low));
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+            wave_m[wave] = m;
+            wave_rest[wave] = rest;
+        }
+        __syncthreads();
+        m = wave_m[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, wave_m[w]);
+        low = m == -kInf ? 0.0f : m;
+        rest = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) rest += wave_rest[w] * term(a, wave_m[w] - low);
+    }
+    const Row r = finish_row(m, rest, token_logit, a.scale);
+    float slope = 0.0f;
+    if (KIND == kTokenPolicy) {
+        const PolicyInputs in = policy_inputs(a, at, order);
+        const PolicyTerms p = policy_terms(a, r.logprob, in);
+        const float w = weight_of(a, all, in.order_count);
+        slope = w * p.slope;
+        if (threadIdx.x == 0) {
+            a.partial[at * 3] = (double)w * p.loss;
+            a.partial[at * 3 + 1] = (double)w * p.kl;
+            a.partial[at * 3 + 2] = (double)w * p.clipped;
+        }
+    } else if (KIND == kTokenBackward) {
+        slope = a.slope[a.slope_per_token ? at : order];
+    }
+    if (KIND != kTokenBackward && threadIdx.x == 0) {
+        a.logprob[at] = (float)r.logprob;
+        if (a.rows) a.rows[at] = make_float2(r.m, r.rest);
+        if (a.gaps) a.gaps[at] = r.logprob - (a.ref ? (double)a.ref[at] : 0.0);
+    }
+    if (KIND == kTokenForward || !a.grad) return;
+    const float pull = slope * a.scale * a.grad_scale / r.total;
+    const float low = m == -kInf ? 0.0f : m;
+    const bool none = m == -kInf;
+#pragma unroll 2
+    for (int j = threadIdx.x * VEC; j < V; j += kLongThreads * VEC) {
+        Pack<S, VEC> p = load_some<VEC>(row + j, V - j);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float e = none ? 0.0f : term(a, widen(p.v[i]) - low);
+            const float g = j + i == k ? r.rest : -e;
+            p.v[i] = narrow<S>(g != 0.0f ? pull * g : 0.0f);
+        }
+        store_some<VEC>(out + j, p, V - j);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- small kernels
+
+// counts[b]: positions of order b that count; parts[workgroup]: positions and orders with any.
+constexpr int kCountBlocks = 256;
+__global__ __launch_bounds__(kThreads) void count_kernel(const int32_t* __restrict__ tokens, const uint8_t* __restrict__ mask, int64_t B,
+                                                         int64_t T, int V, int* __restrict__ counts, int2* __restrict__ parts) {
+    __shared__ int lds[2 * kThreads / 64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int positions = 0, orders = 0;
+    for (int64_t b = (int64_t)blockIdx.x * (kThreads / 64) + wave; b < B; b += (int64_t)gridDim.x * (kThreads / 64)) {
+        int n = 0;
+#pragma unroll 4
+        for (int64_t t = lane; t < T; t += 64)
+            n += (uint32_t)tokens[b * T + t] < (uint32_t)V && (!mask || mask[b * T + t] != 0) ? 1 : 0;
+        n = wave_sum_i32(n);
+        if (lane == 0) counts[b] = n;
+        positions += n;
+        orders += n > 0 ? 1 : 0;
+    }
+    if (lane == 0) {
+        lds[2 * wave] = positions;
+        lds[2 * wave + 1] = orders;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int2 sum = {0, 0};
+        for (int w = 0; w < kThreads / 64; ++w) {
+            sum.x += lds[2 * w];
+            sum.y += lds[2 * w + 1];
+        }
+        parts[blockIdx.x] = sum;
+    }
+}
+
+// The policy loss's three sums over the workgroups' partial sums, in one order.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(const double* __restrict__ partial, int64_t count, float* __restrict__ stats) {
+    __shared__ double lds[3][kSumThreads / 64];
+    double s[3] = {0.0, 0.0, 0.0};
+    for (int64_t i = threadIdx.x; i < count; i += kSumThreads)
+#pragma unroll
+        for (int q = 0; q < 3; ++q) s[q] += partial[i * 3 + q];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        s[q] = wave_sum_f64(s[q]);
+        if ((threadIdx.x & 63) == 0) lds[q][threadIdx.x >> 6] = s[q];
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double sum = 0.0;
+        for (int w = 0; w < kSumThreads / 64; ++w) sum += lds[threadIdx.x][w];
+        stats[threadIdx.x] = (float)sum;
+    }
+}
+
+// A pair: its margin, its share of the loss, and the slope of its two sequences' log-probabilities.
+__global__ __launch_bounds__(kThreads) void pair_kernel(const double* __restrict__ gaps, int64_t pairs, int64_t T, float beta, float smoothing,
+                                                        float* __restrict__ margin, float* __restrict__ slope, double* __restrict__ losses) {
+    __shared__ double lds[kThreads / 64];
+    for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
+        double gap = 0.0;
+        for (int64_t t = threadIdx.x; t < T; t += kThreads) gap += gaps[p * T + t] - gaps[(p + pairs) * T + t];
+        gap = wave_sum_f64(gap);
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = gap;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            gap = 0.0;
+            for (int w = 0; w < kThreads / 64; ++w) gap += lds[w];
+            const double m = (double)beta * gap;
+            // softplus(x) = max(x, 0) + log1p(exp(-|x|))
+            const double tail = log1p(exp(-fabs(m)));
+            const double wrong = fmax(-m, 0.0) + tail, right = fmax(m, 0.0) + tail;
+            losses[p] = ((1.0 - (double)smoothing) * wrong + (double)smoothing * right) / (double)pairs;
+            const double away = 1.0 / (1.0 + exp(m)), by = 1.0 / (1.0 + exp(-m));
+            const float s = (float)((double)beta / (double)pairs * ((double)smoothing * by - (1.0 - (double)smoothing) * away));
+            margin[p] = (float)m;
+            slope[p] = s;
+            slope[p + pairs] = -s;
+        }
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(kSumThreads) void pair_sum_kernel(const double* __restrict__ losses, int64_t pairs, float* __restrict__ loss) {
+    __shared__ double lds[kSumThreads / 64];
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < pairs; i += kSumThreads) s += losses[i];
+    s = wave_sum_f64(s);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.0;
+        for (int w = 0; w < kSumThreads / 64; ++w) s += lds[w];
+        *loss = (float)s;
+    }
+}
+
+// --------------------------------------------------------------------------------------------------------- launches
+
+size_t up256(size_t x) { return (x + 255u) & ~(size_t)255u; }
+
+// Workspace: [counts or slopes: 4 B][parts][gaps or partial sums: 24 BT + 24][row statistics: 8 BT][losses: 8 B]
+struct Layout {
+    size_t counts, parts, sums, rows, losses, total;
+};
+Layout layout(int64_t B, int64_t T) {
+    const size_t b = (size_t)B, bt = (size_t)B * (size_t)T;
+    Layout l;
+    l.counts = 0;
+    l.parts = l.counts + up256(4 * b);
+    l.sums = l.parts + up256(sizeof(int2) * kCountBlocks);
+    l.rows = l.sums + up256(24 * bt + 24);
+    l.losses = l.rows + up256(8 * bt);
+    l.total = l.losses + up256(8 * b);
+    return l;
+}
+
+template <class S, int VEC, int G, int K, int KIND>
+int64_t launch_short(Args& a, bool placed, hipStream_t s) {
+    constexpr int groups = kThreads / G;
+    // A workgroup takes several orders where they have fewer positions than it has groups of lanes; else up to eight rows
+    // per group of one order, fewer where that would leave compute units idle.
+    const int64_t T = a.T;
+    if (T * 2 <= groups) {
+        int64_t orders = groups / T;
+        const int64_t stride = (a.V + 7) & ~7;
+        if (placed && orders * stride > 8192) orders = 8192 / stride;
+        a.order_slots = (int)orders;
+        a.row_slots = (int)T;
+        a.chunks = 1;
+    } else {
+        int64_t passes = 8;
+        while (passes > 1 && a.B * ((T + groups * passes - 1) / (groups * passes)) < 2048) passes /= 2;
+        a.order_slots = 1;
+        a.row_slots = (int)(groups * passes < T ? groups * passes : T);
+        a.chunks = (int)((T + a.row_slots - 1) / a.row_slots);
+    }
+    const int64_t blocks = a.order_slots > 1 ? (a.B + a.order_slots - 1) / a.order_slots : a.B * a.chunks;
+    a.units = blocks;
+    if (placed)
+        hipLaunchKernelGGL((short_rows_kernel<S, VEC, G, K, KIND, true>), grid_of(blocks), dim3(kThreads),
+                           sizeof(int) * a.order_slots * ((a.V + 7) & ~7), s, a);
+    else
+        hipLaunchKernelGGL((short_rows_kernel<S, VEC, G, K, KIND, false>), grid_of(blocks), dim3(kThreads), 0, s, a);
+    return blocks;
+}
+
+// One pass over the rows; returns the number of workgroups.
+template <class S, int KIND>
+int64_t launch_rows(Args& a, bool placed, hipStream_t s) {
+    constexpr int VEC = 16 / sizeof(S);
+    const int V = a.V;
+    if (V <= kShortRow) {
+        if (V < VEC) return launch_short<S, 1, 8, 1, KIND>(a, placed, s);
+        if (V <= 8 * VEC) return launch_short<S, VEC, 8, 1, KIND>(a, placed, s);
+        if (V <= 16 * VEC) return launch_short<S, VEC, 16, 1, KIND>(a, placed, s);
+        if (V <= 32 * VEC) return launch_short<S, VEC, 32, 1, KIND>(a, placed, s);
+        if (V <= 64 * VEC) return launch_short<S, VEC, 64, 1, KIND>(a, placed, s);
+        if (V <= 128 * VEC) return launch_short<S, VEC, 64, 2, KIND>(a, placed, s);
+        if constexpr (VEC == 4) return launch_short<S, VEC, 64, 4, KIND>(a, placed, s);
+    }
+    const int64_t rows = a.B * a.T;
+    hipLaunchKernelGGL((long_rows_kernel<S, KIND>), grid_of(rows), dim3(kLongThreads), 0, s, a);
+    return rows;
+}
+
+template <class S>
+hipError_t run(TokenKind kind, const TokenCall& c, hipStream_t s) {
+    Args a = {};
+    a.logits = c.logits;
+    a.grad = c.grad;
+    a.B = c.B; a.T = c.T; a.V = (int)c.V;
+    a.sb = c.stride_b; a.st = c.stride_t;
+    a.gsb = c.grad_stride_b; a.gst = c.grad_stride_t;
+    a.tokens = c.tokens;
+    a.mask = c.mask;
+    a.scale = c.scale;
+    const double scale2 = (double)c.scale * 1.4426950408889634074;
+    a.scale2 = (float)scale2;
+    a.scale2_rest = (float)(scale2 - (double)a.scale2);
+    a.lowest = (float)(-256.0 / scale2);
+    a.grad_scale = c.grad_scale;
+    a.logprob = c.logprob;
+    a.rows = (float2*)c.rows;
+    a.slope = c.slope;
+    a.slope_per_token = 1;
+    a.old_lp = c.old;
+    a.ref = c.ref;
+    a.advantage = c.advantage;
+    a.advantage_per_token = c.advantage_per_token;
+    a.mean_of_orders = c.mean_of_orders;
+    a.clip_low = c.clip_low;
+    a.clip_high = c.clip_high;
+    a.kl_coef = c.kl_coef;
+    const bool any = c.B > 0 && c.T > 0;
+    if (kind == kTokenForward) {
+        if (any) launch_rows<S, kTokenForward>(a, c.placed, s);
+        return hipGetLastError();
+    }
+    if (kind == kTokenBackward) {
+        if (any) launch_rows<S, kTokenBackward>(a, c.placed, s);
+        return hipGetLastError();
+    }
+    const Layout l = layout(c.B, c.T);
+    char* const w = (char*)c.workspace;
+    if (kind == kTokenPolicy) {
+        int64_t partials = 0;
+        a.partial = (double*)(w + l.sums);
+        if (any) {
+            const int64_t need = (c.B + kThreads / 64 - 1) / (kThreads / 64);
+            a.part_count = (int)(need < kCountBlocks ? need : kCountBlocks);
+            a.counts = (const int*)(w + l.counts);
+            a.parts = (const int2*)(w + l.parts);
+            hipLaunchKernelGGL(count_kernel, dim3((unsigned)a.part_count), dim3(kThreads), 0, s, c.tokens, c.mask, c.B, c.T, a.V,
+                               (int*)(w + l.counts), (int2*)(w + l.parts));
+            partials = launch_rows<S, kTokenPolicy>(a, c.placed, s);
+        }
+        hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(kSumThreads), 0, s, a.partial, partials, c.stats);
+        return hipGetLastError();
+    }
+    // preference: log-probabilities, pairs, gradient
+    const int64_t pairs = c.B / 2;
+    a.rows = (float2*)(w + l.rows);
+    a.gaps = (double*)(w + l.sums);
+    if (any) launch_rows<S, kTokenForward>(a, c.placed, s);
+    if (pairs > 0)
+        hipLaunchKernelGGL(pair_kernel, dim3((unsigned)(pairs < 65536 ? pairs : 65536)), dim3(kThreads), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin,
+                           (float*)(w + l.counts), (double*)(w + l.losses));
+    hipLaunchKernelGGL(pair_sum_kernel, dim3(1), dim3(kSumThreads), 0, s, (const double*)(w + l.losses), pairs, c.stats);
+    if (any && c.grad) {
+        a.slope = (const float*)(w + l.counts);
+        a.slope_per_token = 0;
+        launch_rows<S, kTokenBackward>(a, c.placed, s);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t token_workspace_bytes(int64_t B, int64_t T) { return layout(B, T).total; }
+
+hipError_t launch_token(TokenKind kind, const TokenCall& c, hipStream_t s) {
+    if (c.dtype == kF32) return run<float>(kind, c, s);
+    if (c.dtype == kF16) return run<_Float16>(kind, c, s);
+    return run<__bf16>(kind, c, s);
+}
+
+}  // namespace cc

@@ -1,0 +1,352 @@
+"""Log-probabilities, policy loss and preference loss against their definitions in 64 bits."""
+import pytest
+import torch
+
+import order_model_reference as ref
+import paper_2105_14088_amd as cc
+from gpu_util import say
+from order_model_reference import DTYPES, U, finish, within
+
+pytestmark = [pytest.mark.gpu, pytest.mark.usefixtures("built_library")]
+
+SCALE = 0.75
+
+
+def make(b, t, v, dtype, seed=0, placed=False, masked=True):
+    g = torch.Generator().manual_seed(seed)
+    logits = (2 * torch.randn(b, t, v, generator=g)).to(dtype)
+    if placed:
+        tokens = torch.rand(b, v, generator=g).argsort(1)[:, :t].to(torch.int32)
+    else:
+        tokens = torch.randint(0, v, (b, t), generator=g, dtype=torch.int32)
+    mask = None
+    if masked:
+        mask = torch.rand(b, t, generator=g) < 0.8
+        mask[0] = False
+        mask[-1] = True
+    return logits, tokens.contiguous(), mask
+
+
+def dev(*ts):
+    return [None if x is None else x.cuda() for x in ts]
+
+
+def check_logprob(logits, tokens, mask, placed, seed=1):
+    dtype = logits.dtype
+    p, rest, lp, valid, rel = ref.rows(logits, tokens, mask, placed, SCALE)
+    z, k, m = dev(logits, tokens, mask)
+    got, rows = cc.cc_token_logprob(z, k, m, placed, SCALE)
+    within(got, lp, finish(lp, lp.abs() * U + rel, torch.float32), "logprob")
+    slope = torch.randn(lp.shape, generator=torch.Generator().manual_seed(seed))
+    want = ref.grad_logits(p, rest, tokens, valid, slope.double() * SCALE * 4)
+    grad = cc.cc_token_logprob_backward(z, k, m, placed, SCALE, rows, slope.cuda(), grad_scale=4.0)
+    within(grad, want, finish(want, want.abs() * (2 * rel + 8 * U), dtype), "gradient")
+    place = z.clone()
+    cc.cc_token_logprob_backward(place, k, m, placed, SCALE, rows, slope.cuda(), grad_scale=4.0, grad_logits=place)
+    assert torch.equal(place, grad)
+
+
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [1, 2, 7, 8, 9, 31, 33, 64, 65, 100, 129, 255, 257, 500, 513, 1000, 1024])
+def test_orders(v, name):
+    t = min(v, 40)
+    say(f"logprob placed v={v} t={t} {name}")
+    check_logprob(*make(3, t, v, DTYPES[name], v, placed=True), True)
+
+
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("b,t,v", [(1, 1, 1), (2, 3, 5), (300, 1, 12), (5, 7, 1023), (2, 3, 1025), (2, 2, 2048), (2, 3, 4099), (1, 3, 16385),
+                                   (2, 2, 50001), (1, 2, 65536), (1, 2, 131079), (1, 1, 300007)])
+def test_any_vocabulary(b, t, v, name):
+    say(f"logprob b={b} t={t} v={v} {name}")
+    check_logprob(*make(b, t, v, DTYPES[name], v, masked=b > 1), False)
+
+
+@pytest.mark.parametrize("b,t,v", [(1, 64, 64), (40, 8, 8), (200, 3, 100), (2, 130, 300), (9, 1, 1024)])
+def test_whole_orders_and_short_ones(b, t, v):
+    check_logprob(*make(b, t, v, torch.float32, 5, placed=True, masked=b > 1), True)
+
+
+def test_tokens_that_are_none():
+    """Out of range tokens do not count; a node that stands twice is left out after its first place only for others."""
+    logits, tokens, _ = make(3, 12, 20, torch.float32, 3, placed=True, masked=False)
+    tokens[0, 3], tokens[0, 4], tokens[1, 0], tokens[2, 7] = -1, 20, 2 ** 31 - 1, -(2 ** 31)
+    tokens[2, 5] = tokens[2, 1]
+    for placed in (False, True):
+        check_logprob(logits, tokens, None, placed)
+
+
+def test_what_is_left_out_has_no_effect():
+    """NaN and infinities at nodes that are placed and in positions that do not count change nothing."""
+    logits, tokens, mask = make(4, 30, 30, torch.float32, 6, placed=True)
+    dirty = logits.clone()
+    for b in range(4):
+        for t in range(30):
+            for at, j in enumerate(tokens[b, :t].tolist()):
+                dirty[b, t, j] = (float("nan"), float("inf"), float("-inf"))[at % 3]
+            if not mask[b, t]:
+                dirty[b, t] = float("nan")
+    slope = torch.randn(4, 30).cuda()
+    outs = []
+    for z in (logits, dirty):
+        lp, rows = cc.cc_token_logprob(z.cuda(), tokens.cuda(), mask.cuda(), True, SCALE)
+        outs.append((lp, cc.cc_token_logprob_backward(z.cuda(), tokens.cuda(), mask.cuda(), True, SCALE, rows, slope)))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    assert torch.isfinite(outs[1][1]).all()
+
+
+@pytest.mark.parametrize("v", [6, 300, 5000])
+def test_logits_of_minus_infinity_and_of_the_lowest_value(v):
+    logits, tokens, _ = make(2, 4, v, torch.float32, 8, masked=False)
+    logits[0, 0, 1:] = float("-inf")
+    tokens[0, 0] = 0                                            # the only candidate: certain
+    logits[0, 1] = float("-inf")                                # none at all
+    logits[0, 2, :3] = float("-inf")
+    tokens[0, 2] = 1                                            # impossible
+    logits[0, 3] = torch.finfo(torch.float32).min / 2
+    logits[1, 0, : v // 2] = torch.finfo(torch.float32).min
+    tokens[1, 0] = v - 1
+    check_logprob(logits, tokens, None, False)
+    lp, _ = cc.cc_token_logprob(logits.cuda(), tokens.cuda(), None, False, SCALE)
+    assert float(lp[0, 0]) == 0 and float(lp[0, 1]) == float("-inf") and float(lp[0, 2]) == float("-inf")
+
+
+def test_a_nan_stays_in_its_row():
+    logits, tokens, _ = make(2, 3, 2000, torch.float32, 8, masked=False)
+    clean, _ = cc.cc_token_logprob(logits.cuda(), tokens.cuda(), None, False, SCALE)
+    logits[1, 1, 77] = float("nan")
+    lp, _ = cc.cc_token_logprob(logits.cuda(), tokens.cuda(), None, False, SCALE)
+    assert torch.isnan(lp[1, 1]) and int(torch.isnan(lp).sum()) == 1
+    keep = ~torch.isnan(lp)
+    assert torch.equal(lp[keep], clean[keep])
+
+
+def test_strides_and_odd_addresses():
+    for b, t, v in ((3, 9, 33), (2, 3, 1501)):
+        for dtype in (torch.float32, torch.bfloat16):
+            logits, tokens, mask = make(b, t, v, dtype, 9)
+            room = torch.full((t * b * (v + 2) + 1,), 3.0, dtype=dtype, device="cuda")
+            odd = room[1:].view(t, b, v + 2).transpose(0, 1)[..., 1:v + 1]
+            odd.copy_(logits.cuda())
+            k, m = dev(tokens, mask)
+            lp, rows = cc.cc_token_logprob(odd, k, m, False, SCALE)
+            want, want_rows = cc.cc_token_logprob(logits.cuda(), k, m, False, SCALE)
+            assert torch.equal(lp, want) and torch.equal(rows, want_rows)
+            slope = torch.randn(b, t, device="cuda")
+            grads = torch.full_like(room, 3.0)
+            into = grads[1:].view(t, b, v + 2).transpose(0, 1)[..., 1:v + 1]
+            cc.cc_token_logprob_backward(odd, k, m, False, SCALE, rows, slope, grad_logits=into)
+            assert torch.equal(into, cc.cc_token_logprob_backward(logits.cuda(), k, m, False, SCALE, rows, slope))
+            assert (grads[1:].view(t, b, v + 2)[..., 0] == 3).all() and (grads[1:].view(t, b, v + 2)[..., -1] == 3).all()
+
+
+def test_one_row_of_logits_for_all_orders():
+    """A policy that does not look at the order's past: logits with a stride of zero over orders."""
+    logits, tokens, mask = make(6, 10, 10, torch.float32, 4, placed=True)
+    shared = logits[:1].cuda().expand(6, 10, 10)
+    k, m = dev(tokens, mask)
+    lp, rows = cc.cc_token_logprob(shared, k, m, True, SCALE)
+    assert torch.equal(lp, cc.cc_token_logprob(shared.contiguous(), k, m, True, SCALE)[0])
+
+
+def test_offsets_beyond_32_bits():
+    b, t, v = 2, 2, 1500
+    apart = (1 << 31) + 64
+    room = torch.empty(apart + t * v, dtype=torch.bfloat16, device="cuda")
+    logits, tokens, _ = make(b, t, v, torch.bfloat16, 2)
+    far = torch.as_strided(room, (b, t, v), (apart, v, 1))
+    far.copy_(logits.cuda())
+    say("token: orders 4.3 GB apart")
+    for cut in (v, 900):
+        z, k = far[..., :cut], tokens.clamp(max=cut - 1).cuda()
+        near = z.contiguous()
+        lp, rows = cc.cc_token_logprob(z, k, None, False, SCALE)
+        want, rows2 = cc.cc_token_logprob(near, k, None, False, SCALE)
+        assert torch.equal(lp, want)
+        slope = torch.randn(b, t, device="cuda")
+        want = cc.cc_token_logprob_backward(near, k, None, False, SCALE, rows2, slope)
+        kept = near.clone()
+        cc.cc_token_logprob_backward(z, k, None, False, SCALE, rows, slope, grad_logits=z)
+        assert torch.equal(z, want)
+        z.copy_(kept)
+
+
+# ---------------------------------------------------------------------------------------------------------- policy
+
+
+def policy_inputs(lp, per_token, seed=0):
+    """Old log-probabilities whose ratios stay clear of the clip's borders (0.8, 1.25): the slope jumps there."""
+    g = torch.Generator().manual_seed(seed)
+    ratio = torch.tensor([0.5, 0.7, 0.9, 1.0, 1.1, 1.2, 1.4, 2.0], dtype=torch.float64)
+    ratio = ratio[torch.randint(0, 8, lp.shape, generator=g)]
+    old = torch.where(torch.isfinite(lp), lp, 0.0) - torch.log(ratio)
+    other = torch.where(torch.isfinite(lp), lp, 0.0) + 0.3 * torch.randn(lp.shape, generator=g)
+    adv = torch.randn(lp.shape if per_token else lp.shape[:1], generator=g)
+    return old.float(), other.float(), adv
+
+
+def check_policy(logits, tokens, mask, placed, mean, per_token=False, with_ref=True, coef=0.1):
+    dtype = logits.dtype
+    b, t, v = logits.shape
+    p, rest, lp, valid, rel = ref.rows(logits, tokens, mask, placed, SCALE)
+    old, other, adv = policy_inputs(lp, per_token)
+    if not with_ref:
+        other = None
+    stats, slope, moved, total = ref.policy(lp, valid, old, other, adv, 0.2, 0.25, coef, mean)
+    scale = 128.0 if dtype is torch.float16 else 1.0
+    z, k, m, o, r, a = dev(logits, tokens, mask, old, other, adv)
+    res = cc.cc_policy_loss(z, k, o, a, r, m, placed, SCALE, 0.2, 0.25, coef, mean, grad_scale=scale)
+    lp_err = lp.abs() * U + rel
+    within(res.logprob, lp, finish(lp, lp_err, torch.float32), "logprob")
+    # an exponential of a difference: the difference's error, its rounding, the function's last bits; weights and products
+    slope_err = moved * (rel + 16 * U)
+    loss_err = float(total) * (rel + 16 * U)
+    want_stats_err = torch.tensor([loss_err, loss_err / max(coef, 1e-3) + 16 * U * float(stats[1]), 16 * U * float(stats[2])], dtype=torch.float64)
+    within(res.stats, stats, finish(stats, want_stats_err, torch.float32) + stats.abs() * U, "stats")
+    want = ref.grad_logits(p, rest, tokens, valid, slope * SCALE * scale)
+    err = ref.grad_logits(p, -rest, tokens, valid, slope_err * SCALE * scale).abs() + want.abs() * (2 * rel + 8 * U)
+    within(res.grad_logits, want, finish(want, err, dtype), "gradient")
+    again = cc.cc_policy_loss(z, k, o, a, r, m, placed, SCALE, 0.2, 0.25, coef, mean, grad_scale=scale)
+    assert all(torch.equal(x, y) for x, y in zip(res, again))
+    bare = cc.cc_policy_loss(z, k, o, a, r, m, placed, SCALE, 0.2, 0.25, coef, mean, grad=False)
+    assert bare.grad_logits is None and torch.equal(bare.stats, res.stats) and torch.equal(bare.logprob, res.logprob)
+    place = z.clone()
+    cc.cc_policy_loss(place, k, o, a, r, m, placed, SCALE, 0.2, 0.25, coef, mean, grad_scale=scale, grad_logits=place)
+    assert torch.equal(place, res.grad_logits)
+
+
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("mean", ["tokens", "orders"])
+@pytest.mark.parametrize("b,t,v,placed", [(1, 1, 1, False), (3, 8, 8, True), (50, 5, 9, True), (5, 64, 64, True), (2, 33, 500, True),
+                                          (4, 6, 1000, False), (3, 5, 1030, False), (2, 3, 40001, False)])
+def test_policy(b, t, v, placed, mean, name):
+    say(f"policy b={b} t={t} v={v} placed={placed} {mean} {name}")
+    check_policy(*make(b, t, v, DTYPES[name], v + t, placed, masked=b > 1), placed, mean)
+
+
+def test_policy_with_token_advantages_and_without_a_reference():
+    args = make(6, 20, 50, torch.float32, 1, True)
+    check_policy(*args, True, "tokens", per_token=True)
+    check_policy(*args, True, "orders", with_ref=False, coef=0.0)
+    args = make(3, 4, 3001, torch.bfloat16, 1)
+    check_policy(*args, False, "orders", per_token=True)
+    check_policy(*args, False, "tokens", with_ref=False, coef=0.0)
+
+
+@pytest.mark.parametrize("v", [20, 2000])
+def test_policy_of_nothing_is_zero(v):
+    logits, tokens, _ = make(3, 4, v, torch.float32)
+    logits[:] = float("nan")
+    z, k = dev(logits, tokens)
+    ones = torch.ones(3, 4, device="cuda")
+    for mean in ("tokens", "orders"):
+        res = cc.cc_policy_loss(z, k, ones, ones[:, 0].contiguous(), ones, torch.zeros(3, 4, dtype=torch.bool, device="cuda"), mean=mean)
+        assert (res.stats == 0).all() and (res.logprob == 0).all() and (res.grad_logits == 0).all()
+    res = cc.cc_policy_loss(z[:0], k[:0], ones[:0], ones[:0, 0].contiguous())
+    assert (res.stats == 0).all() and res.grad_logits.shape == (0, 4, v)
+
+
+def test_policy_gradient_against_differences():
+    """Both losses are in 32 bits: their difference is off by at most two of the loss's bounds, over twice the step."""
+    b, t, v, eps = 6, 20, 20, 2.0 ** -5
+    logits, tokens, mask = make(b, t, v, torch.float32, 3, True)
+    _, _, lp, valid, rel = ref.rows(logits, tokens, mask, True, SCALE)
+    old, other, adv = policy_inputs(lp, False)
+    direction = torch.randn(logits.shape, generator=torch.Generator().manual_seed(2)) * 0.02
+    args = dev(tokens, old, adv, other, mask)
+    def run(z):
+        return cc.cc_policy_loss(z.cuda(), *args, True, SCALE, 0.2, 0.25, 0.1)
+    slope = float((run(logits).grad_logits.cpu().double() * direction).sum())
+    up, down = run(logits + eps * direction), run(logits - eps * direction)
+    estimate = (float(up.stats[0]) - float(down.stats[0])) / (2 * eps)
+    total = float(ref.policy(lp, valid, old, other, adv, 0.2, 0.25, 0.1, "tokens")[3])
+    noise = (total * (rel + 16 * U) + abs(float(up.stats[0])) * U) / eps
+    assert float(up.stats[2]) == float(down.stats[2])           # no ratio crossed a border
+    assert abs(estimate - slope) <= noise + 1e-2 * abs(slope)
+
+
+# ------------------------------------------------------------------------------------------------------ preference
+
+
+def check_preference(logits, tokens, mask, placed, with_ref=True, smoothing=0.1, beta=0.25):
+    dtype = logits.dtype
+    pairs = logits.shape[0] // 2
+    p, rest, lp, valid, rel = ref.rows(logits, tokens, mask, placed, SCALE)
+    other = (lp + 0.2 * torch.randn(lp.shape, generator=torch.Generator().manual_seed(4))).float() if with_ref else None
+    if not with_ref:
+        beta = 0.02
+    beta32, smoothing32 = float(torch.tensor(beta)), float(torch.tensor(smoothing))
+    loss, margin, slope = ref.preference(lp, valid, other, beta32, smoothing32)
+    scale = 64.0 if dtype is torch.float16 else 1.0
+    z, k, m, r = dev(logits, tokens, mask, other)
+    res = cc.cc_preference_loss(z, k, r, m, placed, SCALE, beta, smoothing, grad_scale=scale)
+    within(res.logprob, lp, finish(lp, lp.abs() * U + rel, torch.float32), "logprob")
+    # a margin sums what each position may be off; the loss's derivative is at most 1, the slope's a quarter of beta / pairs
+    per_order = (valid * rel).sum(1)
+    margin_err = beta32 * (per_order[:pairs] + per_order[pairs:])
+    within(res.margin, margin, finish(margin, margin_err + margin.abs() * U, torch.float32), "margin")
+    within(res.loss, loss, finish(loss, margin_err.mean() + loss * U, torch.float32), "loss")
+    slope_err = (beta32 / pairs * (margin_err / 4)).repeat(2).unsqueeze(1) + slope.abs() * U
+    want = ref.grad_logits(p, rest, tokens, valid, slope * SCALE * scale)
+    err = ref.grad_logits(p, -rest, tokens, valid, slope_err.expand_as(slope) * SCALE * scale).abs() + want.abs() * (2 * rel + 8 * U)
+    within(res.grad_logits, want, finish(want, err, dtype), "gradient")
+    again = cc.cc_preference_loss(z, k, r, m, placed, SCALE, beta, smoothing, grad_scale=scale)
+    assert all(torch.equal(x, y) for x, y in zip(res, again))
+    bare = cc.cc_preference_loss(z, k, r, m, placed, SCALE, beta, smoothing, grad=False)
+    assert bare.grad_logits is None and torch.equal(bare.loss, res.loss) and torch.equal(bare.margin, res.margin)
+    place = z.clone()
+    cc.cc_preference_loss(place, k, r, m, placed, SCALE, beta, smoothing, grad_scale=scale, grad_logits=place)
+    assert torch.equal(place, res.grad_logits)
+
+
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("b,t,v,placed", [(2, 1, 3, False), (4, 8, 8, True), (60, 4, 10, True), (6, 100, 100, True), (2, 30, 1000, True),
+                                          (4, 7, 1500, False), (2, 3, 40001, False)])
+def test_preference(b, t, v, placed, name):
+    say(f"preference b={b} t={t} v={v} placed={placed} {name}")
+    check_preference(*make(b, t, v, DTYPES[name], v + t, placed), placed)
+
+
+def test_preference_without_a_reference_and_with_smoothing_at_its_ends():
+    args = make(6, 20, 50, torch.float32, 1, True)
+    check_preference(*args, True, with_ref=False)
+    check_preference(*args, True, smoothing=0.0)
+    check_preference(*args, True, smoothing=1.0)
+
+
+def test_preference_of_nothing():
+    z, k = dev(*make(4, 3, 50, torch.float32)[:2])
+    none = torch.zeros(4, 3, dtype=torch.uint8, device="cuda")
+    res = cc.cc_preference_loss(z, k, None, none)
+    assert abs(float(res.loss) - 0.6931471805599453) < 1e-7 and (res.margin == 0).all() and (res.grad_logits == 0).all()
+    res = cc.cc_preference_loss(z[:0], k[:0])
+    assert float(res.loss) == 0 and res.margin.shape == (0,)
+    res = cc.cc_preference_loss(z[:, :0], k[:, :0])
+    assert abs(float(res.loss) - 0.6931471805599453) < 1e-7 and (res.margin == 0).all()
+
+
+def test_a_preference_beyond_doubt():
+    """Margins in the hundreds: the loss is the margin or nothing, and nothing overflows."""
+    logits, tokens, _ = make(2, 200, 30, torch.float32, 5, masked=False)
+    other = torch.zeros(2, 200)
+    other[0] = -60.0
+    for flip in (False, True):
+        r = other.flip(0) if flip else other
+        res = cc.cc_preference_loss(*dev(logits, tokens), r.cuda(), beta=1.0)
+        assert torch.isfinite(res.loss) and torch.isfinite(res.grad_logits).all()
+        assert (float(res.loss) == 0) != flip and abs(float(res.margin[0])) > 1000
+
+
+def test_preference_gradient_against_differences():
+    b, t, v, eps = 6, 20, 20, 2.0 ** -5
+    logits, tokens, mask = make(b, t, v, torch.float32, 3, True)
+    _, _, lp, valid, rel = ref.rows(logits, tokens, mask, True, SCALE)
+    direction = torch.randn(logits.shape, generator=torch.Generator().manual_seed(2)) * 0.1
+    k, m, r = dev(tokens, mask, (lp + 0.1).float())
+    def run(z):
+        return cc.cc_preference_loss(z.cuda(), k, r, m, True, SCALE, 0.25, 0.1)
+    slope = float((run(logits).grad_logits.cpu().double() * direction).sum())
+    up, down = float(run(logits + eps * direction).loss), float(run(logits - eps * direction).loss)
+    per_order = (valid * rel).sum(1)
+    noise = (0.25 * float((per_order[:3] + per_order[3:]).mean()) + abs(up) * U) / eps
+    assert abs((up - down) / (2 * eps) - slope) <= noise + 1e-2 * abs(slope)
