@@ -16,6 +16,8 @@
 // gate, which it has in registers anyway, and then goes back through them.  That reads less than h itself would take.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "cc_internal.h"
 #include "cc_model.h"
 
@@ -49,7 +51,7 @@ struct Args {
     void *h, *grad_x, *grad_gate;
     int64_t xb, xt, gb, gt, hb, ht, dxb, dxt, dgb, dgt;
     int64_t B, T, D;
-    int pairs;                        // threads per sequence: two channels each
+    int lanes;                        // threads per sequence
     const int32_t* lengths;
     const float* h0;
     float* last;
@@ -63,177 +65,260 @@ struct Args {
     const float* starts;              // [segments][B * D], null with one segment
 };
 
-// What a thread owns.
+// What a thread owns: C neighbouring channels of one sequence.  Where the last thread of a row would reach beyond it, it is moved
+// back to end with the row: it then computes a channel of the thread before it as well, and stores it again, the same value.  No load
+// and no store depends on a lane's place in the row, and all of a chunk's are in flight together.
+template <int C>
 struct Lane {
-    int64_t b, first, n;              // sequence; first channel's place in [B, D]; positions that count
-    int d, have;                      // first channel, 1 or 2 of them
+    uint32_t b;
+    int d;
+    int64_t n;                        // positions that count
     bool real;
-    __device__ __forceinline__ Lane(const Args& a) {
-        const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-        b = id / a.pairs;
+    __device__ __forceinline__ explicit Lane(const Args& a) {
+        const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+        b = id / (uint32_t)a.lanes;
         real = b < a.B;
-        d = 2 * (int)(id - b * a.pairs);
-        have = min(2, (int)(a.D - d));
-        first = b * a.D + d;
+        d = min(C * (int)(id - b * (uint32_t)a.lanes), (int)a.D - C);
         n = a.T;
         if (real && a.lengths) n = min(a.T, (int64_t)max(a.lengths[b], 0));
     }
 };
 
-__device__ __forceinline__ void read2(const float* p, int have, float v[2]) {
-    v[0] = p[0];
-    v[1] = have > 1 ? p[1] : 0.0f;
+// A tensor's rows as a thread sees them: a base that is the same in all lanes, kept in scalar registers and moved from chunk to
+// row there, and a lane's offset in bytes of type Off.  With offsets of 32 bits (chosen where the tensor's sequences and a chunk's
+// rows lie within them) a tensor takes one vector register for addresses; pointers of 64 bits to 16 rows of five tensors would
+// take 160.
+template <class S, int C, class Off>
+struct Rows {
+    S* base;
+    int64_t stride;
+    Off lane;
+    __device__ __forceinline__ Rows(void* p, int64_t apart, int64_t stride_, const Lane<C>& l)
+        : base((S*)p), stride(stride_), lane(((Off)l.b * (Off)apart + (Off)l.d) * (Off)sizeof(S)) {}
+    // The base at position t, in scalar registers (the compiler would keep, and advance, one per lane).
+    __device__ __forceinline__ S* at(int64_t t) const {
+        const uint64_t v = (uint64_t)(base + t * stride);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+        return (S*)(__attribute__((address_space(1))) S*)(((uint64_t)hi << 32) | lo);
+    }
+    __device__ __forceinline__ Pack<S, C> load(const S* p, int i) const {
+        return load_pack<C>((const S*)((const char*)(p + i * stride) + lane));
+    }
+    __device__ __forceinline__ Pack<S, C> load_own(const S* p, int i) const {      // i differs between lanes
+        return load_pack<C>((const S*)((const char*)p + (Off)(lane + (Off)i * ((Off)stride * (Off)sizeof(S)))));
+    }
+    __device__ __forceinline__ void store(S* p, int i, const float v[C]) const {
+        Pack<S, C> r;
+#pragma unroll
+        for (int c = 0; c < C; ++c) r.v[c] = narrow<S>(v[c]);
+        store_pack((S*)((char*)(p + i * stride) + lane), r);
+    }
+    // A chunk's rows from position t on.  Of a chunk that does not count as a whole, the others' places hold the last row that does.
+    template <bool FULL>
+    __device__ __forceinline__ void load_chunk(int64_t t, int inside, Pack<S, C> rows[L]) const {
+        const S* const p = at(t);
+#pragma unroll
+        for (int i = 0; i < L; ++i) rows[i] = FULL ? load(p, i) : load_own(p, min(i, inside - 1));
+    }
+};
+// Makes the compiler take a value as new, so that nothing computed from it before is kept.
+template <class S, int C>
+__device__ __forceinline__ void forget(Pack<S, C>& p) {
+    if constexpr (sizeof(p) % 4 == 0) {
+        uint32_t w[sizeof(p) / 4];
+        __builtin_memcpy(w, &p, sizeof(p));
+#pragma unroll
+        for (unsigned k = 0; k < sizeof(p) / 4; ++k) asm("" : "+v"(w[k]));
+        __builtin_memcpy(&p, w, sizeof(p));
+    }
 }
-__device__ __forceinline__ void write2(float* p, int have, const float v[2]) {
-    p[0] = v[0];
-    if (have > 1) p[1] = v[1];
+template <int C, class Off>
+__device__ __forceinline__ void read(const Rows<float, C, Off>& r, int64_t t, float v[C]) {
+    const Pack<float, C> p = r.load(r.at(t), 0);
+#pragma unroll
+    for (int c = 0; c < C; ++c) v[c] = p.v[c];
 }
-template <class S>
-__device__ __forceinline__ void write2(S* p, int have, float v0, float v1) {
-    Pack<S, 2> r;
-    r.v[0] = narrow<S>(v0);
-    r.v[1] = narrow<S>(v1);
-    store_some<2>(p, r, have);
-}
+template <int C, class Off>
+__device__ __forceinline__ void write(const Rows<float, C, Off>& r, int64_t t, const float v[C]) { r.store(r.at(t), 0, v); }
+
+// What the length leaves of a chunk: all of it in all lanes, or something in some.
+struct Part {
+    int count, inside;                // positions of the segment, positions that count
+    bool full;
+    __device__ __forceinline__ Part(int64_t t0, int64_t to, int64_t end) {
+        count = (int)min((int64_t)L, to - t0);
+        inside = (int)max((int64_t)0, min((int64_t)L, end - t0));
+        full = __all(inside >= L);
+    }
+};
 
 // Forward walk.  SUMMARY: only the segment's product of keeps and what it adds; the last segment needs none.
-template <class S, bool SUMMARY>
+template <class S, int C, class Off, bool SUMMARY>
 __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
-    const Lane l(a);
+    const Lane<C> l(a);
     if (!l.real) return;
     const int seg = blockIdx.y;
-    const int64_t from = seg * a.segment, to = min(a.T, from + a.segment);
-    const S* const x = (const S*)a.x + l.b * a.xb + l.d;
-    const S* const g = (const S*)a.gate + l.b * a.gb + l.d;
-    S* const out = SUMMARY ? nullptr : (S*)a.h + l.b * a.hb + l.d;
-    const int64_t row = a.B * a.D;
-    float h[2] = {0.0f, 0.0f}, product[2] = {1.0f, 1.0f};
+    const int64_t from = seg * a.segment, to = min(a.T, from + a.segment), end = min(to, l.n);
+    const Rows<S, C, Off> x((void*)a.x, a.xb, a.xt, l), g((void*)a.gate, a.gb, a.gt, l), out(a.h, a.hb, a.ht, l);
+    const Rows<float, C, Off> states(a.states, a.chunks * a.D, a.D, l), last(a.last, a.D, 0, l), h0((void*)a.h0, a.D, 0, l);
+    const Rows<float, C, Off> starts((void*)a.starts, a.D, a.B * a.D, l), products(a.products, a.D, a.B * a.D, l), sums(a.sums, a.D, a.B * a.D, l);
+    float h[C] = {}, product[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) product[c] = 1.0f;
     if (!SUMMARY) {
-        if (a.starts) read2(a.starts + seg * row + l.first, l.have, h);
-        else if (a.h0) read2(a.h0 + l.first, l.have, h);
+        if (a.starts) read<C>(starts, seg, h);
+        else if (a.h0) read<C>(h0, 0, h);
     }
-    for (int64_t t0 = from; t0 < to; t0 += L) {
-        if (!SUMMARY && a.states) write2(a.states + (l.b * a.chunks + t0 / L) * a.D + l.d, l.have, h);
-        const int count = (int)min((int64_t)L, to - t0), inside = (int)min((int64_t)L, l.n - t0);
-        Pack<S, 2> xs[L], gs[L];
-        if (inside >= L) {
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                xs[i] = load_some<2>(x + (t0 + i) * a.xt, l.have);
-                gs[i] = load_some<2>(g + (t0 + i) * a.gt, l.have);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < L; ++i)
-                if (i < inside) {
-                    xs[i] = load_some<2>(x + (t0 + i) * a.xt, l.have);
-                    gs[i] = load_some<2>(g + (t0 + i) * a.gt, l.have);
-                }
+    const auto walk = [&](auto whole, int64_t t0, const Part& part) {
+        constexpr bool FULL = decltype(whole)::value;
+        Pack<S, C> xs[L], gs[L];
+        if (FULL || part.inside > 0) {
+            x.template load_chunk<FULL>(t0, part.inside, xs);
+            g.template load_chunk<FULL>(t0, part.inside, gs);
         }
+        S* const to_row = SUMMARY ? nullptr : out.at(t0);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            if (i < inside) {
+            const bool in = FULL || i < part.inside;
+            float shown[C];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const Gates gate(widen(gs[i].v[c]));
-                    h[c] = gate.step(h[c], widen(xs[i].v[c]));
-                    if (SUMMARY) product[c] = gate.keep(product[c]);
-                }
+            for (int c = 0; c < C; ++c) {
+                const Gates gate(widen(gs[i].v[c]));
+                const float next = gate.step(h[c], widen(xs[i].v[c]));
+                h[c] = in ? next : h[c];
+                if (SUMMARY) product[c] = in ? gate.keep(product[c]) : product[c];
+                shown[c] = in ? next : 0.0f;
             }
-            if (!SUMMARY && i < count) {
-                const bool in = i < inside;
-                write2(out + (t0 + i) * a.ht, l.have, in ? h[0] : 0.0f, in ? h[1] : 0.0f);
-            }
+            if (!SUMMARY && (FULL || i < part.count)) out.store(to_row, i, shown);
         }
+    };
+    for (int64_t t0 = from; t0 < to; t0 += L) {
+        const Part part(t0, to, end);
+        if (!SUMMARY && a.states) write<C>(states, t0 / L, h);
+        if (part.full) walk(std::true_type(), t0, part);
+        else walk(std::false_type(), t0, part);
     }
     if (SUMMARY) {
-        write2(a.products + seg * row + l.first, l.have, product);
-        write2(a.sums + seg * row + l.first, l.have, h);
+        write<C>(products, seg, product);
+        write<C>(sums, seg, h);
     } else if (seg == a.segments - 1 && a.last) {
-        write2(a.last + l.first, l.have, h);
+        write<C>(last, 0, h);
     }
 }
 
 // Backward walk.  SUMMARY: only the segment's product of keeps and what it sends back; the first segment needs none.
-template <class S, bool SUMMARY>
-__global__ __launch_bounds__(kThreads) void scan_backward_kernel(Args a) {
-    const Lane l(a);
+template <class S, int C, class Off, bool SUMMARY>
+__global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) void scan_backward_kernel(Args a) {
+    const Lane<C> l(a);
     if (!l.real) return;
     const int seg = SUMMARY ? blockIdx.y + 1 : blockIdx.y;
-    const int64_t from = seg * a.segment, to = min(a.T, from + a.segment);
-    const S* const x = (const S*)a.x + l.b * a.xb + l.d;
-    const S* const g = (const S*)a.gate + l.b * a.gb + l.d;
-    const S* const dh = (const S*)a.h_in + l.b * a.hb + l.d;
-    const int64_t row = a.B * a.D;
-    float f[2] = {0.0f, 0.0f}, product[2] = {1.0f, 1.0f};
-    if (!SUMMARY) {
-        if (a.starts) read2(a.starts + seg * row + l.first, l.have, f);
-        else if (a.last_grad) read2(a.last_grad + l.first, l.have, f);
-    }
-    for (int64_t t0 = to > from ? from + (to - from - 1) / L * L : from - L; t0 >= from; t0 -= L) {
-        const int count = (int)min((int64_t)L, to - t0), inside = (int)min((int64_t)L, l.n - t0);
-        Pack<S, 2> xs[L], gs[L], ds[L];
+    const int64_t from = seg * a.segment, to = min(a.T, from + a.segment), end = min(to, l.n);
+    const Rows<S, C, Off> x((void*)a.x, a.xb, a.xt, l), g((void*)a.gate, a.gb, a.gt, l), dh((void*)a.h_in, a.hb, a.ht, l);
+    const Rows<S, C, Off> dx_out(a.grad_x, a.dxb, a.dxt, l), dg_out(a.grad_gate, a.dgb, a.dgt, l);
+    const Rows<float, C, Off> states(a.states, a.chunks * a.D, a.D, l), last_grad((void*)a.last_grad, a.D, 0, l), grad_h0(a.grad_h0, a.D, 0, l);
+    const Rows<float, C, Off> starts((void*)a.starts, a.D, a.B * a.D, l), products(a.products, a.D, a.B * a.D, l), sums(a.sums, a.D, a.B * a.D, l);
+    float f[C] = {}, product[C];
 #pragma unroll
-        for (int i = 0; i < L; ++i)
-            if (i < inside) {
-                gs[i] = load_some<2>(g + (t0 + i) * a.gt, l.have);
-                ds[i] = load_some<2>(dh + (t0 + i) * a.ht, l.have);
-                if (!SUMMARY) xs[i] = load_some<2>(x + (t0 + i) * a.xt, l.have);
+    for (int c = 0; c < C; ++c) product[c] = 1.0f;
+    if (!SUMMARY) {
+        if (a.starts) read<C>(starts, seg, f);
+        else if (a.last_grad) read<C>(last_grad, 0, f);
+    }
+    const auto walk = [&](auto whole, int64_t t0, const Part& part) {
+        constexpr bool FULL = decltype(whole)::value;
+        Pack<S, C> xs[L], gs[L], ds[L];
+        float before[L][C], h[C] = {};
+        if (FULL || part.inside > 0) {
+            g.template load_chunk<FULL>(t0, part.inside, gs);
+            dh.template load_chunk<FULL>(t0, part.inside, ds);
+            if (!SUMMARY) {
+                x.template load_chunk<FULL>(t0, part.inside, xs);
+                read<C>(states, t0 / L, h);
             }
-        float before[L][2], h[2];
+        }
         if (!SUMMARY) {
-            read2(a.states + (l.b * a.chunks + t0 / L) * a.D + l.d, l.have, h);
 #pragma unroll
             for (int i = 0; i < L; ++i)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int c = 0; c < C; ++c) {
                     before[i][c] = h[c];
-                    if (i < inside) h[c] = Gates(widen(gs[i].v[c])).step(h[c], widen(xs[i].v[c]));
+                    if (i + 1 < L) h[c] = Gates(widen(gs[i].v[c])).step(h[c], widen(xs[i].v[c]));   // of use where position i + 1 counts
                 }
         }
+        // The gates are made again on the way back: kept, a chunk's would take 128 registers and three quarters of the wavefronts.
+        if (!SUMMARY) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) forget(gs[i]);
+        }
+        S* const dx_row = SUMMARY ? nullptr : dx_out.at(t0);
+        S* const dg_row = SUMMARY ? nullptr : dg_out.at(t0);
 #pragma unroll
         for (int i = L - 1; i >= 0; --i) {
-            float dx[2] = {0.0f, 0.0f}, dg[2] = {0.0f, 0.0f};
-            if (i < inside) {
+            const bool in = FULL || i < part.inside;
+            float dx[C], dg[C];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const Gates gate(widen(gs[i].v[c]));
-                    const float lambda = widen(ds[i].v[c]) + f[c];
-                    f[c] = gate.keep(lambda);
-                    if (SUMMARY) {
-                        product[c] = gate.keep(product[c]);
-                    } else {
-                        dx[c] = gate.take(lambda);
-                        dg[c] = gate.keep(gate.take(lambda * (before[i][c] - widen(xs[i].v[c]))));
-                    }
+            for (int c = 0; c < C; ++c) {
+                const Gates gate(widen(gs[i].v[c]));
+                const float lambda = widen(ds[i].v[c]) + f[c];
+                f[c] = in ? gate.keep(lambda) : f[c];
+                if (SUMMARY) {
+                    product[c] = in ? gate.keep(product[c]) : product[c];
+                } else {
+                    dx[c] = in ? gate.take(lambda) : 0.0f;
+                    dg[c] = in ? gate.keep(gate.take(lambda * (before[i][c] - widen(xs[i].v[c])))) : 0.0f;
                 }
             }
-            if (!SUMMARY && i < count) {
-                write2((S*)a.grad_x + l.b * a.dxb + (t0 + i) * a.dxt + l.d, l.have, dx[0], dx[1]);
-                write2((S*)a.grad_gate + l.b * a.dgb + (t0 + i) * a.dgt + l.d, l.have, dg[0], dg[1]);
+            if (!SUMMARY && (FULL || i < part.count)) {
+                dx_out.store(dx_row, i, dx);
+                dg_out.store(dg_row, i, dg);
             }
         }
+    };
+    for (int64_t t0 = to > from ? from + (to - from - 1) / L * L : from - L; t0 >= from; t0 -= L) {
+        const Part part(t0, to, end);
+        if (part.full) walk(std::true_type(), t0, part);
+        else walk(std::false_type(), t0, part);
     }
     if (SUMMARY) {
-        write2(a.products + seg * row + l.first, l.have, product);
-        write2(a.sums + seg * row + l.first, l.have, f);
+        write<C>(products, seg, product);
+        write<C>(sums, seg, f);
     } else if (seg == 0 && a.grad_h0) {
-        write2(a.grad_h0 + l.first, l.have, f);
+        write<C>(grad_h0, 0, f);
     }
 }
 
-// Chains the segments: what each starts from, left in the place of its product.  Forward from the first segment, backward
-// from the last.
+// Chains the segments: what each starts from, left in the place of its product.  Forward from the first segment, backward from the
+// last.  A workgroup has 64 channels and cuts the segments into kParts parts: each part's product and sum, then the parts in
+// turn, then each part's segments from what it starts with.
+constexpr int kParts = 16;
 template <bool BACKWARD>
-__global__ __launch_bounds__(kThreads) void scan_chain_kernel(float* products, const float* sums, const float* first, int segments, int64_t row) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= row) return;
-    float h = first ? first[i] : 0.0f;
+__global__ __launch_bounds__(64 * kParts) void scan_chain_kernel(float* products, const float* sums, const float* first, int segments, int64_t row) {
+    __shared__ float part_product[kParts][64], part_sum[kParts][64];
+    const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+    const int64_t i = (int64_t)blockIdx.x * 64 + lane;
+    const bool real = i < row;
+    const int each = (segments + kParts - 1) / kParts, from = min(segments, part * each), to = min(segments, from + each);
+    const auto place = [&](int s) { return (int64_t)(BACKWARD ? segments - 1 - s : s) * row + i; };
+    float product = 1.0f, sum = 0.0f;
+    if (real) {
 #pragma unroll 8
-    for (int s = 0; s < segments; ++s) {
-        const int64_t at = (BACKWARD ? segments - 1 - s : s) * row + i;
-        const float p = s + 1 < segments ? products[at] : 0.0f, q = s + 1 < segments ? sums[at] : 0.0f;   // the last is not summed up
-        products[at] = h;
+        for (int s = from; s < to; ++s) {
+            if (s + 1 == segments) break;             // the last is not summed up
+            const float p = products[place(s)];
+            sum = fmaf(p, sum, sums[place(s)]);
+            product *= p;
+        }
+    }
+    part_product[part][lane] = product;
+    part_sum[part][lane] = sum;
+    __syncthreads();
+    if (!real) return;
+    float h = first ? first[i] : 0.0f;
+    for (int p = 0; p < part; ++p) h = fmaf(part_product[p][lane], h, part_sum[p][lane]);
+#pragma unroll 8
+    for (int s = from; s < to; ++s) {
+        const float p = s + 1 < segments ? products[place(s)] : 0.0f, q = s + 1 < segments ? sums[place(s)] : 0.0f;
+        products[place(s)] = h;
         h = fmaf(p, h, q);
     }
 }
@@ -260,13 +345,13 @@ Split split(int64_t B, int64_t T, int64_t D) {
 
 size_t up256(size_t x) { return (x + 255u) & ~(size_t)255u; }
 
-Args arguments(const ScanCall& c, const Split& s) {
+Args arguments(const ScanCall& c, const Split& s, int channels) {
     Args a = {};
     a.x = c.x.p; a.xb = c.x.b; a.xt = c.x.t;
     a.gate = c.gate.p; a.gb = c.gate.b; a.gt = c.gate.t;
     a.hb = c.h.b; a.ht = c.h.t;
     a.B = c.B; a.T = c.T; a.D = c.D;
-    a.pairs = (int)((c.D + 1) / 2);
+    a.lanes = (int)((c.D + channels - 1) / channels);
     a.lengths = c.lengths;
     a.states = c.states;
     a.chunks = (c.T + L - 1) / L;
@@ -280,42 +365,64 @@ Args arguments(const ScanCall& c, const Split& s) {
     return a;
 }
 
-template <class S>
+template <class S, int C, class Off>
 hipError_t forward(const ScanCall& c, hipStream_t s) {
     const Split p = split(c.B, c.T, c.D);
-    Args a = arguments(c, p);
+    Args a = arguments(c, p, C);
     a.h = c.h.p;
     a.h0 = c.h0;
     a.last = c.last;
-    const unsigned blocks = (unsigned)((c.B * a.pairs + kThreads - 1) / kThreads);
+    const unsigned blocks = (unsigned)((c.B * a.lanes + kThreads - 1) / kThreads);
     const int64_t row = c.B * c.D;
     if (p.segments > 1) {
-        hipLaunchKernelGGL((scan_kernel<S, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
-        hipLaunchKernelGGL((scan_chain_kernel<false>), dim3((unsigned)((row + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a.products,
-                           a.sums, c.h0, p.segments, row);
+        hipLaunchKernelGGL((scan_kernel<S, C, Off, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((scan_chain_kernel<false>), dim3((unsigned)((row + 63) / 64)), dim3(64 * kParts), 0, s, a.products, a.sums, c.h0,
+                           p.segments, row);
     }
-    hipLaunchKernelGGL((scan_kernel<S, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((scan_kernel<S, C, Off, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
-template <class S>
+template <class S, int C, class Off>
 hipError_t backward(const ScanCall& c, hipStream_t s) {
     const Split p = split(c.B, c.T, c.D);
-    Args a = arguments(c, p);
+    Args a = arguments(c, p, C);
     a.h_in = c.h.p;
     a.last_grad = c.last;
     a.grad_x = c.grad_x.p; a.dxb = c.grad_x.b; a.dxt = c.grad_x.t;
     a.grad_gate = c.grad_gate.p; a.dgb = c.grad_gate.b; a.dgt = c.grad_gate.t;
     a.grad_h0 = c.grad_h0;
-    const unsigned blocks = (unsigned)((c.B * a.pairs + kThreads - 1) / kThreads);
+    const unsigned blocks = (unsigned)((c.B * a.lanes + kThreads - 1) / kThreads);
     const int64_t row = c.B * c.D;
     if (p.segments > 1) {
-        hipLaunchKernelGGL((scan_backward_kernel<S, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
-        hipLaunchKernelGGL((scan_chain_kernel<true>), dim3((unsigned)((row + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a.products,
-                           a.sums, (const float*)c.last, p.segments, row);
+        hipLaunchKernelGGL((scan_backward_kernel<S, C, Off, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((scan_chain_kernel<true>), dim3((unsigned)((row + 63) / 64)), dim3(64 * kParts), 0, s, a.products, a.sums,
+                           (const float*)c.last, p.segments, row);
     }
-    hipLaunchKernelGGL((scan_backward_kernel<S, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((scan_backward_kernel<S, C, Off, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
     return hipGetLastError();
+}
+
+// Whether a lane's offsets fit 32 bits: sequences and channels of a tensor, and a chunk's rows.
+bool near(const Strided& t, const ScanCall& c, int64_t bytes) {
+    return (double)bytes * ((double)(c.B > 0 ? c.B - 1 : 0) * (double)t.b + (double)c.D + (double)L * (double)t.t) < 4294967296.0;
+}
+bool all_near(const ScanCall& c, bool backward) {
+    const int64_t e = c.dtype == kF32 ? 4 : 2, chunks = (c.T + L - 1) / L;
+    const Strided states = {nullptr, chunks * c.D, c.D};
+    return near(c.x, c, e) && near(c.gate, c, e) && near(c.h, c, e) && near(states, c, 4) &&
+           (!backward || (near(c.grad_x, c, e) && near(c.grad_gate, c, e)));
+}
+
+template <class S, bool BACKWARD>
+hipError_t choose(const ScanCall& c, hipStream_t s) {
+    // A thread that is moved back reads the first state of a channel that another thread owns: not where that one may have
+    // overwritten it with the last.
+    const void *in = BACKWARD ? (const void*)c.last : (const void*)c.h0, *out = BACKWARD ? (const void*)c.grad_h0 : (const void*)c.last;
+    const bool in_place = in && in == out;
+    if (c.D == 1 || ((c.D & 1) && in_place)) return BACKWARD ? backward<S, 1, uint64_t>(c, s) : forward<S, 1, uint64_t>(c, s);
+    if (all_near(c, BACKWARD)) return BACKWARD ? backward<S, 2, uint32_t>(c, s) : forward<S, 2, uint32_t>(c, s);
+    return BACKWARD ? backward<S, 2, uint64_t>(c, s) : forward<S, 2, uint64_t>(c, s);
 }
 
 }  // namespace
@@ -326,15 +433,15 @@ size_t scan_workspace_bytes(int64_t B, int64_t T, int64_t D) {
 }
 
 hipError_t launch_scan(const ScanCall& c, hipStream_t s) {
-    if (c.dtype == kF32) return forward<float>(c, s);
-    if (c.dtype == kF16) return forward<_Float16>(c, s);
-    return forward<__bf16>(c, s);
+    if (c.dtype == kF32) return choose<float, false>(c, s);
+    if (c.dtype == kF16) return choose<_Float16, false>(c, s);
+    return choose<__bf16, false>(c, s);
 }
 
 hipError_t launch_scan_backward(const ScanCall& c, hipStream_t s) {
-    if (c.dtype == kF32) return backward<float>(c, s);
-    if (c.dtype == kF16) return backward<_Float16>(c, s);
-    return backward<__bf16>(c, s);
+    if (c.dtype == kF32) return choose<float, true>(c, s);
+    if (c.dtype == kF16) return choose<_Float16, true>(c, s);
+    return choose<__bf16, true>(c, s);
 }
 
 }  // namespace cc
