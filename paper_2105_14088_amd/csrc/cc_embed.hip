@@ -39,14 +39,16 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(const S* __restrict__ t
         const int id = ids[first + r];
         const int left = D - (int)at;
         Pack<S, VEC> p;
+        float f[VEC];
         if ((uint32_t)id < (uint32_t)V) {
             p = load_some<VEC>(table + (int64_t)id * table_stride + at, left);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) p.v[k] = narrow<S>(widen(p.v[k]) * scale);
+            for (int k = 0; k < VEC; ++k) f[k] = p.get(k) * scale;
         } else {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) p.v[k] = (S)0.0f;
+            for (int k = 0; k < VEC; ++k) f[k] = 0.0f;
         }
+        p = Pack<S, VEC>::from(f);
         store_some<VEC>(out + (first + r) * out_stride + at, p, left);
     }
 }
@@ -59,12 +61,6 @@ constexpr int kTile = 4096, kSortWaves = 4, kSortThreads = kSortWaves * 64, kPer
 constexpr int kMaxBits = 11;
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t V) { return (uint32_t)id < V ? (uint32_t)id : V; }
-
-// Between accesses of a wavefront's lanes to each other's words of LDS: the hardware keeps their order, the compiler has to.
-__device__ __forceinline__ void wave_order() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
 
 // hist[tile][digit]: how many tokens of the tile have the digit
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t* __restrict__ ids, int64_t n, uint32_t V, int shift,
@@ -200,15 +196,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t*
 
 template <int VEC, class GT>
 __device__ __forceinline__ void write_row(GT* p, const float* acc, float scale, bool accumulate, int left) {
-    Pack<GT, VEC> r;
+    float f[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) f[k] = scale * acc[k];
     if (accumulate) {
         const Pack<GT, VEC> old = load_some<VEC>(p, left);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) r.v[k] = narrow<GT>(widen(old.v[k]) + scale * acc[k]);
-    } else {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) r.v[k] = narrow<GT>(scale * acc[k]);
+        for (int k = 0; k < VEC; ++k) f[k] = old.get(k) + scale * acc[k];
     }
+    const Pack<GT, VEC> r = Pack<GT, VEC>::from(f);
     store_some<VEC>(p, r, left);
 }
 
@@ -268,10 +264,7 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restric
         if (current >= a.V) return;                   // no token
         if (open || goes_on) {
             float* const p = open ? slot : slot + a.D;
-            Pack<float, VEC> r;
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) r.v[k] = acc[k];
-            store_some<VEC>(p, r, left);
+            store_some<VEC>(p, Pack<float, VEC>::from(acc), left);
         } else {
             write_row<VEC>(out + (int64_t)current * a.out_stride + at, acc, a.scale, a.accumulate != 0, left);
         }
@@ -296,7 +289,7 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restric
             }
             if (key[u] < a.V)
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) acc[k] += widen(row[u].v[k]);
+                for (int k = 0; k < VEC; ++k) acc[k] += row[u].get(k);
         }
     }
     flush(current == after);
@@ -317,12 +310,12 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(GT* __restrict__ o
             float acc[VEC];
             Pack<float, VEC> p = load_some<VEC>(a.partial + (seg * 2 + 1) * a.D + at, left);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) acc[k] = p.v[k];
+            for (int k = 0; k < VEC; ++k) acc[k] = p.get(k);
 #pragma unroll 4
             for (int64_t s = seg + 1; s <= last; ++s) {
                 p = load_some<VEC>(a.partial + s * 2 * a.D + at, left);
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) acc[k] += p.v[k];
+                for (int k = 0; k < VEC; ++k) acc[k] += p.get(k);
             }
             write_row<VEC>(out + (int64_t)key * a.out_stride + at, acc, a.scale, a.accumulate != 0, left);
         }

@@ -108,10 +108,7 @@ struct Rows {
         return load_pack<C>((const S*)((const char*)p + (Off)(lane + (Off)i * ((Off)stride * (Off)sizeof(S)))));
     }
     __device__ __forceinline__ void store(S* p, int i, const float v[C]) const {
-        Pack<S, C> r;
-#pragma unroll
-        for (int c = 0; c < C; ++c) r.v[c] = narrow<S>(v[c]);
-        store_pack((S*)((char*)(p + i * stride) + lane), r);
+        store_pack((S*)((char*)(p + i * stride) + lane), Pack<S, C>::from(v));
     }
     // A chunk's rows from position t on.  Of a chunk that does not count as a whole, the others' places hold the last row that does.
     template <bool FULL>
@@ -121,22 +118,11 @@ struct Rows {
         for (int i = 0; i < L; ++i) rows[i] = FULL ? load(p, i) : load_own(p, min(i, inside - 1));
     }
 };
-// Makes the compiler take a value as new, so that nothing computed from it before is kept.
-template <class S, int C>
-__device__ __forceinline__ void forget(Pack<S, C>& p) {
-    if constexpr (sizeof(p) % 4 == 0) {
-        uint32_t w[sizeof(p) / 4];
-        __builtin_memcpy(w, &p, sizeof(p));
-#pragma unroll
-        for (unsigned k = 0; k < sizeof(p) / 4; ++k) asm("" : "+v"(w[k]));
-        __builtin_memcpy(&p, w, sizeof(p));
-    }
-}
 template <int C, class Off>
 __device__ __forceinline__ void read(const Rows<float, C, Off>& r, int64_t t, float v[C]) {
     const Pack<float, C> p = r.load(r.at(t), 0);
 #pragma unroll
-    for (int c = 0; c < C; ++c) v[c] = p.v[c];
+    for (int c = 0; c < C; ++c) v[c] = p.get(c);
 }
 template <int C, class Off>
 __device__ __forceinline__ void write(const Rows<float, C, Off>& r, int64_t t, const float v[C]) { r.store(r.at(t), 0, v); }
@@ -183,8 +169,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
             float shown[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const Gates gate(widen(gs[i].v[c]));
-                const float next = gate.step(h[c], widen(xs[i].v[c]));
+                const Gates gate(gs[i].get(c));
+                const float next = gate.step(h[c], xs[i].get(c));
                 h[c] = in ? next : h[c];
                 if (SUMMARY) product[c] = in ? gate.keep(product[c]) : product[c];
                 shown[c] = in ? next : 0.0f;
@@ -242,7 +228,7 @@ __global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) voi
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
                     before[i][c] = h[c];
-                    if (i + 1 < L) h[c] = Gates(widen(gs[i].v[c])).step(h[c], widen(xs[i].v[c]));   // of use where position i + 1 counts
+                    if (i + 1 < L) h[c] = Gates(gs[i].get(c)).step(h[c], xs[i].get(c));   // of use where position i + 1 counts
                 }
         }
         // The gates are made again on the way back: kept, a chunk's would take 128 registers and three quarters of the wavefronts.
@@ -258,14 +244,14 @@ __global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) voi
             float dx[C], dg[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const Gates gate(widen(gs[i].v[c]));
-                const float lambda = widen(ds[i].v[c]) + f[c];
+                const Gates gate(gs[i].get(c));
+                const float lambda = ds[i].get(c) + f[c];
                 f[c] = in ? gate.keep(lambda) : f[c];
                 if (SUMMARY) {
                     product[c] = in ? gate.keep(product[c]) : product[c];
                 } else {
                     dx[c] = in ? gate.take(lambda) : 0.0f;
-                    dg[c] = in ? gate.keep(gate.take(lambda * (before[i][c] - widen(xs[i].v[c])))) : 0.0f;
+                    dg[c] = in ? gate.keep(gate.take(lambda * (before[i][c] - xs[i].get(c)))) : 0.0f;
                 }
             }
             if (!SUMMARY && (FULL || i < part.count)) {

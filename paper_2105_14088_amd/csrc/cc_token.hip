@@ -67,6 +67,7 @@ dim3 grid_of(int64_t units) {
 // Row statistics of a row and its token, in the form that loss and gradient need.
 struct Row {
     float m, rest, own, total;        // own: e_k
+    bool none;                        // no candidate
     double logprob;
 };
 
@@ -75,22 +76,19 @@ struct Row {
 __device__ __forceinline__ Row finish_row(float m, float rest, float token_logit, float scale) {
     Row r;
     r.m = m;
-    r.rest = rest;
-    const double d = (double)scale * ((double)token_logit - (double)m);
-    r.own = exp_fast((float)d);
-    if (m == -kInf) {                 // no candidate at all: nothing is probable and nothing has a gradient
+    r.none = m == -kInf;
+    if (r.none) {                     // nothing is probable and nothing has a gradient
         r.own = 0.0f;
         r.total = 1.0f;
         r.rest = 0.0f;
         r.logprob = -(double)kInf;
         return r;
     }
+    const double d = (double)scale * ((double)token_logit - (double)m);
+    r.rest = rest;
+    r.own = exp_fast((float)d);
     r.total = rest + r.own;
-    if (rest < r.own) {
-        r.logprob = -(double)log1pf(rest / r.own);
-    } else {
-        r.logprob = d - log((double)r.total);
-    }
+    r.logprob = rest < r.own ? -(double)log1pf(rest / r.own) : d - log((double)r.total);
     return r;
 }
 
@@ -137,28 +135,11 @@ __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, co
     return r;
 }
 
-// Positions and orders that count, from the counting kernel's parts.  Every lane of the workgroup ends with them.
-template <int THREADS>
-__device__ __forceinline__ int2 all_counts(const Args& a, int* lds) {
-    int2 sum = {0, 0};
-    for (int i = threadIdx.x; i < a.part_count; i += THREADS) {
-        const int2 p = a.parts[i];
-        sum.x += p.x;
-        sum.y += p.y;
-    }
-    sum.x = wave_sum_i32(sum.x);
-    sum.y = wave_sum_i32(sum.y);
-    if ((threadIdx.x & 63) == 0) {
-        lds[(threadIdx.x >> 6) * 2] = sum.x;
-        lds[(threadIdx.x >> 6) * 2 + 1] = sum.y;
-    }
-    __syncthreads();
-    sum = {0, 0};
-    for (int w = 0; w < THREADS / 64; ++w) {
-        sum.x += lds[2 * w];
-        sum.y += lds[2 * w + 1];
-    }
-    return sum;
+// Positions and orders that count, from the counting kernel's parts, one a lane.  Every wavefront adds them for itself.
+__device__ __forceinline__ int2 all_counts(const Args& a) {
+    const int lane = threadIdx.x & 63;
+    const int2 p = lane < a.part_count ? a.parts[lane] : make_int2(0, 0);
+    return make_int2(group_sum<64>(p.x), group_sum<64>(p.y));
 }
 __device__ __forceinline__ float weight_of(const Args& a, const int2& all, int order_count) {
     if (!a.mean_of_orders) return all.x > 0 ? 1.0f / (float)all.x : 0.0f;
@@ -191,43 +172,44 @@ __device__ __forceinline__ void store_partial(double* out, double s0, double s1,
 
 // ------------------------------------------------------------------------------------------------------ short rows
 
-// G lanes per row, K vectors of VEC logits per lane.  A workgroup has order_slots orders, row_slots rows of each.
+// G lanes per row, K vectors of VEC logits per lane.  A workgroup has order_slots orders, row_slots rows of each; its wavefronts take
+// batches of (64 / G) * ITER of these rows:
+//   0. a lane per row: token and mask, what the loss needs of the position
+//   1. G lanes per row, ITER rows each: all their vectors in flight, largest logit, exponentials (kept in registers), sum
+//   2. a lane per row: log-probability and loss, in 64 bits and coalesced; G lanes would do that work G times
+//   3. G lanes per row: the gradient
+// with a wavefront's own words of LDS between the phases and no barrier.
 //
-// A lane's vector starts at element j0; one that would end beyond the row is moved back to end with it.  It then repeats elements of
+// A lane's vector starts at element j; one that would end beyond the row is moved back to end with it.  It then repeats elements of
 // the lane before it: these are left out of the sum, and their gradient is written twice, with the same value.  Every
 // lane so has a whole vector to load and store.
-//
-// The next row is loaded before the present one is reduced.
-template <class S, int VEC, int K>
-struct RowLoad {
-    Pack<S, VEC> p[K];
-    float token_logit;
-    float2 saved;
-    float slope;
-    PolicyInputs in;
-    int64_t order, at;
-    int k, t, o;
-    bool real, valid;
+struct RowInfo {
+    int k, t, o, real;                // token (-1: the position does not count), position, order within the workgroup, whether there is a row
 };
 
-template <class S, int VEC, int G, int K, int KIND, bool PLACED>
-__global__ __launch_bounds__(kThreads) void short_rows_kernel(Args a) {
-    constexpr int GROUPS = kThreads / G;
+template <class S, int VEC, int G, int K, int ITER, int KIND, bool PLACED>
+__global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_rows_kernel(Args a) {
+    constexpr int WAVES = kThreads / 64, PER = 64 / G, BATCH = PER * ITER;
     extern __shared__ int first_at[];                 // PLACED: [order_slots][stride] earliest position of each node
-    __shared__ int count_lds[2 * kThreads / 64];
-    __shared__ double sum_lds[3 * kThreads / 64];
-    const int group = threadIdx.x / G, lane = threadIdx.x % G, V = a.V;
+    __shared__ RowInfo info[WAVES][BATCH];
+    __shared__ float2 sums[WAVES][BATCH];             // {m, rest}
+    __shared__ float own[WAVES][BATCH];               // the token's logit
+    __shared__ float2 pulls[WAVES][BATCH];            // what multiplies the other terms, and the token's gradient
+    __shared__ double sum_lds[3 * WAVES];
+    const int wave = threadIdx.x >> 6, wlane = threadIdx.x & 63, group = wlane / G, lane = wlane % G, V = a.V;
     const int stride = (V + 7) & ~7;
     const int64_t unit = workgroup();
     if (unit >= a.units) return;
     const int64_t first_order = a.order_slots > 1 ? unit * a.order_slots : unit / a.chunks;
-    const int first_row = a.order_slots > 1 ? 0 : (int)(unit - first_order * a.chunks) * a.row_slots;
+    const int64_t first_row = a.order_slots > 1 ? 0 : (unit - first_order * a.chunks) * a.row_slots;
     const int orders = (int)min((int64_t)a.order_slots, a.B - first_order);
     const int rows = (int)min((int64_t)a.row_slots, a.T - first_row);
+    int2 all = {0, 0};
+    if (KIND == kTokenPolicy) all = all_counts(a);
     if (PLACED) {
         for (int i = threadIdx.x; i < orders * stride; i += kThreads) first_at[i] = 0x7fffffff;
         __syncthreads();
-        const int upto = first_row + rows - 1;        // positions before the last row's
+        const int upto = (int)first_row + rows - 1;   // positions before the last row's
         for (int i = threadIdx.x; i < orders * upto; i += kThreads) {
             const int o = i / upto, t = i - o * upto;
             const int k = a.tokens[(first_order + o) * a.T + t];
@@ -235,103 +217,141 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(Args a) {
         }
         __syncthreads();
     }
-    int2 all = {0, 0};
-    if (KIND == kTokenPolicy) all = all_counts<kThreads>(a, count_lds);
     double sum_loss = 0.0, sum_kl = 0.0, sum_clipped = 0.0;
     const int slots = orders * rows;
-    const auto load = [&](int slot) {
-        RowLoad<S, VEC, K> r = {};
-        r.real = slot < slots;
-        r.o = r.real ? slot / rows : 0;
-        r.t = r.real ? first_row + slot - r.o * rows : 0;
-        r.order = first_order + r.o;
-        r.at = r.order * a.T + r.t;
-        r.k = r.real ? a.tokens[r.at] : -1;
-        r.valid = r.real && counts_here(a, r.at, r.k);
-        if (r.valid) {
-            const S* const row = (const S*)a.logits + r.order * a.sb + (int64_t)r.t * a.st;
-#pragma unroll
-            for (int c = 0; c < K; ++c) r.p[c] = load_pack<VEC>(row + min((c * G + lane) * VEC, V - VEC));
-            r.token_logit = widen(row[r.k]);
-            if (KIND == kTokenPolicy) r.in = policy_inputs(a, r.at, r.order);
+    for (int base = wave * BATCH; base < slots; base += WAVES * BATCH) {
+        // 0.
+        wave_order();                                 // after the batch before, whose words these are
+        const int slot = base + wlane;
+        const bool mine = wlane < BATCH && slot < slots;
+        const int o_mine = mine && orders > 1 ? slot / rows : 0;
+        const int t_mine = mine ? (int)first_row + slot - o_mine * rows : 0;
+        const int64_t order = first_order + o_mine, at = order * a.T + t_mine;
+        bool valid = false;
+        PolicyInputs in = {};
+        float2 saved = {0.0f, 0.0f};
+        float slope = 0.0f, ref = 0.0f;
+        if (mine) {
+            const int k = a.tokens[at];
+            valid = counts_here(a, at, k);
+            info[wave][wlane] = {valid ? k : -1, t_mine, o_mine, 1};
+            if (KIND == kTokenPolicy) in = policy_inputs(a, at, order);
+            if (KIND == kTokenForward && a.gaps && a.ref) ref = a.ref[at];
             if (KIND == kTokenBackward) {
-                r.saved = a.rows[r.at];
-                r.slope = a.slope[a.slope_per_token ? r.at : r.order];
+                saved = a.rows[at];
+                slope = a.slope[a.slope_per_token ? at : order];
+                sums[wave][wlane] = saved;
             }
+        } else if (wlane < BATCH) {
+            info[wave][wlane] = {-1, 0, 0, 0};
         }
-        return r;
-    };
-    RowLoad<S, VEC, K> next = load(group);
-    for (int base = 0; base < slots; base += GROUPS) {
-        const RowLoad<S, VEC, K> now = next;
-        if (base + GROUPS < slots) next = load(base + GROUPS + group);
-        float z[K * VEC];
-        // what is no candidate becomes minus infinity, before it is looked at
+        wave_order();
+        // 1.
+        Pack<S, VEC> packs[ITER][K];
 #pragma unroll
-        for (int c = 0; c < K; ++c) {
-            const int j0 = min((c * G + lane) * VEC, V - VEC);
-            int first[VEC];
-            if (PLACED) {
+        for (int it = 0; it < ITER; ++it) {
+            if (base + it * PER >= slots) break;
+            const RowInfo r = info[wave][it * PER + group];
+            if (r.k < 0) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) first[i] = first_at[now.o * stride + j0 + i];
+                for (int c = 0; c < K; ++c) packs[it][c] = Pack<S, VEC>();
+                continue;
             }
+            const S* const row = (const S*)a.logits + (first_order + r.o) * a.sb + (int64_t)r.t * a.st;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                z[c * VEC + i] = widen(now.p[c].v[i]);
-                if (PLACED) z[c * VEC + i] = (int)(j0 + i == now.k) | (int)(first[i] >= now.t) ? z[c * VEC + i] : -kInf;
+            for (int c = 0; c < K; ++c) packs[it][c] = load_pack<VEC>(row + min((c * G + lane) * VEC, V - VEC));
+        }
+        float e[ITER][K * VEC];
+#pragma unroll
+        for (int it = 0; it < ITER; ++it) {
+            if (base + it * PER >= slots) break;
+            const int at_row = it * PER + group;
+            const RowInfo r = info[wave][at_row];
+            float m = -kInf;
+            // what is no candidate becomes minus infinity, before it is looked at
+#pragma unroll
+            for (int c = 0; c < K; ++c) {
+                const int j0 = min((c * G + lane) * VEC, V - VEC);
+                int first[VEC];
+                if (PLACED) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) first[i] = first_at[r.o * stride + j0 + i];
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    float z = packs[it][c].get(i);
+                    if (j0 + i == r.k) own[wave][at_row] = z;
+                    if (PLACED) z = (int)(j0 + i == r.k) | (int)(first[i] >= r.t) ? z : -kInf;
+                    e[it][c * VEC + i] = z;
+                    m = fmaxf(m, z);
+                }
             }
-        }
-        float m = now.saved.x, rest = now.saved.y;
-        if (KIND != kTokenBackward) {
-            m = -kInf;
-#pragma unroll
-            for (int e = 0; e < K * VEC; ++e) m = fmaxf(m, z[e]);
-            m = group_max<G>(m);
-        }
-        const float low = m == -kInf ? 0.0f : m;
-#pragma unroll
-        for (int e = 0; e < K * VEC; ++e) z[e] = term(a, z[e] - low);
-        if (KIND != kTokenBackward) {
-            rest = 0.0f;
+            m = KIND == kTokenBackward ? sums[wave][at_row].x : group_max<G>(m);
+            const float low = m == -kInf ? 0.0f : m;
+            float rest = 0.0f;
 #pragma unroll
             for (int c = 0; c < K; ++c) {
                 const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) rest += (int)(j0 + i >= j) & (int)(j0 + i != now.k) ? z[c * VEC + i] : 0.0f;
+                for (int i = 0; i < VEC; ++i) {
+                    float& v = e[it][c * VEC + i];
+                    v = term(a, v - low);
+                    if (KIND != kTokenBackward) rest += (int)(j0 + i >= j) & (int)(j0 + i != r.k) ? v : 0.0f;
+                }
             }
-            rest = group_sum<G>(rest);
-        }
-        const Row r = finish_row(m, rest, now.token_logit, a.scale);
-        float slope = now.slope;
-        if (KIND == kTokenPolicy && now.valid) {
-            const PolicyTerms p = policy_terms(a, r.logprob, now.in);
-            const float w = weight_of(a, all, now.in.order_count);
-            slope = w * p.slope;
-            if (lane == 0) {
-                sum_loss += (double)w * p.loss;
-                sum_kl += (double)w * p.kl;
-                sum_clipped += (double)w * p.clipped;
+            if (KIND != kTokenBackward) {
+                rest = group_sum<G>(rest);
+                if (lane == 0) sums[wave][at_row] = make_float2(m, rest);
             }
         }
-        if (KIND != kTokenBackward && now.real && lane == 0) {
-            a.logprob[now.at] = now.valid ? (float)r.logprob : 0.0f;
-            if (a.rows) a.rows[now.at] = now.valid ? make_float2(r.m, r.rest) : make_float2(0.0f, 0.0f);
-            if (a.gaps) a.gaps[now.at] = now.valid ? r.logprob - (a.ref ? (double)a.ref[now.at] : 0.0) : 0.0;
+        wave_order();
+        // 2.
+        if (mine) {
+            Row r = {};
+            if (valid) {
+                if (KIND != kTokenBackward) saved = sums[wave][wlane];
+                r = finish_row(saved.x, saved.y, own[wave][wlane], a.scale);
+                if (KIND == kTokenPolicy) {
+                    const PolicyTerms p = policy_terms(a, r.logprob, in);
+                    const float w = weight_of(a, all, in.order_count);
+                    slope = w * p.slope;
+                    sum_loss += (double)w * p.loss;
+                    sum_kl += (double)w * p.kl;
+                    sum_clipped += (double)w * p.clipped;
+                }
+            }
+            if (KIND != kTokenBackward) {
+                a.logprob[at] = (float)r.logprob;
+                if (a.rows) a.rows[at] = make_float2(r.m, r.rest);
+                if (KIND == kTokenForward && a.gaps) a.gaps[at] = valid ? r.logprob - (double)ref : 0.0;
+            }
+            if (KIND != kTokenForward) {
+                const float pull = valid && !r.none ? slope * a.scale * a.grad_scale / r.total : 0.0f;
+                pulls[wave][wlane] = make_float2(-pull, pull * r.rest);
+            }
         }
-        if (KIND == kTokenForward || !a.grad || !now.real) continue;
-        const float pull = now.valid ? slope * a.scale * a.grad_scale / r.total : 0.0f;
-        S* const out = (S*)a.grad + now.order * a.gsb + (int64_t)now.t * a.gst;
+        if (KIND == kTokenForward || !a.grad) continue;
+        wave_order();
+        // 3.
 #pragma unroll
-        for (int c = 0; c < K; ++c) {
-            const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
-            if (j >= V) continue;
-            Pack<S, VEC> p;
+        for (int it = 0; it < ITER; ++it) {
+            if (base + it * PER >= slots) break;
+            const RowInfo r = info[wave][it * PER + group];
+            const float2 pull = pulls[wave][it * PER + group];
+            S* const out = (S*)a.grad + (first_order + r.o) * a.gsb + (int64_t)r.t * a.gst;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float e = j0 + i == now.k ? r.rest : -z[c * VEC + i];
-                p.v[i] = narrow<S>((int)now.valid & (int)(e != 0.0f) ? pull * e : 0.0f);
+            for (int c = 0; c < K; ++c) {
+                const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
+                float g[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    float v = e[it][c * VEC + i] * pull.x;
+                    if (PLACED) v = e[it][c * VEC + i] == 0.0f ? 0.0f : v;     // no candidate: zero, whatever the row's others are
+                    v = j0 + i == r.k ? pull.y : v;
+                    g[i] = r.k < 0 ? 0.0f : v;
+                }
+                if ((int)(j < V) & r.real) store_pack(out + j0, Pack<S, VEC>::from(g));
             }
-            store_pack(out + j0, p);
         }
     }
     if (KIND == kTokenPolicy) store_partial<kThreads>(a.partial + unit * 3, sum_loss, sum_kl, sum_clipped, sum_lds);
@@ -339,15 +359,31 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(Args a) {
 
 // ------------------------------------------------------------------------------------------------------- long rows
 
-// A workgroup per row, which is read twice: once for its maximum and sum, kept as a running pair in each lane, once for
-// the gradient.
-constexpr int kLongThreads = 512;
-template <class S, int KIND>
-__global__ __launch_bounds__(kLongThreads) void long_rows_kernel(Args a) {
-    constexpr int VEC = 16 / sizeof(S), WAVES = kLongThreads / 64;
-    __shared__ float wave_m[WAVES], wave_rest[WAVES];
-    __shared__ int count_lds[2 * WAVES];
-    const int V = a.V;
+// A workgroup per row.  K > 0: the row, up to THREADS * K vectors, stays in registers as it was loaded, so that it is read once
+// for log-probability, loss and gradient; its exponentials are taken twice, since 32 bits of each would not fit.  K = 0: rows
+// longer than that are read twice.  As for short rows, a vector that would end beyond the row is moved back.
+//
+// The token's own term and repeated elements are taken out of the sum where they are, by the lane that has them, in a branch
+// that other wavefronts skip.
+template <class S, int VEC>
+__device__ __forceinline__ void widen_row(const Pack<S, VEC>& p, float z[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) z[i] = p.get(i);
+}
+
+// What was widened is not kept: the row stays in registers as it was loaded.
+template <class S, int VEC, int N>
+__device__ __forceinline__ void forget_all(Pack<S, VEC> (&p)[N]) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) forget(p[c]);
+}
+
+template <class S, int THREADS, int K, int KIND>
+__global__ __launch_bounds__(THREADS, K > 8 || (K == 0 && KIND == kTokenPolicy) ? 4 : 8) void long_rows_kernel(Args a) {
+    constexpr int VEC = 16 / sizeof(S), WAVES = THREADS / 64, STEP = THREADS * VEC, KEPT = K > 0 ? K : 4;
+    __shared__ float2 wave_sums[WAVES];               // {m, rest}
+    __shared__ float2 shared_pull;
+    const int V = a.V, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t at = workgroup();
     if (at >= a.B * a.T) return;
     const int64_t order = at / a.T, t = at - order * a.T;
@@ -355,6 +391,7 @@ __global__ __launch_bounds__(kLongThreads) void long_rows_kernel(Args a) {
     const bool valid = counts_here(a, at, k);
     const S* const row = (const S*)a.logits + order * a.sb + t * a.st;
     S* const out = (S*)a.grad + order * a.gsb + t * a.gst;
+    int mine = threadIdx.x * VEC;
     if (!valid) {
         if (KIND != kTokenBackward && threadIdx.x == 0) {
             a.logprob[at] = 0.0f;
@@ -363,124 +400,199 @@ __global__ __launch_bounds__(kLongThreads) void long_rows_kernel(Args a) {
         }
         if (KIND == kTokenPolicy && threadIdx.x < 3) a.partial[at * 3 + threadIdx.x] = 0.0;
         if (KIND == kTokenForward || !a.grad) return;
-        Pack<S, VEC> p;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) p.v[i] = (S)0.0f;
-        for (int j = threadIdx.x * VEC; j < V; j += kLongThreads * VEC) store_some<VEC>(out + j, p, V - j);
+        const float zero[VEC] = {};
+        const Pack<S, VEC> p = Pack<S, VEC>::from(zero);
+        for (int j = mine; j < V; j += STEP) store_pack(out + min(j, V - VEC), p);
         return;
+    }
+    Pack<S, VEC> kept[KEPT];
+    if (K > 0) {
+#pragma unroll
+        for (int c = 0; c < K; ++c)
+            if (c * STEP < V) kept[c] = load_pack<VEC>(row + min(c * STEP + mine, V - VEC));
     }
     const float token_logit = widen(row[k]);
     int2 all = {0, 0};
-    if (KIND == kTokenPolicy) all = all_counts<kLongThreads>(a, count_lds);
+    PolicyInputs in = {};
+    if (KIND == kTokenPolicy && wave == 0) {
+        all = all_counts(a);
+        in = policy_inputs(a, at, order);
+    }
     float m = -kInf, rest = 0.0f;
     if (KIND == kTokenBackward) {
         const float2 saved = a.rows[at];
         m = saved.x;
         rest = saved.y;
-        __syncthreads();              // the gradient may take the logits' place: the token's has been read by all
+        __syncthreads();                              // the gradient may take the logits' place: the token's has been read by all
     } else {
-#pragma unroll 4
-        for (int j = threadIdx.x * VEC; j < V; j += kLongThreads * VEC) {
-            const Pack<S, VEC> p = load_some<VEC>(row + j, V - j);
-            float z[VEC], top = m;
+        // Elements of the vector at j that are not summed: the token, and those that the vector before it has.
+        const auto leave_out = [&](int j, float z[VEC]) {
+            const int j0 = min(j, V - VEC);
+            if ((uint32_t)(k - j0) < (uint32_t)VEC || j0 != j) {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                z[i] = j + i < V ? widen(p.v[i]) : -kInf;
-                top = fmaxf(top, z[i]);
+                for (int i = 0; i < VEC; ++i) z[i] = j0 + i == k || j0 + i < j ? -kInf : z[i];
             }
-            const float low = top == -kInf ? 0.0f : top;
-            rest *= term(a, m - low);
+        };
+        if (K > 0) {
+            // The lane's largest logit, the token's among them, then its sum.
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float e = term(a, z[i] - low);
-                rest += j + i == k ? 0.0f : e;
+            for (int c = 0; c < K; ++c)
+                if (c * STEP < V) {
+                    float z[VEC];
+                    widen_row(kept[c], z);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
+                }
+            const float low = m == -kInf ? 0.0f : m;
+            forget_all(kept);
+            asm("" : "+v"(mine));                     // and places in the row are made again
+#pragma unroll
+            for (int c = 0; c < K; ++c)
+                if (c * STEP < V) {
+                    float z[VEC];
+                    widen_row(kept[c], z);
+                    leave_out(c * STEP + mine, z);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) rest += term(a, z[i] - low);
+                    __builtin_amdgcn_sched_barrier(0);    // one vector's values at a time: registers are for the row
+                }
+        } else {
+            // KEPT vectors at a time, with a running maximum.
+            for (int c0 = 0; c0 < V; c0 += KEPT * STEP) {
+#pragma unroll
+                for (int c = 0; c < KEPT; ++c)
+                    if (c0 + c * STEP < V) kept[c] = load_pack<VEC>(row + min(c0 + c * STEP + mine, V - VEC));
+                float top = m;
+#pragma unroll
+                for (int c = 0; c < KEPT; ++c)
+                    if (c0 + c * STEP < V) {
+                        float z[VEC];
+                        widen_row(kept[c], z);
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) top = fmaxf(top, z[i]);
+                    }
+                const float low = top == -kInf ? 0.0f : top;
+                rest *= term(a, m - low);
+#pragma unroll
+                for (int c = 0; c < KEPT; ++c)
+                    if (c0 + c * STEP < V) {
+                        float z[VEC];
+                        widen_row(kept[c], z);
+                        leave_out(c0 + c * STEP + mine, z);
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) rest += term(a, z[i] - low);
+                    }
+                m = top;
             }
-            m = top;
         }
         const float lane_m = m;
         m = group_max<64>(m);
         float low = m == -kInf ? 0.0f : m;
         rest = group_sum<64>(rest * term(a, lane_m - low));
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-            wave_m[wave] = m;
-            wave_rest[wave] = rest;
-        }
+        if (lane == 0) wave_sums[wave] = make_float2(m, rest);
         __syncthreads();
-        m = wave_m[0];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, wave_m[w]);
+        // every wavefront joins the wavefronts' pairs, one a lane
+        const float2 w = lane < WAVES ? wave_sums[lane] : make_float2(-kInf, 0.0f);
+        m = group_max<64>(w.x);
         low = m == -kInf ? 0.0f : m;
-        rest = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) rest += wave_rest[w] * term(a, wave_m[w] - low);
+        rest = group_sum<64>(w.y * term(a, w.x - low));
     }
-    const Row r = finish_row(m, rest, token_logit, a.scale);
-    float slope = 0.0f;
-    if (KIND == kTokenPolicy) {
-        const PolicyInputs in = policy_inputs(a, at, order);
-        const PolicyTerms p = policy_terms(a, r.logprob, in);
-        const float w = weight_of(a, all, in.order_count);
-        slope = w * p.slope;
-        if (threadIdx.x == 0) {
-            a.partial[at * 3] = (double)w * p.loss;
-            a.partial[at * 3 + 1] = (double)w * p.kl;
-            a.partial[at * 3 + 2] = (double)w * p.clipped;
+    if (wave == 0) {
+        const Row r = finish_row(m, rest, token_logit, a.scale);
+        float slope = 0.0f;
+        if (KIND == kTokenPolicy) {
+            const PolicyTerms p = policy_terms(a, r.logprob, in);
+            const float w = weight_of(a, all, in.order_count);
+            slope = w * p.slope;
+            if (threadIdx.x == 0) {
+                a.partial[at * 3] = (double)w * p.loss;
+                a.partial[at * 3 + 1] = (double)w * p.kl;
+                a.partial[at * 3 + 2] = (double)w * p.clipped;
+            }
+        } else if (KIND == kTokenBackward) {
+            slope = a.slope[a.slope_per_token ? at : order];
         }
-    } else if (KIND == kTokenBackward) {
-        slope = a.slope[a.slope_per_token ? at : order];
-    }
-    if (KIND != kTokenBackward && threadIdx.x == 0) {
-        a.logprob[at] = (float)r.logprob;
-        if (a.rows) a.rows[at] = make_float2(r.m, r.rest);
-        if (a.gaps) a.gaps[at] = r.logprob - (a.ref ? (double)a.ref[at] : 0.0);
+        if (KIND != kTokenBackward && threadIdx.x == 0) {
+            a.logprob[at] = (float)r.logprob;
+            if (a.rows) a.rows[at] = make_float2(r.m, r.rest);
+            if (a.gaps) a.gaps[at] = r.logprob - (a.ref ? (double)a.ref[at] : 0.0);
+        }
+        if (KIND != kTokenForward && threadIdx.x == 0) {
+            const float pull = r.none ? 0.0f : slope * a.scale * a.grad_scale / r.total;
+            shared_pull = make_float2(-pull, pull * r.rest);
+        }
     }
     if (KIND == kTokenForward || !a.grad) return;
-    const float pull = slope * a.scale * a.grad_scale / r.total;
+    __syncthreads();
+    const float2 pull = shared_pull;
     const float low = m == -kInf ? 0.0f : m;
-    const bool none = m == -kInf;
-#pragma unroll 2
-    for (int j = threadIdx.x * VEC; j < V; j += kLongThreads * VEC) {
-        Pack<S, VEC> p = load_some<VEC>(row + j, V - j);
+    const auto gradient = [&](int j, const Pack<S, VEC>& p) {
+        const int j0 = min(j, V - VEC);
+        float z[VEC];
+        widen_row(p, z);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float e = none ? 0.0f : term(a, widen(p.v[i]) - low);
-            const float g = j + i == k ? r.rest : -e;
-            p.v[i] = narrow<S>(g != 0.0f ? pull * g : 0.0f);
+        for (int i = 0; i < VEC; ++i) z[i] = term(a, z[i] - low) * pull.x;
+        if ((uint32_t)(k - j0) < (uint32_t)VEC) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) z[i] = j0 + i == k ? pull.y : z[i];
         }
-        store_some<VEC>(out + j, p, V - j);
+        const Pack<S, VEC> g = Pack<S, VEC>::from(z);
+        if (K == 0 && j0 != j) {
+            // Read again, in place perhaps: what this vector repeats may hold its gradient by now.  Only its own elements are stored.
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (j0 + i >= j) out[j0 + i] = g.element(i);
+        } else if (j < V) {
+            store_pack(out + j0, g);
+        }
+    };
+    if (K > 0) {
+        forget_all(kept);
+        asm("" : "+v"(mine));
+#pragma unroll
+        for (int c = 0; c < K; ++c)
+            if (c * STEP < V) {
+                gradient(c * STEP + mine, kept[c]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    } else {
+        for (int c0 = 0; c0 < V; c0 += KEPT * STEP) {
+#pragma unroll
+            for (int c = 0; c < KEPT; ++c)
+                if (c0 + c * STEP < V) kept[c] = load_pack<VEC>(row + min(c0 + c * STEP + mine, V - VEC));
+#pragma unroll
+            for (int c = 0; c < KEPT; ++c)
+                if (c0 + c * STEP < V) gradient(c0 + c * STEP + mine, kept[c]);
+        }
     }
 }
 
 // ---------------------------------------------------------------------------------------------------- small kernels
 
 // counts[b]: positions of order b that count; parts[workgroup]: positions and orders with any.
-constexpr int kCountBlocks = 256;
-__global__ __launch_bounds__(kThreads) void count_kernel(const int32_t* __restrict__ tokens, const uint8_t* __restrict__ mask, int64_t B,
-                                                         int64_t T, int V, int* __restrict__ counts, int2* __restrict__ parts) {
-    __shared__ int lds[2 * kThreads / 64];
+constexpr int kCountBlocks = 64, kCountThreads = 1024;
+__global__ __launch_bounds__(kCountThreads) void count_kernel(const int32_t* __restrict__ tokens, const uint8_t* __restrict__ mask, int64_t B,
+                                                              int64_t T, int V, int* __restrict__ counts, int2* __restrict__ parts) {
+    constexpr int WAVES = kCountThreads / 64;
+    __shared__ int2 lds[WAVES];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int positions = 0, orders = 0;
-    for (int64_t b = (int64_t)blockIdx.x * (kThreads / 64) + wave; b < B; b += (int64_t)gridDim.x * (kThreads / 64)) {
+    int2 sum = {0, 0};
+    for (int64_t b = (int64_t)blockIdx.x * WAVES + wave; b < B; b += (int64_t)gridDim.x * WAVES) {
         int n = 0;
 #pragma unroll 4
         for (int64_t t = lane; t < T; t += 64)
-            n += (uint32_t)tokens[b * T + t] < (uint32_t)V && (!mask || mask[b * T + t] != 0) ? 1 : 0;
-        n = wave_sum_i32(n);
+            n += (int)((uint32_t)tokens[b * T + t] < (uint32_t)V) & (int)(!mask || mask[b * T + t] != 0);
+        n = group_sum<64>(n);
         if (lane == 0) counts[b] = n;
-        positions += n;
-        orders += n > 0 ? 1 : 0;
+        sum.x += n;
+        sum.y += n > 0 ? 1 : 0;
     }
-    if (lane == 0) {
-        lds[2 * wave] = positions;
-        lds[2 * wave + 1] = orders;
-    }
+    if (lane == 0) lds[wave] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        int2 sum = {0, 0};
-        for (int w = 0; w < kThreads / 64; ++w) {
-            sum.x += lds[2 * w];
-            sum.y += lds[2 * w + 1];
+        for (int w = 1; w < WAVES; ++w) {
+            sum.x += lds[w].x;
+            sum.y += lds[w].y;
         }
         parts[blockIdx.x] = sum;
     }
@@ -571,35 +683,44 @@ Layout layout(int64_t B, int64_t T) {
 
 template <class S, int VEC, int G, int K, int KIND>
 int64_t launch_short(Args& a, bool placed, hipStream_t s) {
-    constexpr int groups = kThreads / G;
-    // A workgroup takes several orders where they have fewer positions than it has groups of lanes; else up to eight rows
-    // per group of one order, fewer where that would leave compute units idle.
+    // up to 32 registers of exponentials per lane, beside the vectors they are made of
+    constexpr int ITER = 32 / (K * VEC) < 4 ? 32 / (K * VEC) : 4, batch = 64 / G * ITER, rows_at_once = batch * (kThreads / 64);
+    // A workgroup takes several orders where their positions do not fill its batches; else up to four batches a wavefront of one
+    // order's positions (the more, the fewer times the order's nodes are looked up), fewer where that would leave compute units idle.
     const int64_t T = a.T;
-    if (T * 2 <= groups) {
-        int64_t orders = groups / T;
+    if (T * 2 <= rows_at_once) {
+        int64_t orders = rows_at_once / T;
         const int64_t stride = (a.V + 7) & ~7;
         if (placed && orders * stride > 8192) orders = 8192 / stride;
+        while (orders > 1 && (a.B + orders - 1) / orders < 512) orders = (orders + 1) / 2;
         a.order_slots = (int)orders;
         a.row_slots = (int)T;
         a.chunks = 1;
     } else {
-        int64_t passes = 8;
-        while (passes > 1 && a.B * ((T + groups * passes - 1) / (groups * passes)) < 2048) passes /= 2;
+        int64_t passes = 4;
+        while (passes > 1 && a.B * ((T + rows_at_once * passes - 1) / (rows_at_once * passes)) < 1024) passes /= 2;
         a.order_slots = 1;
-        a.row_slots = (int)(groups * passes < T ? groups * passes : T);
+        a.row_slots = (int)(rows_at_once * passes < T ? rows_at_once * passes : T);
         a.chunks = (int)((T + a.row_slots - 1) / a.row_slots);
     }
     const int64_t blocks = a.order_slots > 1 ? (a.B + a.order_slots - 1) / a.order_slots : a.B * a.chunks;
     a.units = blocks;
     if (placed)
-        hipLaunchKernelGGL((short_rows_kernel<S, VEC, G, K, KIND, true>), grid_of(blocks), dim3(kThreads),
+        hipLaunchKernelGGL((short_rows_kernel<S, VEC, G, K, ITER, KIND, true>), grid_of(blocks), dim3(kThreads),
                            sizeof(int) * a.order_slots * ((a.V + 7) & ~7), s, a);
     else
-        hipLaunchKernelGGL((short_rows_kernel<S, VEC, G, K, KIND, false>), grid_of(blocks), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((short_rows_kernel<S, VEC, G, K, ITER, KIND, false>), grid_of(blocks), dim3(kThreads), 0, s, a);
     return blocks;
 }
 
-// One pass over the rows; returns the number of workgroups.
+template <class S, int THREADS, int K, int KIND>
+int64_t launch_long(Args& a, hipStream_t s) {
+    const int64_t rows = a.B * a.T;
+    hipLaunchKernelGGL((long_rows_kernel<S, THREADS, K, KIND>), grid_of(rows), dim3(THREADS), 0, s, a);
+    return rows;
+}
+
+// One pass over the rows; returns the number of workgroups, each of which leaves a partial sum of the loss.
 template <class S, int KIND>
 int64_t launch_rows(Args& a, bool placed, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(S);
@@ -613,9 +734,19 @@ int64_t launch_rows(Args& a, bool placed, hipStream_t s) {
         if (V <= 128 * VEC) return launch_short<S, VEC, 64, 2, KIND>(a, placed, s);
         if constexpr (VEC == 4) return launch_short<S, VEC, 64, 4, KIND>(a, placed, s);
     }
-    const int64_t rows = a.B * a.T;
-    hipLaunchKernelGGL((long_rows_kernel<S, KIND>), grid_of(rows), dim3(kLongThreads), 0, s, a);
-    return rows;
+    // Only the policy loss needs a row twice.  Threads and vectors per thread: enough to hold it.
+    if constexpr (KIND == kTokenPolicy) {
+        if (V <= 256 * VEC * 2) return launch_long<S, 256, 2, KIND>(a, s);
+        if (V <= 256 * VEC * 4) return launch_long<S, 256, 4, KIND>(a, s);
+        if (V <= 256 * VEC * 8) return launch_long<S, 256, 8, KIND>(a, s);
+        if (V <= 512 * VEC * 8) return launch_long<S, 512, 8, KIND>(a, s);
+        if (V <= 1024 * VEC * 8) return launch_long<S, 1024, 8, KIND>(a, s);
+        if (V <= 1024 * VEC * 16) return launch_long<S, 1024, 16, KIND>(a, s);
+        return launch_long<S, 1024, 0, KIND>(a, s);
+    } else {
+        if (V <= 256 * VEC * 4) return launch_long<S, 256, 0, KIND>(a, s);
+        return launch_long<S, 512, 0, KIND>(a, s);
+    }
 }
 
 template <class S>
@@ -661,11 +792,11 @@ hipError_t run(TokenKind kind, const TokenCall& c, hipStream_t s) {
         int64_t partials = 0;
         a.partial = (double*)(w + l.sums);
         if (any) {
-            const int64_t need = (c.B + kThreads / 64 - 1) / (kThreads / 64);
+            const int64_t need = (c.B + kCountThreads / 64 - 1) / (kCountThreads / 64);
             a.part_count = (int)(need < kCountBlocks ? need : kCountBlocks);
             a.counts = (const int*)(w + l.counts);
             a.parts = (const int2*)(w + l.parts);
-            hipLaunchKernelGGL(count_kernel, dim3((unsigned)a.part_count), dim3(kThreads), 0, s, c.tokens, c.mask, c.B, c.T, a.V,
+            hipLaunchKernelGGL(count_kernel, dim3((unsigned)a.part_count), dim3(kCountThreads), 0, s, c.tokens, c.mask, c.B, c.T, a.V,
                                (int*)(w + l.counts), (int2*)(w + l.parts));
             partials = launch_rows<S, kTokenPolicy>(a, c.placed, s);
         }
