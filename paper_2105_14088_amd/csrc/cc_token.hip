@@ -18,6 +18,8 @@
 //   longer rows: a workgroup per row.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
+
 #include "cc_internal.h"
 #include "cc_model.h"
 
@@ -39,7 +41,6 @@ struct Args {
     const uint8_t* mask;
     float scale, grad_scale;
     float scale2, scale2_rest;        // scale * log2(e) as a float, and what that leaves out
-    float lowest;                     // a difference of logits from which on a term is 0
     float* logprob;
     float2* rows;                     // {m, rest}
     double* gaps;                     // logprob - ref in 64 bits, for the margins
@@ -93,12 +94,9 @@ __device__ __forceinline__ Row finish_row(float m, float rest, float token_logit
 }
 
 // exp(scale * x) for a difference x of two logits.  With the rest of the scale: what its rounding leaves out would make every term
-// of every row too small or every term too large, and sums of log-probabilities would show it.  Below `lowest` the result is 0; a
-// NaN stays one.
-__device__ __forceinline__ float term(const Args& a, float x) {
-    x = __builtin_elementwise_maximum(x, a.lowest);
-    return __builtin_amdgcn_exp2f(fmaf(x, a.scale2, x * a.scale2_rest));
-}
+// of every row too small or every term too large, and sums of log-probabilities would show it.  The scale is rounded
+// towards zero and the rest is positive: for x = -infinity both products are.
+__device__ __forceinline__ float term(const Args& a, float x) { return __builtin_amdgcn_exp2f(fmaf(x, a.scale2, x * a.scale2_rest)); }
 
 // What a policy row adds to the loss, the divergence and the clipped share, and its slope.
 struct PolicyTerms {
@@ -196,7 +194,7 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
     __shared__ float own[WAVES][BATCH];               // the token's logit
     __shared__ float2 pulls[WAVES][BATCH];            // what multiplies the other terms, and the token's gradient
     __shared__ double sum_lds[3 * WAVES];
-    const int wave = threadIdx.x >> 6, wlane = threadIdx.x & 63, group = wlane / G, lane = wlane % G, V = a.V;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wlane = threadIdx.x & 63, group = wlane / G, lane = wlane % G, V = a.V;
     const int stride = (V + 7) & ~7;
     const int64_t unit = workgroup();
     if (unit >= a.units) return;
@@ -217,6 +215,15 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
         }
         __syncthreads();
     }
+    // The positions of the nodes that a lane's vectors hold: the same for all rows of one order.
+    int first[PLACED ? K * VEC : 1];
+    const auto look_up = [&](int o) {
+#pragma unroll
+        for (int c = 0; c < K; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) first[c * VEC + i] = first_at[o * stride + min((c * G + lane) * VEC, V - VEC) + i];
+    };
+    if (PLACED && orders == 1) look_up(0);
     double sum_loss = 0.0, sum_kl = 0.0, sum_clipped = 0.0;
     const int slots = orders * rows;
     for (int base = wave * BATCH; base < slots; base += WAVES * BATCH) {
@@ -267,23 +274,30 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
             if (base + it * PER >= slots) break;
             const int at_row = it * PER + group;
             const RowInfo r = info[wave][at_row];
+            if (PLACED && orders > 1) look_up(r.o);
             float m = -kInf;
-            // what is no candidate becomes minus infinity, before it is looked at
+            // What is no candidate becomes minus infinity, before it is looked at; so does the token once the maximum has seen it: its
+            // own term is no part of the sum.
 #pragma unroll
             for (int c = 0; c < K; ++c) {
                 const int j0 = min((c * G + lane) * VEC, V - VEC);
-                int first[VEC];
-                if (PLACED) {
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) first[i] = first_at[r.o * stride + j0 + i];
-                }
+                float* const z = e[it] + c * VEC;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    float z = packs[it][c].get(i);
-                    if (j0 + i == r.k) own[wave][at_row] = z;
-                    if (PLACED) z = (int)(j0 + i == r.k) | (int)(first[i] >= r.t) ? z : -kInf;
-                    e[it][c * VEC + i] = z;
-                    m = fmaxf(m, z);
+                    z[i] = packs[it][c].get(i);
+                    if (PLACED) z[i] = first[c * VEC + i] >= r.t ? z[i] : -kInf;
+                    m = fmaxf(m, z[i]);
+                }
+                if ((uint32_t)(r.k - j0) < (uint32_t)VEC) {
+                    float token_logit = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (j0 + i == r.k) {
+                            token_logit = packs[it][c].get(i);
+                            z[i] = -kInf;
+                        }
+                    m = fmaxf(m, token_logit);
+                    own[wave][at_row] = token_logit;
                 }
             }
             m = KIND == kTokenBackward ? sums[wave][at_row].x : group_max<G>(m);
@@ -292,12 +306,19 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
 #pragma unroll
             for (int c = 0; c < K; ++c) {
                 const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
+                float* const z = e[it] + c * VEC;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    float& v = e[it][c * VEC + i];
-                    v = term(a, v - low);
-                    if (KIND != kTokenBackward) rest += (int)(j0 + i >= j) & (int)(j0 + i != r.k) ? v : 0.0f;
+                for (int i = 0; i < VEC; ++i) z[i] = term(a, z[i] - low);
+                if (KIND == kTokenBackward) continue;
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum += z[i];
+                if (j0 != j) {                        // without what the lane before it has
+                    sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) sum += j0 + i >= j ? z[i] : 0.0f;
                 }
+                rest += sum;
             }
             if (KIND != kTokenBackward) {
                 rest = group_sum<G>(rest);
@@ -344,11 +365,15 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
                 const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
                 float g[VEC];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    float v = e[it][c * VEC + i] * pull.x;
-                    if (PLACED) v = e[it][c * VEC + i] == 0.0f ? 0.0f : v;     // no candidate: zero, whatever the row's others are
-                    v = j0 + i == r.k ? pull.y : v;
-                    g[i] = r.k < 0 ? 0.0f : v;
+                for (int i = 0; i < VEC; ++i) g[i] = e[it][c * VEC + i] * pull.x;
+                if (PLACED && !(fabsf(pull.x) < kInf)) {
+                    // what is no candidate has no gradient, whatever the row's others have
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) g[i] = e[it][c * VEC + i] == 0.0f ? 0.0f : g[i];
+                }
+                if ((uint32_t)(r.k - j0) < (uint32_t)VEC) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) g[i] = j0 + i == r.k ? pull.y : g[i];
                 }
                 if ((int)(j < V) & r.real) store_pack(out + j0, Pack<S, VEC>::from(g));
             }
@@ -379,7 +404,7 @@ __device__ __forceinline__ void forget_all(Pack<S, VEC> (&p)[N]) {
 }
 
 template <class S, int THREADS, int K, int KIND>
-__global__ __launch_bounds__(THREADS, K > 8 || (K == 0 && KIND == kTokenPolicy) ? 4 : 8) void long_rows_kernel(Args a) {
+__global__ __launch_bounds__(THREADS, K > 8 || (K == 0 && KIND != kTokenBackward) ? 4 : 8) void long_rows_kernel(Args a) {
     constexpr int VEC = 16 / sizeof(S), WAVES = THREADS / 64, STEP = THREADS * VEC, KEPT = K > 0 ? K : 4;
     __shared__ float2 wave_sums[WAVES];               // {m, rest}
     __shared__ float2 shared_pull;
@@ -734,8 +759,9 @@ int64_t launch_rows(Args& a, bool placed, hipStream_t s) {
         if (V <= 128 * VEC) return launch_short<S, VEC, 64, 2, KIND>(a, placed, s);
         if constexpr (VEC == 4) return launch_short<S, VEC, 64, 4, KIND>(a, placed, s);
     }
-    // Only the policy loss needs a row twice.  Threads and vectors per thread: enough to hold it.
-    if constexpr (KIND == kTokenPolicy) {
+    // Threads and vectors per thread: enough to hold the row, all of it on its way at once.  The gradient alone needs no sum and
+    // takes a few vectors at a time.
+    if constexpr (KIND != kTokenBackward) {
         if (V <= 256 * VEC * 2) return launch_long<S, 256, 2, KIND>(a, s);
         if (V <= 256 * VEC * 4) return launch_long<S, 256, 4, KIND>(a, s);
         if (V <= 256 * VEC * 8) return launch_long<S, 256, 8, KIND>(a, s);
@@ -762,8 +788,8 @@ hipError_t run(TokenKind kind, const TokenCall& c, hipStream_t s) {
     a.scale = c.scale;
     const double scale2 = (double)c.scale * 1.4426950408889634074;
     a.scale2 = (float)scale2;
+    if ((double)a.scale2 >= scale2) a.scale2 = std::nextafterf(a.scale2, 0.0f);
     a.scale2_rest = (float)(scale2 - (double)a.scale2);
-    a.lowest = (float)(-256.0 / scale2);
     a.grad_scale = c.grad_scale;
     a.logprob = c.logprob;
     a.rows = (float2*)c.rows;
