@@ -75,6 +75,23 @@ __device__ __forceinline__ void store_some(S* p, const Pack<S, N>& r, int have) 
         if (i < have) p[i] = r.element(i);
 }
 
+// The largest of N elements (a NaN among them is passed over).
+template <class S, int N>
+__device__ __forceinline__ float largest(const Pack<S, N>& p) {
+    if constexpr (__is_same(S, _Float16) && N % 2 == 0) {
+        typedef _Float16 Two __attribute__((ext_vector_type(2)));
+        Two m = __builtin_bit_cast(Two, p.w[0]);
+#pragma unroll
+        for (int i = 1; i < N / 2; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(Two, p.w[i]));
+        return fmaxf((float)m[0], (float)m[1]);
+    } else {
+        float m = p.get(0);
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = fmaxf(m, p.get(i));
+        return m;
+    }
+}
+
 // Makes the compiler take a value as new, so that nothing computed from it before is kept.
 template <class S, int N>
 __device__ __forceinline__ void forget(Pack<S, N>& p) {

@@ -404,7 +404,7 @@ __device__ __forceinline__ void forget_all(Pack<S, VEC> (&p)[N]) {
 }
 
 template <class S, int THREADS, int K, int KIND>
-__global__ __launch_bounds__(THREADS, K > 8 || (K == 0 && KIND != kTokenBackward) ? 4 : 8) void long_rows_kernel(Args a) {
+__global__ __launch_bounds__(THREADS, K > 8 || (K == 0 && KIND != kTokenBackward) ? 5 - K / 16 : 8) void long_rows_kernel(Args a) {
     constexpr int VEC = 16 / sizeof(S), WAVES = THREADS / 64, STEP = THREADS * VEC, KEPT = K > 0 ? K : 4;
     __shared__ float2 wave_sums[WAVES];               // {m, rest}
     __shared__ float2 shared_pull;
@@ -462,12 +462,7 @@ __global__ __launch_bounds__(THREADS, K > 8 || (K == 0 && KIND != kTokenBackward
             // The lane's largest logit, the token's among them, then its sum.
 #pragma unroll
             for (int c = 0; c < K; ++c)
-                if (c * STEP < V) {
-                    float z[VEC];
-                    widen_row(kept[c], z);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
-                }
+                if (c * STEP < V) m = fmaxf(m, largest(kept[c]));
             const float low = m == -kInf ? 0.0f : m;
             forget_all(kept);
             asm("" : "+v"(mine));                     // and places in the row are made again
@@ -482,20 +477,22 @@ __global__ __launch_bounds__(THREADS, K > 8 || (K == 0 && KIND != kTokenBackward
                     __builtin_amdgcn_sched_barrier(0);    // one vector's values at a time: registers are for the row
                 }
         } else {
-            // KEPT vectors at a time, with a running maximum.
-            for (int c0 = 0; c0 < V; c0 += KEPT * STEP) {
+            // KEPT vectors at a time, with a running maximum, the next ones on their way.
+            const auto load = [&](int c0, Pack<S, VEC> (&to)[KEPT]) {
 #pragma unroll
                 for (int c = 0; c < KEPT; ++c)
-                    if (c0 + c * STEP < V) kept[c] = load_pack<VEC>(row + min(c0 + c * STEP + mine, V - VEC));
+                    if (c0 + c * STEP < V) to[c] = load_pack<VEC>(row + min(c0 + c * STEP + mine, V - VEC));
+            };
+            Pack<S, VEC> next[KEPT];
+            load(0, next);
+            for (int c0 = 0; c0 < V; c0 += KEPT * STEP) {
+#pragma unroll
+                for (int c = 0; c < KEPT; ++c) kept[c] = next[c];
+                load(c0 + KEPT * STEP, next);
                 float top = m;
 #pragma unroll
                 for (int c = 0; c < KEPT; ++c)
-                    if (c0 + c * STEP < V) {
-                        float z[VEC];
-                        widen_row(kept[c], z);
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) top = fmaxf(top, z[i]);
-                    }
+                    if (c0 + c * STEP < V) top = fmaxf(top, largest(kept[c]));
                 const float low = top == -kInf ? 0.0f : top;
                 rest *= term(a, m - low);
 #pragma unroll
@@ -759,9 +756,9 @@ int64_t launch_rows(Args& a, bool placed, hipStream_t s) {
         if (V <= 128 * VEC) return launch_short<S, VEC, 64, 2, KIND>(a, placed, s);
         if constexpr (VEC == 4) return launch_short<S, VEC, 64, 4, KIND>(a, placed, s);
     }
-    // Threads and vectors per thread: enough to hold the row, all of it on its way at once.  The gradient alone needs no sum and
-    // takes a few vectors at a time.
-    if constexpr (KIND != kTokenBackward) {
+    // The policy loss needs a row twice: threads and vectors per thread enough to hold it.  One pass takes a few vectors at a time,
+    // in workgroups small enough that one's sums overlap others' loads.
+    if constexpr (KIND == kTokenPolicy) {
         if (V <= 256 * VEC * 2) return launch_long<S, 256, 2, KIND>(a, s);
         if (V <= 256 * VEC * 4) return launch_long<S, 256, 4, KIND>(a, s);
         if (V <= 256 * VEC * 8) return launch_long<S, 256, 8, KIND>(a, s);
@@ -770,8 +767,8 @@ int64_t launch_rows(Args& a, bool placed, hipStream_t s) {
         if (V <= 1024 * VEC * 16) return launch_long<S, 1024, 16, KIND>(a, s);
         return launch_long<S, 1024, 0, KIND>(a, s);
     } else {
-        if (V <= 256 * VEC * 4) return launch_long<S, 256, 0, KIND>(a, s);
-        return launch_long<S, 512, 0, KIND>(a, s);
+        if (V <= 512 * VEC * 8 || a.B * a.T >= 2048) return launch_long<S, 256, 0, KIND>(a, s);
+        return launch_long<S, 1024, 0, KIND>(a, s);
     }
 }
 
