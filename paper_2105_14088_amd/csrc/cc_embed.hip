@@ -24,40 +24,50 @@ constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------------------------------------------------- lookup
 
-// A workgroup takes `rows` tokens; its threads take vectors of their rows in turn.
-template <class S>
+// A workgroup takes `rows` tokens; its threads take vectors of their rows in turn, U of them at once.  A vector that would end beyond
+// its row is moved back to end with it and repeats what the one before it writes, so that every thread loads and stores a whole one.
+template <class S, int VEC>
 __global__ __launch_bounds__(kThreads) void embed_kernel(const S* __restrict__ table, int V, int D, int64_t table_stride,
                                                          const int32_t* __restrict__ ids, int64_t n, float scale,
                                                          S* __restrict__ out, int64_t out_stride, int rows) {
-    constexpr int VEC = 16 / sizeof(S);
-    const int per_row = (D + VEC - 1) / VEC;
+    constexpr int U = 4;
+    const uint32_t per_row = (uint32_t)(D + VEC - 1) / VEC;
     const int64_t first = (int64_t)blockIdx.x * rows;
     const int have = (int)min((int64_t)rows, n - first);
-    const uint32_t count = (uint32_t)have * (uint32_t)per_row;
-    for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
-        const uint32_t r = i / (uint32_t)per_row, at = (i - r * per_row) * VEC;
-        const int id = ids[first + r];
-        const int left = D - (int)at;
-        Pack<S, VEC> p;
-        float f[VEC];
-        if ((uint32_t)id < (uint32_t)V) {
-            p = load_some<VEC>(table + (int64_t)id * table_stride + at, left);
+    const uint32_t count = (uint32_t)have * per_row;
+    for (uint32_t i0 = threadIdx.x; i0 < count; i0 += U * kThreads) {
+        uint32_t row[U];
+        int at[U], id[U];
+        Pack<S, VEC> p[U];
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) f[k] = p.get(k) * scale;
-        } else {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) f[k] = 0.0f;
+        for (int u = 0; u < U; ++u) {
+            const uint32_t i = min(i0 + u * kThreads, count - 1);
+            row[u] = i / per_row;
+            at[u] = min((int)(i - row[u] * per_row) * VEC, D - VEC);
+            id[u] = ids[first + row[u]];
         }
-        p = Pack<S, VEC>::from(f);
-        store_some<VEC>(out + (first + r) * out_stride + at, p, left);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if ((uint32_t)id[u] < (uint32_t)V) p[u] = load_pack<VEC>(table + (int64_t)id[u] * table_stride + at[u]);
+            else p[u] = Pack<S, VEC>();
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * kThreads >= count) break;
+            float f[VEC];
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) f[k] = (uint32_t)id[u] < (uint32_t)V ? p[u].get(k) * scale : 0.0f;
+            store_pack(out + (first + row[u]) * out_stride + at[u], Pack<S, VEC>::from(f));
+        }
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------ sort
 
 // One pass of a stable counting sort by `bits` bits from `shift` up.  Tiles of kTile tokens, kSortWaves wavefronts each,
-// a wavefront's tokens consecutive.
-constexpr int kTile = 4096, kSortWaves = 4, kSortThreads = kSortWaves * 64, kPerThread = kTile / kSortThreads;
+// a wavefront's tokens consecutive.  Short tiles: what a tile takes is a chain of ballots and LDS words per 64 tokens, and a list
+// is cut into as many tiles as there are compute units soon enough.
+constexpr int kTile = 1024, kSortWaves = 4, kSortThreads = kSortWaves * 64, kPerThread = kTile / kSortThreads;
 constexpr int kMaxBits = 11;
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t V) { return (uint32_t)id < V ? (uint32_t)id : V; }
@@ -194,23 +204,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t*
 
 // ------------------------------------------------------------------------------------------------------------ sums
 
-template <int VEC, class GT>
-__device__ __forceinline__ void write_row(GT* p, const float* acc, float scale, bool accumulate, int left) {
-    float f[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) f[k] = scale * acc[k];
-    if (accumulate) {
-        const Pack<GT, VEC> old = load_some<VEC>(p, left);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) f[k] = old.get(k) + scale * acc[k];
-    }
-    const Pack<GT, VEC> r = Pack<GT, VEC>::from(f);
-    store_some<VEC>(p, r, left);
-}
-
 struct SumArgs {
-    const int32_t* keys;          // sorted, n of them and 8 more that may be read
-    const int32_t* pos;
     int64_t n;
     int V, D;
     int64_t grad_stride, out_stride;
@@ -222,9 +216,40 @@ struct SumArgs {
     int64_t sum_blocks;           // workgroups that sum; those behind them clear the rows of absent ids
 };
 
-// First index whose key is at least v.
-__device__ __forceinline__ int64_t lower_bound(const int32_t* keys, int64_t n, int v) {
-    int64_t lo = 0, hi = n;
+// A lane's vector of a row: where it starts, and from which element on it is the lane's own.  One that would end beyond the row is
+// moved back to end with it; it is loaded as a whole and stored from its own elements on.
+template <int VEC>
+struct Part {
+    int at, skip;
+    bool real;
+    __device__ __forceinline__ Part(int want, int D) : at(min(want, D - VEC)), skip(want - min(want, D - VEC)), real(want < D) {}
+    template <class T>
+    __device__ __forceinline__ void store(T* row, const Pack<T, VEC>& p) const {
+        if (skip == 0) {
+            store_pack(row + at, p);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            if (k >= skip) row[at + k] = p.element(k);
+    }
+};
+
+template <int VEC, class GT>
+__device__ __forceinline__ void write_row(GT* row, const Part<VEC>& part, const float* acc, float scale, bool accumulate) {
+    float f[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) f[k] = scale * acc[k];
+    if (accumulate) {
+        const Pack<GT, VEC> old = load_pack<VEC>(row + part.at);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) f[k] = old.get(k) + scale * acc[k];
+    }
+    part.store(row, Pack<GT, VEC>::from(f));
+}
+
+// First index from `lo` on whose key is at least v.
+__device__ __forceinline__ int64_t lower_bound(const int32_t* keys, int64_t lo, int64_t hi, int v) {
     while (lo < hi) {
         const int64_t mid = (lo + hi) >> 1;
         if (keys[mid] < v) lo = mid + 1; else hi = mid;
@@ -232,51 +257,64 @@ __device__ __forceinline__ int64_t lower_bound(const int32_t* keys, int64_t n, i
     return lo;
 }
 
-template <class S, class GT, int G>
-__global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restrict__ grad, GT* __restrict__ out, SumArgs a) {
-    constexpr int VEC = 16 / sizeof(S), U = 8;
-    const int lane = threadIdx.x % G;
-    const int at = (blockIdx.y * G + lane) * VEC, left = a.D - at;
-    float acc[VEC];
+// The sums: G lanes along a row (and blockIdx.y where a row is longer), a segment each.  keys and pos: sorted, with 8 more than n that
+// may be read.
+template <class S, class GT, int VEC, int G>
+__global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restrict__ grad, const int32_t* __restrict__ keys,
+                                                              const int32_t* __restrict__ pos, GT* __restrict__ out, SumArgs a) {
+    constexpr int U = 8;
     if ((int64_t)blockIdx.x >= a.sum_blocks) {
-        // rows of ids that do not occur
-        if (left <= 0) return;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
-        const int64_t step = ((int64_t)gridDim.x - a.sum_blocks) * (kThreads / G);
-        for (int64_t v = ((int64_t)blockIdx.x - a.sum_blocks) * (kThreads / G) + threadIdx.x / G; v < a.V; v += step) {
-            const int64_t i = lower_bound(a.keys, a.n, (int)v);
-            if (i < a.n && a.keys[i] == (int)v) continue;
-            write_row<VEC>(out + v * a.out_stride + at, acc, 0.0f, false, left);
+        // Rows of ids that do not occur: 64 of them a workgroup, a lane looks for one of them, then the wavefronts clear them in turn.
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int64_t step = ((int64_t)gridDim.x - a.sum_blocks) * 64;
+        for (int64_t v0 = ((int64_t)blockIdx.x - a.sum_blocks) * 64; v0 < a.V; v0 += step) {
+            const int64_t v = v0 + lane;
+            bool absent = false;
+            if (v < a.V) {
+                const int64_t i = lower_bound(keys, 0, a.n, (int)v);
+                absent = i >= a.n || keys[i] != (int)v;
+            }
+            unsigned long long rows = __ballot(absent);
+            const float zero[VEC] = {};
+            for (int k = 0; rows != 0; ++k) {
+                const int r = __ffsll((long long)rows) - 1;
+                rows &= rows - 1;
+                if ((k & (kThreads / 64 - 1)) != wave) continue;
+                GT* const row = out + (v0 + r) * a.out_stride;
+                for (int want = lane * VEC; want < a.D; want += 64 * VEC) write_row(row, Part<VEC>(want, a.D), zero, 0.0f, false);
+            }
         }
         return;
     }
-    const int64_t seg = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
-    if (seg >= a.segments || left <= 0) return;
+    int group = threadIdx.x / G;
+    if (G >= 64) group = __builtin_amdgcn_readfirstlane(group);       // a segment's list is then read by scalar loads
+    const Part<VEC> part((blockIdx.y * G + threadIdx.x % G) * VEC, a.D);
+    const int64_t seg = (int64_t)blockIdx.x * (kThreads / G) + group;
+    if (seg >= a.segments || !part.real) return;
     const int64_t from = seg * a.segment, to = min(a.n, from + a.segment);
-    const int before = from > 0 ? a.keys[from - 1] : -1, after = to < a.n ? a.keys[to] : -1;
-    int current = a.keys[from];
+    const int before = from > 0 ? keys[from - 1] : -1, after = to < a.n ? keys[to] : -1;
+    int current = keys[from];
     bool open = current == before;                    // the run began in an earlier segment
-    float* const slot = a.partial + seg * 2 * a.D + at;
+    float* const slot = a.partial + seg * 2 * a.D;
+    float acc[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
     const auto flush = [&](bool goes_on) {
         if (current >= a.V) return;                   // no token
-        if (open || goes_on) {
-            float* const p = open ? slot : slot + a.D;
-            store_some<VEC>(p, Pack<float, VEC>::from(acc), left);
-        } else {
-            write_row<VEC>(out + (int64_t)current * a.out_stride + at, acc, a.scale, a.accumulate != 0, left);
-        }
+        if (open || goes_on) part.store(open ? slot : slot + a.D, Pack<float, VEC>::from(acc));
+        else write_row(out + (int64_t)current * a.out_stride, part, acc, a.scale, a.accumulate != 0);
     };
     for (int64_t i = from; i < to; i += U) {
         int key[U];
         Pack<S, VEC> row[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) key[u] = a.keys[i + u];
+        for (int u = 0; u < U; ++u) key[u] = keys[i + u];
+        // beyond the segment's end, and for what is no token, the segment's first row stands in
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + u < to && key[u] < a.V) row[u] = load_some<VEC>(grad + (int64_t)a.pos[i + u] * a.grad_stride + at, left);
+        for (int u = 0; u < U; ++u) {
+            const int p = i + u < to ? pos[i + u] : pos[from];
+            row[u] = load_pack<VEC>(grad + (int64_t)p * a.grad_stride + part.at);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (i + u >= to) break;
@@ -287,37 +325,43 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restric
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
             }
-            if (key[u] < a.V)
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) acc[k] += row[u].get(k);
+            for (int k = 0; k < VEC; ++k) acc[k] += row[u].get(k);
         }
     }
     flush(current == after);
 }
 
-// Runs that cross borders: the segment in which a run begins adds the partial sums of the segments that it reaches.
-template <class GT>
-__global__ __launch_bounds__(kThreads) void embed_join_kernel(GT* __restrict__ out, SumArgs a) {
-    constexpr int VEC = 4;
+// Runs that cross borders: the segment in which a run begins adds the partial sums of the segments that it reaches.  How far it
+// reaches is looked for in steps that double.
+template <class GT, int VEC>
+__global__ __launch_bounds__(kThreads) void embed_join_kernel(const int32_t* __restrict__ keys, GT* __restrict__ out, SumArgs a) {
     for (int64_t seg = blockIdx.x; seg + 1 < a.segments; seg += gridDim.x) {
         const int64_t from = seg * a.segment, to = from + a.segment;
-        const int key = a.keys[to - 1];
-        if (key >= a.V || a.keys[to] != key) continue;                                 // ends here
-        if (a.keys[from] == key && from > 0 && a.keys[from - 1] == key) continue;      // began earlier
-        const int64_t end = lower_bound(a.keys, a.n, key + 1), last = (end - 1) / a.segment;
-        for (int at = threadIdx.x * VEC; at < a.D; at += kThreads * VEC) {
-            const int left = a.D - at;
+        const int key = keys[to - 1];
+        if (key >= a.V || keys[to] != key) continue;                                   // ends here
+        if (keys[from] == key && from > 0 && keys[from - 1] == key) continue;          // began earlier
+        // the last segment whose first key is the run's
+        int64_t last = seg + 1, step = 1;
+        while (last + step < a.segments && keys[(last + step) * a.segment] == key) {
+            last += step;
+            step *= 2;
+        }
+        for (; step > 0; step /= 2)
+            if (last + step < a.segments && keys[(last + step) * a.segment] == key) last += step;
+        for (int want = threadIdx.x * VEC; want < a.D; want += kThreads * VEC) {
+            const Part<VEC> part(want, a.D);
             float acc[VEC];
-            Pack<float, VEC> p = load_some<VEC>(a.partial + (seg * 2 + 1) * a.D + at, left);
+            Pack<float, VEC> p = load_pack<VEC>(a.partial + (seg * 2 + 1) * a.D + part.at);
 #pragma unroll
             for (int k = 0; k < VEC; ++k) acc[k] = p.get(k);
-#pragma unroll 4
+#pragma unroll 8
             for (int64_t s = seg + 1; s <= last; ++s) {
-                p = load_some<VEC>(a.partial + s * 2 * a.D + at, left);
+                p = load_pack<VEC>(a.partial + s * 2 * a.D + part.at);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) acc[k] += p.get(k);
             }
-            write_row<VEC>(out + (int64_t)key * a.out_stride + at, acc, a.scale, a.accumulate != 0, left);
+            write_row(out + (int64_t)key * a.out_stride, part, acc, a.scale, a.accumulate != 0);
         }
     }
 }
@@ -361,26 +405,34 @@ Layout layout(int64_t V, int64_t D, int64_t n) {
     return l;
 }
 
-template <class S>
-hipError_t embed(const EmbedCall& c, hipStream_t s) {
-    constexpr int VEC = 16 / sizeof(S);
+template <class S, int VEC>
+void launch_lookup(const EmbedCall& c, hipStream_t s) {
     const int64_t per_row = (c.D + VEC - 1) / VEC;
     // rows per workgroup: four vectors a thread, fewer where that leaves compute units without a workgroup
     int64_t rows = (4 * kThreads + per_row - 1) / per_row;
     while (rows > 1 && (c.n + rows - 1) / rows < 1024) rows = (rows + 1) / 2;
-    hipLaunchKernelGGL((embed_kernel<S>), dim3((unsigned)((c.n + rows - 1) / rows)), dim3(kThreads), 0, s, (const S*)c.table, (int)c.V,
+    hipLaunchKernelGGL((embed_kernel<S, VEC>), dim3((unsigned)((c.n + rows - 1) / rows)), dim3(kThreads), 0, s, (const S*)c.table, (int)c.V,
                        (int)c.D, c.table_stride, c.ids, c.n, c.scale, (S*)c.out, c.out_stride, (int)rows);
+}
+
+// Vectors of 16 bytes where a row has one.
+template <class S>
+hipError_t embed(const EmbedCall& c, hipStream_t s) {
+    constexpr int VEC = 16 / sizeof(S);
+    if (c.D >= VEC) launch_lookup<S, VEC>(c, s);
+    else launch_lookup<S, 1>(c, s);
     return hipGetLastError();
 }
 
-template <class S, class GT, int G>
-void launch_sums(const S* grad, GT* out, SumArgs& a, hipStream_t s) {
-    constexpr int VEC = 16 / sizeof(S), per_block = kThreads / G;
+template <class S, class GT, int VEC, int G>
+void launch_sums(const S* grad, const int32_t* keys, const int32_t* pos, GT* out, SumArgs& a, hipStream_t s) {
+    constexpr int per_block = kThreads / G;
     a.sum_blocks = (a.segments + per_block - 1) / per_block;
-    int64_t clear = a.accumulate ? 0 : ((int64_t)a.V + per_block - 1) / per_block;
+    int64_t clear = a.accumulate ? 0 : ((int64_t)a.V + 63) / 64;
     if (clear > 65536) clear = 65536;
     const unsigned columns = (unsigned)((a.D + G * VEC - 1) / (G * VEC));
-    hipLaunchKernelGGL((embed_sums_kernel<S, GT, G>), dim3((unsigned)(a.sum_blocks + clear), columns), dim3(kThreads), 0, s, grad, out, a);
+    hipLaunchKernelGGL((embed_sums_kernel<S, GT, VEC, G>), dim3((unsigned)(a.sum_blocks + clear), columns), dim3(kThreads), 0, s, grad, keys,
+                       pos, out, a);
 }
 
 template <class S, class GT>
@@ -405,9 +457,8 @@ hipError_t backward(const EmbedCall& c, hipStream_t s) {
             hipLaunchKernelGGL(place, dim3((unsigned)l.tiles), dim3(kSortThreads), lds, s, in, pin, c.n, (uint32_t)c.V, shift, l.bits, hist,
                                totals, keys[p & 1], pos[p & 1]);
     }
+    const int32_t *sorted = keys[(l.passes + 1) & 1], *places = pos[(l.passes + 1) & 1];
     SumArgs a;
-    a.keys = keys[(l.passes + 1) & 1];
-    a.pos = pos[(l.passes + 1) & 1];
     a.n = c.n;
     a.V = (int)c.V;
     a.D = (int)c.D;
@@ -423,14 +474,18 @@ hipError_t backward(const EmbedCall& c, hipStream_t s) {
     const S* grad = (const S*)c.out;
     GT* out = (GT*)c.grad_table;
     // lanes along a row: the power of two that covers it
-    if (per_row <= 8) launch_sums<S, GT, 8>(grad, out, a, s);
-    else if (per_row <= 16) launch_sums<S, GT, 16>(grad, out, a, s);
-    else if (per_row <= 32) launch_sums<S, GT, 32>(grad, out, a, s);
-    else if (per_row <= 64) launch_sums<S, GT, 64>(grad, out, a, s);
-    else if (per_row <= 128) launch_sums<S, GT, 128>(grad, out, a, s);
-    else launch_sums<S, GT, 256>(grad, out, a, s);
-    if (l.segments > 1)
-        hipLaunchKernelGGL((embed_join_kernel<GT>), dim3((unsigned)(l.segments - 1 < 2048 ? l.segments - 1 : 2048)), dim3(kThreads), 0, s, out, a);
+    if (c.D < VEC) launch_sums<S, GT, 1, 8>(grad, sorted, places, out, a, s);
+    else if (per_row <= 8) launch_sums<S, GT, VEC, 8>(grad, sorted, places, out, a, s);
+    else if (per_row <= 16) launch_sums<S, GT, VEC, 16>(grad, sorted, places, out, a, s);
+    else if (per_row <= 32) launch_sums<S, GT, VEC, 32>(grad, sorted, places, out, a, s);
+    else if (per_row <= 64) launch_sums<S, GT, VEC, 64>(grad, sorted, places, out, a, s);
+    else if (per_row <= 128) launch_sums<S, GT, VEC, 128>(grad, sorted, places, out, a, s);
+    else launch_sums<S, GT, VEC, 256>(grad, sorted, places, out, a, s);
+    if (l.segments > 1) {
+        const unsigned blocks = (unsigned)(l.segments - 1 < 4096 ? l.segments - 1 : 4096);
+        if (c.D < 4) hipLaunchKernelGGL((embed_join_kernel<GT, 1>), dim3(blocks), dim3(kThreads), 0, s, sorted, out, a);
+        else hipLaunchKernelGGL((embed_join_kernel<GT, 4>), dim3(blocks), dim3(kThreads), 0, s, sorted, out, a);
+    }
     return hipGetLastError();
 }
 
