@@ -74,6 +74,10 @@ struct Row {
 
 // m, rest and the token's logit make the row's log-probability, in 64 bits: sums of log-probabilities are compared with
 // sums of others, and 2^-24 of each term's size would be what is left of a difference.
+//
+// With d = scale * (l_k - m): logprob = -log(1 + x), x = rest / e_k, where the token has most of the sum; else d - log(total), total =
+// f 2^e.  Both logarithms are log((1 + s) / (1 - s)) = 2 (s + s^3 / 3 + s^5 / 5 + ...) with s = x / (2 + x) or (f - 1) / (f + 1),
+// |s| <= 1/5: what follows s^15 / 15 is below 5e-13.  Neither loses what is small in a sum with 1.
 __device__ __forceinline__ Row finish_row(float m, float rest, float token_logit, float scale) {
     Row r;
     r.m = m;
@@ -89,7 +93,28 @@ __device__ __forceinline__ Row finish_row(float m, float rest, float token_logit
     r.rest = rest;
     r.own = exp_fast((float)d);
     r.total = rest + r.own;
-    r.logprob = rest < r.own ? -(double)log1pf(rest / r.own) : d - log((double)r.total);
+    const bool most = 2.0f * rest < r.own;
+    int e = 0;
+    float f = __builtin_frexpf(r.total, &e);          // 1/2 <= f < 1
+    if (f < 0.75f) {
+        f *= 2.0f;
+        e -= 1;
+    }
+    const double top = most ? (double)rest : (double)f - 1.0, bottom = most ? 2.0 * (double)r.own + (double)rest : (double)f + 1.0;
+    // the quotient: a reciprocal of 32 bits, made exact in two steps
+    double inverse = (double)__builtin_amdgcn_rcpf((float)bottom);
+    inverse = inverse * (2.0 - bottom * inverse);
+    const double s = top * inverse * (2.0 - bottom * inverse), q = s * s;
+    double series = 1.0 / 15;
+    series = series * q + 1.0 / 13;
+    series = series * q + 1.0 / 11;
+    series = series * q + 1.0 / 9;
+    series = series * q + 1.0 / 7;
+    series = series * q + 1.0 / 5;
+    series = series * q + 1.0 / 3;
+    const double log = 2.0 * (s + s * q * series);
+    r.logprob = most ? -log : d - ((double)e * kLn2 + log);
+    if (!(r.total < kInf)) r.logprob = __builtin_nan("");             // an infinite or undefined logit among the candidates
     return r;
 }
 
@@ -181,15 +206,19 @@ __device__ __forceinline__ void store_partial(double* out, double s0, double s1,
 // A lane's vector starts at element j; one that would end beyond the row is moved back to end with it.  It then repeats elements of
 // the lane before it: these are left out of the sum, and their gradient is written twice, with the same value.  Every
 // lane so has a whole vector to load and store.
+//
+// The next batch's vectors are loaded before this one is worked, and the tokens of the one after it, which say what to load; the
+// first batch's before the order's nodes are looked up.
 struct RowInfo {
     int k, t, o, real;                // token (-1: the position does not count), position, order within the workgroup, whether there is a row
+    int64_t in, out;                  // the row's place in the logits and in the gradient
 };
 
 template <class S, int VEC, int G, int K, int ITER, int KIND, bool PLACED>
 __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_rows_kernel(Args a) {
     constexpr int WAVES = kThreads / 64, PER = 64 / G, BATCH = PER * ITER;
     extern __shared__ int first_at[];                 // PLACED: [order_slots][stride] earliest position of each node
-    __shared__ RowInfo info[WAVES][BATCH];
+    __shared__ RowInfo infos[2][WAVES][BATCH];
     __shared__ float2 sums[WAVES][BATCH];             // {m, rest}
     __shared__ float own[WAVES][BATCH];               // the token's logit
     __shared__ float2 pulls[WAVES][BATCH];            // what multiplies the other terms, and the token's gradient
@@ -202,6 +231,73 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
     const int64_t first_row = a.order_slots > 1 ? 0 : (unit - first_order * a.chunks) * a.row_slots;
     const int orders = (int)min((int64_t)a.order_slots, a.B - first_order);
     const int rows = (int)min((int64_t)a.row_slots, a.T - first_row);
+    const int slots = orders * rows;
+
+    // 0. in two parts: the token of the lane's row, then what it decides.
+    struct Position {
+        int64_t order, at;
+        int t, o, k;
+        bool mine, masked;
+    };
+    const auto position = [&](int base) {
+        Position p;
+        const int slot = base + wlane;
+        p.mine = wlane < BATCH && slot < slots;
+        p.o = p.mine && orders > 1 ? slot / rows : 0;
+        p.t = p.mine ? (int)first_row + slot - p.o * rows : 0;
+        p.order = first_order + p.o;
+        p.at = p.order * a.T + p.t;
+        p.k = p.mine ? a.tokens[p.at] : -1;
+        p.masked = p.mine && a.mask && a.mask[p.at] == 0;
+        return p;
+    };
+    struct Batch {
+        Pack<S, VEC> packs[ITER][K];
+        PolicyInputs in;
+        float2 saved;
+        float slope, ref;
+        int64_t at;
+        bool mine, valid;
+    };
+    const auto stage = [&](const Position& p, int base, RowInfo* info) {
+        Batch r = {};
+        r.mine = p.mine;
+        r.at = p.at;
+        r.valid = p.mine && !p.masked && (uint32_t)p.k < (uint32_t)V;
+        if (wlane < BATCH) {
+            RowInfo row;
+            row.k = r.valid ? p.k : -1;
+            row.t = p.t;
+            row.o = p.o;
+            row.real = p.mine ? 1 : 0;
+            row.in = p.order * a.sb + (int64_t)p.t * a.st;
+            row.out = p.order * a.gsb + (int64_t)p.t * a.gst;
+            info[wlane] = row;
+        }
+        wave_order();
+#pragma unroll
+        for (int it = 0; it < ITER; ++it) {
+            if (base + it * PER >= slots) break;
+            const RowInfo row = info[it * PER + group];
+            if (row.k < 0) continue;
+#pragma unroll
+            for (int c = 0; c < K; ++c) r.packs[it][c] = load_pack<VEC>((const S*)a.logits + row.in + min((c * G + lane) * VEC, V - VEC));
+        }
+        if (p.mine) {
+            if (KIND == kTokenPolicy) r.in = policy_inputs(a, p.at, p.order);
+            if (KIND == kTokenForward && a.gaps && a.ref) r.ref = a.ref[p.at];
+            if (KIND == kTokenBackward) {
+                r.saved = a.rows[p.at];
+                r.slope = a.slope[a.slope_per_token ? p.at : p.order];
+            }
+        }
+        return r;
+    };
+    constexpr int STEP = WAVES * BATCH;
+    const int start = wave * BATCH;
+    Position coming = position(start);
+    Batch next = stage(coming, start, infos[0][wave]);
+    coming = position(start + STEP);
     int2 all = {0, 0};
     if (KIND == kTokenPolicy) all = all_counts(a);
     if (PLACED) {
@@ -225,55 +321,23 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
     };
     if (PLACED && orders == 1) look_up(0);
     double sum_loss = 0.0, sum_kl = 0.0, sum_clipped = 0.0;
-    const int slots = orders * rows;
-    for (int base = wave * BATCH; base < slots; base += WAVES * BATCH) {
-        // 0.
-        wave_order();                                 // after the batch before, whose words these are
-        const int slot = base + wlane;
-        const bool mine = wlane < BATCH && slot < slots;
-        const int o_mine = mine && orders > 1 ? slot / rows : 0;
-        const int t_mine = mine ? (int)first_row + slot - o_mine * rows : 0;
-        const int64_t order = first_order + o_mine, at = order * a.T + t_mine;
-        bool valid = false;
-        PolicyInputs in = {};
-        float2 saved = {0.0f, 0.0f};
-        float slope = 0.0f, ref = 0.0f;
-        if (mine) {
-            const int k = a.tokens[at];
-            valid = counts_here(a, at, k);
-            info[wave][wlane] = {valid ? k : -1, t_mine, o_mine, 1};
-            if (KIND == kTokenPolicy) in = policy_inputs(a, at, order);
-            if (KIND == kTokenForward && a.gaps && a.ref) ref = a.ref[at];
-            if (KIND == kTokenBackward) {
-                saved = a.rows[at];
-                slope = a.slope[a.slope_per_token ? at : order];
-                sums[wave][wlane] = saved;
-            }
-        } else if (wlane < BATCH) {
-            info[wave][wlane] = {-1, 0, 0, 0};
+    int parity = 0;
+    for (int base = start; base < slots; base += STEP, parity ^= 1) {
+        const Batch now = next;
+        const RowInfo* const info = infos[parity][wave];
+        if (base + STEP < slots) {
+            next = stage(coming, base + STEP, infos[parity ^ 1][wave]);
+            coming = position(base + 2 * STEP);
         }
+        if (KIND == kTokenBackward && wlane < BATCH) sums[wave][wlane] = now.saved;
         wave_order();
         // 1.
-        Pack<S, VEC> packs[ITER][K];
-#pragma unroll
-        for (int it = 0; it < ITER; ++it) {
-            if (base + it * PER >= slots) break;
-            const RowInfo r = info[wave][it * PER + group];
-            if (r.k < 0) {
-#pragma unroll
-                for (int c = 0; c < K; ++c) packs[it][c] = Pack<S, VEC>();
-                continue;
-            }
-            const S* const row = (const S*)a.logits + (first_order + r.o) * a.sb + (int64_t)r.t * a.st;
-#pragma unroll
-            for (int c = 0; c < K; ++c) packs[it][c] = load_pack<VEC>(row + min((c * G + lane) * VEC, V - VEC));
-        }
         float e[ITER][K * VEC];
 #pragma unroll
         for (int it = 0; it < ITER; ++it) {
             if (base + it * PER >= slots) break;
             const int at_row = it * PER + group;
-            const RowInfo r = info[wave][at_row];
+            const RowInfo r = info[at_row];
             if (PLACED && orders > 1) look_up(r.o);
             float m = -kInf;
             // What is no candidate becomes minus infinity, before it is looked at; so does the token once the maximum has seen it: its
@@ -284,7 +348,7 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
                 float* const z = e[it] + c * VEC;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    z[i] = packs[it][c].get(i);
+                    z[i] = now.packs[it][c].get(i);
                     if (PLACED) z[i] = first[c * VEC + i] >= r.t ? z[i] : -kInf;
                     m = fmaxf(m, z[i]);
                 }
@@ -293,7 +357,7 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
 #pragma unroll
                     for (int i = 0; i < VEC; ++i)
                         if (j0 + i == r.k) {
-                            token_logit = packs[it][c].get(i);
+                            token_logit = now.packs[it][c].get(i);
                             z[i] = -kInf;
                         }
                     m = fmaxf(m, token_logit);
@@ -327,14 +391,15 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
         }
         wave_order();
         // 2.
-        if (mine) {
+        if (now.mine) {
             Row r = {};
-            if (valid) {
-                if (KIND != kTokenBackward) saved = sums[wave][wlane];
-                r = finish_row(saved.x, saved.y, own[wave][wlane], a.scale);
+            float slope = now.slope;
+            if (now.valid) {
+                const float2 s = KIND == kTokenBackward ? now.saved : sums[wave][wlane];
+                r = finish_row(s.x, s.y, own[wave][wlane], a.scale);
                 if (KIND == kTokenPolicy) {
-                    const PolicyTerms p = policy_terms(a, r.logprob, in);
-                    const float w = weight_of(a, all, in.order_count);
+                    const PolicyTerms p = policy_terms(a, r.logprob, now.in);
+                    const float w = weight_of(a, all, now.in.order_count);
                     slope = w * p.slope;
                     sum_loss += (double)w * p.loss;
                     sum_kl += (double)w * p.kl;
@@ -342,12 +407,12 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
                 }
             }
             if (KIND != kTokenBackward) {
-                a.logprob[at] = (float)r.logprob;
-                if (a.rows) a.rows[at] = make_float2(r.m, r.rest);
-                if (KIND == kTokenForward && a.gaps) a.gaps[at] = valid ? r.logprob - (double)ref : 0.0;
+                a.logprob[now.at] = (float)r.logprob;
+                if (a.rows) a.rows[now.at] = make_float2(r.m, r.rest);
+                if (KIND == kTokenForward && a.gaps) a.gaps[now.at] = now.valid ? r.logprob - (double)now.ref : 0.0;
             }
             if (KIND != kTokenForward) {
-                const float pull = valid && !r.none ? slope * a.scale * a.grad_scale / r.total : 0.0f;
+                const float pull = now.valid && !r.none ? slope * a.scale * a.grad_scale / r.total : 0.0f;
                 pulls[wave][wlane] = make_float2(-pull, pull * r.rest);
             }
         }
@@ -357,9 +422,9 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
 #pragma unroll
         for (int it = 0; it < ITER; ++it) {
             if (base + it * PER >= slots) break;
-            const RowInfo r = info[wave][it * PER + group];
+            const RowInfo r = info[it * PER + group];
             const float2 pull = pulls[wave][it * PER + group];
-            S* const out = (S*)a.grad + (first_order + r.o) * a.gsb + (int64_t)r.t * a.gst;
+            S* const out = (S*)a.grad + r.out;
 #pragma unroll
             for (int c = 0; c < K; ++c) {
                 const int j = (c * G + lane) * VEC, j0 = min(j, V - VEC);
@@ -705,8 +770,8 @@ Layout layout(int64_t B, int64_t T) {
 
 template <class S, int VEC, int G, int K, int KIND>
 int64_t launch_short(Args& a, bool placed, hipStream_t s) {
-    // up to 32 registers of exponentials per lane, beside the vectors they are made of
-    constexpr int ITER = 32 / (K * VEC) < 4 ? 32 / (K * VEC) : 4, batch = 64 / G * ITER, rows_at_once = batch * (kThreads / 64);
+    // Two batches' vectors and one's exponentials, of 32 bits each, in registers: 16 elements a lane and batch of 32 bits, 32 of 16.
+    constexpr int MOST = (sizeof(S) == 4 ? 16 : 32) / (K * VEC), ITER = MOST < 4 ? MOST : 4, batch = 64 / G * ITER, rows_at_once = batch * (kThreads / 64);
     // A workgroup takes several orders where their positions do not fill its batches; else up to four batches a wavefront of one
     // order's positions (the more, the fewer times the order's nodes are looked up), fewer where that would leave compute units idle.
     const int64_t T = a.T;
