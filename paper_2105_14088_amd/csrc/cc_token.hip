@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
         Pack<S, VEC> packs[ITER][K];
         PolicyInputs in;
         float2 saved;
-        float slope, ref;
+        float slope, ref, token_logit;
         int64_t at;
         bool mine, valid;
     };
@@ -283,7 +283,8 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
 #pragma unroll
             for (int c = 0; c < K; ++c) r.packs[it][c] = load_pack<VEC>((const S*)a.logits + row.in + min((c * G + lane) * VEC, V - VEC));
         }
-        if (p.mine) {
+        if (r.valid) {
+            r.token_logit = widen(((const S*)a.logits)[p.order * a.sb + (int64_t)p.t * a.st + p.k]);
             if (KIND == kTokenPolicy) r.in = policy_inputs(a, p.at, p.order);
             if (KIND == kTokenForward && a.gaps && a.ref) r.ref = a.ref[p.at];
             if (KIND == kTokenBackward) {
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
     if (PLACED) {
         for (int i = threadIdx.x; i < orders * stride; i += kThreads) first_at[i] = 0x7fffffff;
         __syncthreads();
-        const int upto = (int)first_row + rows - 1;   // positions before the last row's
+        const int upto = (int)first_row + rows;       // positions up to the last row's
         for (int i = threadIdx.x; i < orders * upto; i += kThreads) {
             const int o = i / upto, t = i - o * upto;
             const int k = a.tokens[(first_order + o) * a.T + t];
@@ -329,7 +330,10 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
             next = stage(coming, base + STEP, infos[parity ^ 1][wave]);
             coming = position(base + 2 * STEP);
         }
-        if (KIND == kTokenBackward && wlane < BATCH) sums[wave][wlane] = now.saved;
+        if (wlane < BATCH) {
+            own[wave][wlane] = now.token_logit;
+            if (KIND == kTokenBackward) sums[wave][wlane] = now.saved;
+        }
         wave_order();
         // 1.
         float e[ITER][K * VEC];
@@ -339,9 +343,10 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
             const int at_row = it * PER + group;
             const RowInfo r = info[at_row];
             if (PLACED && orders > 1) look_up(r.o);
-            float m = -kInf;
-            // What is no candidate becomes minus infinity, before it is looked at; so does the token once the maximum has seen it: its
-            // own term is no part of the sum.
+            const float token_logit = own[wave][at_row];
+            float m = token_logit;
+            // What is no candidate becomes minus infinity, before it is looked at, and so does the token: its own term is no part of
+            // the sum.  Where nodes are left out that is one comparison: the token stands at this position or before.
 #pragma unroll
             for (int c = 0; c < K; ++c) {
                 const int j0 = min((c * G + lane) * VEC, V - VEC);
@@ -349,20 +354,14 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     z[i] = now.packs[it][c].get(i);
-                    if (PLACED) z[i] = first[c * VEC + i] >= r.t ? z[i] : -kInf;
-                    m = fmaxf(m, z[i]);
+                    if (PLACED) z[i] = first[c * VEC + i] > r.t ? z[i] : -kInf;
                 }
-                if ((uint32_t)(r.k - j0) < (uint32_t)VEC) {
-                    float token_logit = 0.0f;
+                if (!PLACED && (uint32_t)(r.k - j0) < (uint32_t)VEC) {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i)
-                        if (j0 + i == r.k) {
-                            token_logit = now.packs[it][c].get(i);
-                            z[i] = -kInf;
-                        }
-                    m = fmaxf(m, token_logit);
-                    own[wave][at_row] = token_logit;
+                    for (int i = 0; i < VEC; ++i) z[i] = j0 + i == r.k ? -kInf : z[i];
                 }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
             }
             m = KIND == kTokenBackward ? sums[wave][at_row].x : group_max<G>(m);
             const float low = m == -kInf ? 0.0f : m;
@@ -396,7 +395,7 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
             float slope = now.slope;
             if (now.valid) {
                 const float2 s = KIND == kTokenBackward ? now.saved : sums[wave][wlane];
-                r = finish_row(s.x, s.y, own[wave][wlane], a.scale);
+                r = finish_row(s.x, s.y, now.token_logit, a.scale);
                 if (KIND == kTokenPolicy) {
                     const PolicyTerms p = policy_terms(a, r.logprob, now.in);
                     const float w = weight_of(a, all, now.in.order_count);
@@ -685,8 +684,9 @@ __global__ __launch_bounds__(kCountThreads) void count_kernel(const int32_t* __r
     }
 }
 
-// The policy loss's three sums over the workgroups' partial sums, in one order.
 constexpr int kSumThreads = 1024;
+
+// The policy loss's three sums over the workgroups' partial sums, in one order.
 __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(const double* __restrict__ partial, int64_t count, float* __restrict__ stats) {
     __shared__ double lds[3][kSumThreads / 64];
     double s[3] = {0.0, 0.0, 0.0};
@@ -706,32 +706,53 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(const double* _
     }
 }
 
-// A pair: its margin, its share of the loss, and the slope of its two sequences' log-probabilities.
-__global__ __launch_bounds__(kThreads) void pair_kernel(const double* __restrict__ gaps, int64_t pairs, int64_t T, float beta, float smoothing,
-                                                        float* __restrict__ margin, float* __restrict__ slope, double* __restrict__ losses) {
-    __shared__ double lds[kThreads / 64];
-    for (int64_t p = blockIdx.x; p < pairs; p += gridDim.x) {
+// A pair: its margin, its share of the loss, and the slope of its two sequences' log-probabilities.  WAVES wavefronts share a pair's
+// positions.  Where one workgroup has all pairs it also adds their shares up; else pair_sum_kernel does.
+template <int THREADS, int WAVES>
+__global__ __launch_bounds__(THREADS) void pair_kernel(const double* __restrict__ gaps, int64_t pairs, int64_t T, float beta, float smoothing,
+                                                       float* __restrict__ margin, float* __restrict__ slope, double* __restrict__ losses,
+                                                       float* __restrict__ loss) {
+    constexpr int TEAMS = THREADS / 64 / WAVES;
+    __shared__ double lds[THREADS / 64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, team = wave / WAVES, member = wave % WAVES;
+    double sum = 0.0;
+    for (int64_t p0 = (int64_t)blockIdx.x * TEAMS; p0 < pairs; p0 += (int64_t)gridDim.x * TEAMS) {
+        const int64_t p = p0 + team;
         double gap = 0.0;
-        for (int64_t t = threadIdx.x; t < T; t += kThreads) gap += gaps[p * T + t] - gaps[(p + pairs) * T + t];
+        if (p < pairs) {
+#pragma unroll 4
+            for (int64_t t = member * 64 + lane; t < T; t += WAVES * 64) gap += gaps[p * T + t] - gaps[(p + pairs) * T + t];
+        }
         gap = wave_sum_f64(gap);
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = gap;
-        __syncthreads();
-        if (threadIdx.x == 0) {
+        if (WAVES > 1) {
+            if (lane == 0) lds[wave] = gap;
+            __syncthreads();
             gap = 0.0;
-            for (int w = 0; w < kThreads / 64; ++w) gap += lds[w];
+            for (int w = 0; w < WAVES; ++w) gap += lds[team * WAVES + w];
+            __syncthreads();
+        }
+        if (member == 0 && lane == 0 && p < pairs) {
             const double m = (double)beta * gap;
             // softplus(x) = max(x, 0) + log1p(exp(-|x|))
             const double tail = log1p(exp(-fabs(m)));
             const double wrong = fmax(-m, 0.0) + tail, right = fmax(m, 0.0) + tail;
-            losses[p] = ((1.0 - (double)smoothing) * wrong + (double)smoothing * right) / (double)pairs;
+            const double share = ((1.0 - (double)smoothing) * wrong + (double)smoothing * right) / (double)pairs;
             const double away = 1.0 / (1.0 + exp(m)), by = 1.0 / (1.0 + exp(-m));
             const float s = (float)((double)beta / (double)pairs * ((double)smoothing * by - (1.0 - (double)smoothing) * away));
             margin[p] = (float)m;
             slope[p] = s;
             slope[p + pairs] = -s;
+            if (loss) sum += share;
+            else losses[p] = share;
         }
-        __syncthreads();
     }
+    if (!loss) return;
+    if (lane == 0) lds[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = 0.0;
+    for (int w = 0; w < THREADS / 64; ++w) sum += lds[w];
+    *loss = (float)sum;
 }
 
 __global__ __launch_bounds__(kSumThreads) void pair_sum_kernel(const double* __restrict__ losses, int64_t pairs, float* __restrict__ loss) {
@@ -771,7 +792,8 @@ Layout layout(int64_t B, int64_t T) {
 template <class S, int VEC, int G, int K, int KIND>
 int64_t launch_short(Args& a, bool placed, hipStream_t s) {
     // Two batches' vectors and one's exponentials, of 32 bits each, in registers: 16 elements a lane and batch of 32 bits, 32 of 16.
-    constexpr int MOST = (sizeof(S) == 4 ? 16 : 32) / (K * VEC), ITER = MOST < 4 ? MOST : 4, batch = 64 / G * ITER, rows_at_once = batch * (kThreads / 64);
+    // The forward pass keeps no exponentials and takes twice the rows.
+    constexpr int MOST = (sizeof(S) == 4 ? 16 : 32) / (K * VEC) * (KIND == kTokenForward ? 2 : 1), ITER = MOST < 4 ? MOST : 4, batch = 64 / G * ITER, rows_at_once = batch * (kThreads / 64);
     // A workgroup takes several orders where their positions do not fill its batches; else up to four batches a wavefront of one
     // order's positions (the more, the fewer times the order's nodes are looked up), fewer where that would leave compute units idle.
     const int64_t T = a.T;
@@ -896,10 +918,17 @@ hipError_t run(TokenKind kind, const TokenCall& c, hipStream_t s) {
     a.rows = (float2*)(w + l.rows);
     a.gaps = (double*)(w + l.sums);
     if (any) launch_rows<S, kTokenForward>(a, c.placed, s);
-    if (pairs > 0)
-        hipLaunchKernelGGL(pair_kernel, dim3((unsigned)(pairs < 65536 ? pairs : 65536)), dim3(kThreads), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin,
-                           (float*)(w + l.counts), (double*)(w + l.losses));
-    hipLaunchKernelGGL(pair_sum_kernel, dim3(1), dim3(kSumThreads), 0, s, (const double*)(w + l.losses), pairs, c.stats);
+    double* const losses = (double*)(w + l.losses);
+    float* const slopes = (float*)(w + l.counts);
+    if (pairs * c.T <= 8192) {
+        // one workgroup takes 6.5 us for 4 x 777 positions, two launches 9.2; for 32 x 1000 it is 18 against 9.3
+        const auto kernel = pairs <= 4 ? pair_kernel<1024, 4> : pair_kernel<1024, 1>;
+        hipLaunchKernelGGL(kernel, dim3(1), dim3(1024), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin, slopes, losses, c.stats);
+    } else {
+        hipLaunchKernelGGL((pair_kernel<256, 4>), dim3((unsigned)(pairs < 65536 ? pairs : 65536)), dim3(256), 0, s, a.gaps, pairs, c.T, c.beta,
+                           c.smoothing, c.margin, slopes, losses, (float*)nullptr);
+        hipLaunchKernelGGL(pair_sum_kernel, dim3(1), dim3(kSumThreads), 0, s, losses, pairs, c.stats);
+    }
     if (any && c.grad) {
         a.slope = (const float*)(w + l.counts);
         a.slope_per_token = 0;
