@@ -257,6 +257,9 @@ __device__ __forceinline__ int64_t lower_bound(const int32_t* keys, int64_t lo, 
     return lo;
 }
 
+// Where the ids are looked for by many, a workgroup keeps every step-th key of the sorted list: most of a search is then in LDS.
+constexpr int kSamples = 1024;
+
 // The sums: G lanes along a row (and blockIdx.y where a row is longer), a segment each.  keys and pos: sorted, with 8 more than n that
 // may be read.
 template <class S, class GT, int VEC, int G>
@@ -265,13 +268,20 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restric
     constexpr int U = 8;
     if ((int64_t)blockIdx.x >= a.sum_blocks) {
         // Rows of ids that do not occur: 64 of them a workgroup, a lane looks for one of them, then the wavefronts clear them in turn.
+        __shared__ int32_t samples[kSamples];
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int64_t every = (a.n + kSamples - 1) / kSamples;
+        const int count = every > 0 ? (int)((a.n + every - 1) / every) : 0;
+        for (int i = threadIdx.x; i < count; i += kThreads) samples[i] = keys[i * every];
+        __syncthreads();
         const int64_t step = ((int64_t)gridDim.x - a.sum_blocks) * 64;
         for (int64_t v0 = ((int64_t)blockIdx.x - a.sum_blocks) * 64; v0 < a.V; v0 += step) {
             const int64_t v = v0 + lane;
             bool absent = false;
             if (v < a.V) {
-                const int64_t i = lower_bound(keys, 0, a.n, (int)v);
+                // the first sample that is not smaller; the key itself is not before the sample before it
+                const int64_t s = lower_bound(samples, 0, count, (int)v);
+                const int64_t i = lower_bound(keys, s > 0 ? (s - 1) * every + 1 : 0, min(a.n, s * every), (int)v);
                 absent = i >= a.n || keys[i] != (int)v;
             }
             unsigned long long rows = __ballot(absent);
@@ -383,9 +393,13 @@ Layout layout(int64_t V, int64_t D, int64_t n) {
     l.passes = (all + kMaxBits - 1) / kMaxBits;
     l.bits = (all + l.passes - 1) / l.passes;
     l.tiles = (n + kTile - 1) / kTile;
-    // Segments of 32 tokens at least; no more than 4096 of them, which bounds what a run over all of them costs to join.
+    // Short segments where tokens are few, so that there are some thousand wavefronts (2^21 elements of 8 a lane make 4096 of them); no
+    // more than 4096 segments, which bounds what a run over all of them costs to join.
     int64_t s = (n + 4095) / 4096;
-    s = s < 32 ? 32 : s;
+    const int64_t even = n * D >> 21;
+    if (even > s) s = even;
+    if (s < 8) s = 8;
+    if (s > 1 << 20) s = 1 << 20;
     l.segment = (int)((s + 7) & ~(int64_t)7);
     l.segments = (n + l.segment - 1) / l.segment;
     size_t at = 0;

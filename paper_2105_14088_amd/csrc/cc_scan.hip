@@ -309,7 +309,12 @@ __global__ __launch_bounds__(64 * kParts) void scan_chain_kernel(float* products
     }
 }
 
-// Segments for B sequences of T positions and D channels: as many as make 2^17 threads, of 64 positions at least.
+// Segments for B sequences of T positions and D channels: as many as make 2^17 threads, of 32 positions at least; fewer than four
+// cost more in launches and second readings than their threads bring.  Forward and backward in us, bf16, by segments:
+//   8 x 4096 x 512     1: 490, 924   16: 68, 95    64: 41, 54   128: 41, 52
+//   32 x 1024 x 1024   1: 126, 274    2: 126, 202   8: 62, 94    32: 63, 90
+//   64 x 1024 x 1024   1: 150, 293    2: 152, 223   4: 126, 188  16: 136, 202
+//   1024 x 64 x 64     1: 13, 22      2: 18, 23     4: 17, 21
 struct Split {
     int64_t segment;
     int segments;
@@ -317,7 +322,8 @@ struct Split {
 Split split(int64_t B, int64_t T, int64_t D) {
     const int64_t threads = B * ((D + 1) / 2);
     int64_t want = threads > 0 ? ((1 << 17) + threads - 1) / threads : 1;
-    if (want > T / 64) want = T / 64;
+    if (want > T / 32) want = T / 32;
+    if (want < 4) want = 1;
     if (want > 16384) want = 16384;
     if (want < 1) want = 1;
     Split s;

@@ -706,48 +706,55 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(const double* _
     }
 }
 
-// A pair: its margin, its share of the loss, and the slope of its two sequences' log-probabilities.  WAVES wavefronts share a pair's
-// positions.  Where one workgroup has all pairs it also adds their shares up; else pair_sum_kernel does.
-template <int THREADS, int WAVES>
+// A pair: its margin, its share of the loss, and the slope of its two sequences' log-probabilities.
+__device__ __forceinline__ double finish_pair(double gap, int64_t p, int64_t pairs, float beta, float smoothing, float* __restrict__ margin,
+                                              float* __restrict__ slope) {
+    const double m = (double)beta * gap;
+    // softplus(x) = max(x, 0) + log1p(exp(-|x|))
+    const double small = exp(-fabs(m)), tail = log1p(small), part = small / (1.0 + small);
+    const double away = m >= 0.0 ? part : 1.0 - part, by = m >= 0.0 ? 1.0 - part : part;       // sigmoid(-m), sigmoid(m)
+    const float s = (float)((double)beta / (double)pairs * ((double)smoothing * by - (1.0 - (double)smoothing) * away));
+    margin[p] = (float)m;
+    slope[p] = s;
+    slope[p + pairs] = -s;
+    return ((1.0 - (double)smoothing) * (fmax(-m, 0.0) + tail) + (double)smoothing * (fmax(m, 0.0) + tail)) / (double)pairs;
+}
+
+// TEAM threads share a pair's positions: one where they are few (a pair's 64-bit functions are then taken for 64 pairs at once), a
+// workgroup's wavefronts or all of it where they are many.  Where one workgroup has all pairs it also adds their shares up; else
+// pair_sum_kernel does.
+template <int THREADS, int TEAM>
 __global__ __launch_bounds__(THREADS) void pair_kernel(const double* __restrict__ gaps, int64_t pairs, int64_t T, float beta, float smoothing,
                                                        float* __restrict__ margin, float* __restrict__ slope, double* __restrict__ losses,
                                                        float* __restrict__ loss) {
-    constexpr int TEAMS = THREADS / 64 / WAVES;
+    constexpr int TEAMS = THREADS / TEAM;
     __shared__ double lds[THREADS / 64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, team = wave / WAVES, member = wave % WAVES;
+    const int wave = threadIdx.x >> 6, team = threadIdx.x / TEAM, member = threadIdx.x % TEAM;
     double sum = 0.0;
     for (int64_t p0 = (int64_t)blockIdx.x * TEAMS; p0 < pairs; p0 += (int64_t)gridDim.x * TEAMS) {
         const int64_t p = p0 + team;
         double gap = 0.0;
         if (p < pairs) {
 #pragma unroll 4
-            for (int64_t t = member * 64 + lane; t < T; t += WAVES * 64) gap += gaps[p * T + t] - gaps[(p + pairs) * T + t];
+            for (int64_t t = member; t < T; t += TEAM) gap += gaps[p * T + t] - gaps[(p + pairs) * T + t];
         }
-        gap = wave_sum_f64(gap);
-        if (WAVES > 1) {
-            if (lane == 0) lds[wave] = gap;
+        if (TEAM >= 64) gap = wave_sum_f64(gap);
+        if (TEAM > 64) {
+            if ((threadIdx.x & 63) == 0) lds[wave] = gap;
             __syncthreads();
             gap = 0.0;
-            for (int w = 0; w < WAVES; ++w) gap += lds[team * WAVES + w];
+            for (int w = 0; w < TEAM / 64; ++w) gap += lds[team * (TEAM / 64) + w];
             __syncthreads();
         }
-        if (member == 0 && lane == 0 && p < pairs) {
-            const double m = (double)beta * gap;
-            // softplus(x) = max(x, 0) + log1p(exp(-|x|))
-            const double tail = log1p(exp(-fabs(m)));
-            const double wrong = fmax(-m, 0.0) + tail, right = fmax(m, 0.0) + tail;
-            const double share = ((1.0 - (double)smoothing) * wrong + (double)smoothing * right) / (double)pairs;
-            const double away = 1.0 / (1.0 + exp(m)), by = 1.0 / (1.0 + exp(-m));
-            const float s = (float)((double)beta / (double)pairs * ((double)smoothing * by - (1.0 - (double)smoothing) * away));
-            margin[p] = (float)m;
-            slope[p] = s;
-            slope[p + pairs] = -s;
+        if (member == 0 && p < pairs) {
+            const double share = finish_pair(gap, p, pairs, beta, smoothing, margin, slope);
             if (loss) sum += share;
             else losses[p] = share;
         }
     }
     if (!loss) return;
-    if (lane == 0) lds[wave] = sum;
+    sum = wave_sum_f64(sum);
+    if ((threadIdx.x & 63) == 0) lds[wave] = sum;
     __syncthreads();
     if (threadIdx.x != 0) return;
     sum = 0.0;
@@ -920,13 +927,20 @@ hipError_t run(TokenKind kind, const TokenCall& c, hipStream_t s) {
     if (any) launch_rows<S, kTokenForward>(a, c.placed, s);
     double* const losses = (double*)(w + l.losses);
     float* const slopes = (float*)(w + l.counts);
-    if (pairs * c.T <= 8192) {
-        // one workgroup takes 6.5 us for 4 x 777 positions, two launches 9.2; for 32 x 1000 it is 18 against 9.3
-        const auto kernel = pairs <= 4 ? pair_kernel<1024, 4> : pair_kernel<1024, 1>;
-        hipLaunchKernelGGL(kernel, dim3(1), dim3(1024), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin, slopes, losses, c.stats);
+    if (c.T <= 64 && pairs <= 1024) {
+        // a thread per pair, one workgroup
+        hipLaunchKernelGGL((pair_kernel<1024, 1>), dim3(1), dim3(1024), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin, slopes, losses,
+                           c.stats);
+    } else if (pairs <= 4 && c.T <= 2048) {
+        // 4 x 777 positions: 6.5 us in one workgroup, 9.2 in two launches; 32 x 1000: 18 against 9.3
+        hipLaunchKernelGGL((pair_kernel<1024, 256>), dim3(1), dim3(1024), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin, slopes, losses,
+                           c.stats);
     } else {
-        hipLaunchKernelGGL((pair_kernel<256, 4>), dim3((unsigned)(pairs < 65536 ? pairs : 65536)), dim3(256), 0, s, a.gaps, pairs, c.T, c.beta,
-                           c.smoothing, c.margin, slopes, losses, (float*)nullptr);
+        const int64_t teams = c.T <= 64 ? 256 : 1, blocks = (pairs + teams - 1) / teams;
+        const auto kernel = c.T <= 64 ? pair_kernel<256, 1> : pair_kernel<256, 256>;
+        if (pairs > 0)
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing,
+                               c.margin, slopes, losses, (float*)nullptr);
         hipLaunchKernelGGL(pair_sum_kernel, dim3(1), dim3(kSumThreads), 0, s, losses, pairs, c.stats);
     }
     if (any && c.grad) {

@@ -5,6 +5,7 @@ As in binding.py, only arguments are marshalled here: device tensors in, device 
 one given.  Tensors may be strided as long as their last dimension is contiguous; a tensor made here is contiguous."""
 from __future__ import annotations
 
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -25,28 +26,42 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     return code
 
 
+# A small call is bound by what Python does for it: a tensor that is as it should be is looked at once, and what is wrong
+# with another is found out afterwards.
 def _strided(t: torch.Tensor, shape, dtype, name: str):
     """Where a tensor with a contiguous last dimension lies, and its other strides."""
+    strides = t.stride()
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and (strides[-1] == 1 or shape[-1] <= 1):
+        return (t.data_ptr(), *strides[:-1])
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if t.dtype is not dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {list(shape)}")
-    strides = t.stride()
-    if strides[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{name}'s last dimension must be contiguous")
-    return (t.data_ptr(), *strides[:-1])
+    raise ValueError(f"{name}'s last dimension must be contiguous")
 
 
-def _fp32(t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
-    if t is not None and tuple(t.shape) != tuple(shape):
+def _plain(t: Optional[torch.Tensor], shape, dtype, name: str) -> Optional[int]:
+    """Where a contiguous tensor lies, or None for none."""
+    if t is None:
+        return None
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}")
-    return _dev(t, torch.float32, name)
+    return _dev(t, dtype, name)
 
 
-def _int32(t: torch.Tensor, shape, name: str) -> int:
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {list(shape)}")
-    return _dev(t, torch.int32, name)
+@functools.lru_cache(maxsize=4096)
+def _scan_bytes(b: int, t: int, d: int) -> int:
+    return lib().cc_gated_scan_workspace_bytes(b, t, d)
+
+
+@functools.lru_cache(maxsize=4096)
+def _embed_bytes(v: int, d: int, n: int) -> int:
+    return lib().cc_embed_workspace_bytes(v, d, n)
+
+
+@functools.lru_cache(maxsize=4096)
+def _token_bytes(b: int, t: int) -> int:
+    return lib().cc_token_workspace_bytes(b, t)
 
 
 def _workspace(workspace: Optional[torch.Tensor], nbytes: int, device, stream):
@@ -107,7 +122,7 @@ def cc_embed_backward(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: 
         to_code = _dtype(grad_table, "grad_table")
         to, to_apart = _strided(grad_table, (vocab, d), grad_table.dtype, "grad_table")
     L = lib()
-    held, ws, nbytes = _workspace(workspace, L.cc_embed_workspace_bytes(vocab, d, n), grad.device, stream)
+    held, ws, nbytes = _workspace(workspace, _embed_bytes(vocab, d, n), grad.device, stream)
     _check(L.cc_embed_backward(where, code, n, d, apart, _dev(ids, torch.int32, "ids"), vocab, scale, to, to_code, to_apart,
                                1 if accumulate else 0, ws, nbytes, _stream(stream)), "cc_embed_backward")
     return grad_table
@@ -138,10 +153,10 @@ def cc_gated_scan(x: torch.Tensor, gate: torch.Tensor, h0: Optional[torch.Tensor
     if states is None and save_states:
         states = _new(kept, torch.float32, x.device, stream)
     L = lib()
-    held, ws, nbytes = _workspace(workspace, L.cc_gated_scan_workspace_bytes(b, t, d), x.device, stream)
+    held, ws, nbytes = _workspace(workspace, _scan_bytes(b, t, d), x.device, stream)
     _check(L.cc_gated_scan(*_strided(x, shape, x.dtype, "x"), *_strided(gate, shape, x.dtype, "gate"), code, b, t, d,
-                           _int32(lengths, (b,), "lengths"), _fp32(h0, (b, d), "h0"), *_strided(out, shape, x.dtype, "out"),
-                           _fp32(last, (b, d), "last"), _fp32(states, kept, "states"), ws, nbytes, _stream(stream)),
+                           _plain(lengths, (b,), torch.int32, "lengths"), _plain(h0, (b, d), torch.float32, "h0"), *_strided(out, shape, x.dtype, "out"),
+                           _plain(last, (b, d), torch.float32, "last"), _plain(states, kept, torch.float32, "states"), ws, nbytes, _stream(stream)),
            "cc_gated_scan")
     return out, last, states
 
@@ -164,12 +179,12 @@ def cc_gated_scan_backward(x: torch.Tensor, gate: torch.Tensor, states: torch.Te
         grad_h0 = _new((b, d), torch.float32, x.device, stream)
     kept = (b, (t + CC_SCAN_CHUNK - 1) // CC_SCAN_CHUNK, d)
     L = lib()
-    held, ws, nbytes = _workspace(workspace, L.cc_gated_scan_workspace_bytes(b, t, d), x.device, stream)
+    held, ws, nbytes = _workspace(workspace, _scan_bytes(b, t, d), x.device, stream)
     _check(L.cc_gated_scan_backward(*_strided(x, shape, x.dtype, "x"), *_strided(gate, shape, x.dtype, "gate"), code, b, t, d,
-                                    _int32(lengths, (b,), "lengths"), _fp32(states, kept, "states"),
-                                    *_strided(grad_h, shape, x.dtype, "grad_h"), _fp32(grad_last, (b, d), "grad_last"),
+                                    _plain(lengths, (b,), torch.int32, "lengths"), _plain(states, kept, torch.float32, "states"),
+                                    *_strided(grad_h, shape, x.dtype, "grad_h"), _plain(grad_last, (b, d), torch.float32, "grad_last"),
                                     *_strided(grad_x, shape, x.dtype, "grad_x"),
-                                    *_strided(grad_gate, shape, x.dtype, "grad_gate"), _fp32(grad_h0, (b, d), "grad_h0"),
+                                    *_strided(grad_gate, shape, x.dtype, "grad_gate"), _plain(grad_h0, (b, d), torch.float32, "grad_h0"),
                                     ws, nbytes, _stream(stream)), "cc_gated_scan_backward")
     return grad_x, grad_gate, grad_h0
 
@@ -204,7 +219,7 @@ def _logits(logits: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Ten
         if mask.dtype not in (torch.bool, torch.uint8) or mask.shape != positions:
             raise ValueError("mask must be bool or uint8 [B, T]")
         at = _dev(mask, mask.dtype, "mask")
-    return (where, code, *shape, sb, st, _int32(tokens, positions, "tokens"), at, 1 if placed else 0, scale), positions
+    return (where, code, *shape, sb, st, _plain(tokens, positions, torch.int32, "tokens"), at, 1 if placed else 0, scale), positions
 
 
 def _gradient(logits: torch.Tensor, grad_logits: Optional[torch.Tensor], stream):
@@ -222,7 +237,7 @@ def cc_token_logprob(logits: torch.Tensor, tokens: torch.Tensor, mask: Optional[
         logprob = _new(positions, torch.float32, logits.device, stream)
     if rows is None:
         rows = _new((*positions, 2), torch.float32, logits.device, stream)
-    _check(lib().cc_token_logprob(*args, _fp32(logprob, positions, "logprob"), _fp32(rows, (*positions, 2), "rows"),
+    _check(lib().cc_token_logprob(*args, _plain(logprob, positions, torch.float32, "logprob"), _plain(rows, (*positions, 2), torch.float32, "rows"),
                                   _stream(stream)), "cc_token_logprob")
     return logprob, rows
 
@@ -233,8 +248,8 @@ def cc_token_logprob_backward(logits: torch.Tensor, tokens: torch.Tensor, mask: 
     """grad_logits [B, T, V]; the first five arguments are cc_token_logprob's.  `grad_logits` may be the logits."""
     args, positions = _logits(logits, tokens, mask, placed, scale)
     grad_logits, to = _gradient(logits, grad_logits, stream)
-    _check(lib().cc_token_logprob_backward(*args, _fp32(rows, (*positions, 2), "rows"),
-                                           _fp32(grad_logprob, positions, "grad_logprob"), grad_scale, *to, _stream(stream)),
+    _check(lib().cc_token_logprob_backward(*args, _plain(rows, (*positions, 2), torch.float32, "rows"),
+                                           _plain(grad_logprob, positions, torch.float32, "grad_logprob"), grad_scale, *to, _stream(stream)),
            "cc_token_logprob_backward")
     return grad_logits
 
@@ -261,9 +276,9 @@ def cc_policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logprob: torc
     stats = _new(3, torch.float32, logits.device, stream)
     logprob = _new(positions, torch.float32, logits.device, stream)
     L = lib()
-    held, ws, nbytes = _workspace(workspace, L.cc_token_workspace_bytes(*positions), logits.device, stream)
-    _check(L.cc_policy_loss(*args, _fp32(old_logprob, positions, "old_logprob"), _fp32(ref_logprob, positions, "ref_logprob"),
-                            _fp32(advantage, positions if per_token else positions[:1], "advantage"), 1 if per_token else 0,
+    held, ws, nbytes = _workspace(workspace, _token_bytes(*positions), logits.device, stream)
+    _check(L.cc_policy_loss(*args, _plain(old_logprob, positions, torch.float32, "old_logprob"), _plain(ref_logprob, positions, torch.float32, "ref_logprob"),
+                            _plain(advantage, positions if per_token else positions[:1], torch.float32, "advantage"), 1 if per_token else 0,
                             clip_low, clip_high, kl_coef, MEANS[mean], grad_scale, stats.data_ptr(), logprob.data_ptr(), *to,
                             ws, nbytes, _stream(stream)), "cc_policy_loss")
     return PolicyLoss(stats, logprob, grad_logits if grad else None)
@@ -284,8 +299,8 @@ def cc_preference_loss(logits: torch.Tensor, tokens: torch.Tensor, ref_logprob: 
     margin = _new(positions[0] // 2, torch.float32, logits.device, stream)
     logprob = _new(positions, torch.float32, logits.device, stream)
     L = lib()
-    held, ws, nbytes = _workspace(workspace, L.cc_token_workspace_bytes(*positions), logits.device, stream)
-    _check(L.cc_preference_loss(*args, _fp32(ref_logprob, positions, "ref_logprob"), beta, label_smoothing, grad_scale,
+    held, ws, nbytes = _workspace(workspace, _token_bytes(*positions), logits.device, stream)
+    _check(L.cc_preference_loss(*args, _plain(ref_logprob, positions, torch.float32, "ref_logprob"), beta, label_smoothing, grad_scale,
                                 loss.data_ptr(), margin.data_ptr(), logprob.data_ptr(), *to, ws, nbytes, _stream(stream)),
            "cc_preference_loss")
     return PreferenceLoss(loss, margin, logprob, grad_logits if grad else None)
