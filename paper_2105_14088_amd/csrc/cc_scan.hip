@@ -29,21 +29,39 @@ using namespace ccm;
 constexpr int kThreads = 256, L = kScanChunk;
 
 // keep and take from e = exp(-|gate|): 1 / (1 + e) and e / (1 + e), neither of them as one minus the other, so that both keep
-// their relative precision.  The smaller one is held as two factors, each with half of the exponential's argument: what it
-// multiplies is then rounded once where the product is subnormal, and the exponential instruction, which gives 0 for
-// subnormal results, is never asked for one that matters.
+// their relative precision.
+//
+// The smaller one is held as two factors, each with half of the exponential's argument.  What it multiplies is then rounded once
+// where the product is subnormal, and the exponential instruction, which gives 0 for subnormal results, is never asked for
+// one that matters.  MIXED: gates of up to kMild need none of that, and are the same as MildGates to the last bit, wherever a
+// position is worked on: in a chunk, at its end or alone.
+constexpr float kMild = 64.0f;
+template <bool MIXED>
 struct Gates {
     float keep1, keep2, take1, take2;
     __device__ __forceinline__ explicit Gates(float g) {
-        const float half = exp_fast(-0.5f * fabsf(g)), large = __builtin_amdgcn_rcpf(fmaf(half, half, 1.0f)), small2 = half * large;
-        keep1 = g >= 0.0f ? 1.0f : half;
+        const bool mild = MIXED && fabsf(g) <= kMild;
+        const float q = exp_fast(mild ? -fabsf(g) : -0.5f * fabsf(g)), other = mild ? 1.0f : q;
+        const float large = __builtin_amdgcn_rcpf(fmaf(q, other, 1.0f)), small2 = q * large;
+        keep1 = g >= 0.0f ? 1.0f : other;
         keep2 = g >= 0.0f ? large : small2;
-        take1 = g >= 0.0f ? half : 1.0f;
+        take1 = g >= 0.0f ? other : 1.0f;
         take2 = g >= 0.0f ? small2 : large;
     }
     __device__ __forceinline__ float keep(float v) const { return v * keep1 * keep2; }
     __device__ __forceinline__ float take(float v) const { return v * take1 * take2; }
     __device__ __forceinline__ float step(float h, float x) const { return fmaf(h * keep1, keep2, take(x)); }
+};
+struct MildGates {
+    float k, t;
+    __device__ __forceinline__ explicit MildGates(float g) {
+        const float e = exp_fast(-fabsf(g)), large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
+        k = g >= 0.0f ? large : small;
+        t = g >= 0.0f ? small : large;
+    }
+    __device__ __forceinline__ float keep(float v) const { return v * k; }
+    __device__ __forceinline__ float take(float v) const { return v * t; }
+    __device__ __forceinline__ float step(float h, float x) const { return fmaf(h, k, take(x)); }
 };
 
 struct Args {
@@ -127,6 +145,25 @@ __device__ __forceinline__ void read(const Rows<float, C, Off>& r, int64_t t, fl
 template <int C, class Off>
 __device__ __forceinline__ void write(const Rows<float, C, Off>& r, int64_t t, const float v[C]) { r.store(r.at(t), 0, v); }
 
+// MILD kernels ask whether a wavefront's gates of a chunk can be MildGates: five operations fewer each, for elements of 16 bits, whose
+// walks wait for operations as much as for memory (32 x 1024 x 1024 bf16, forward and backward: 162 us with Gates alone, 152 so;
+// of 32 bits there is no difference).
+template <class S, int C>
+__device__ __forceinline__ bool mild(const Pack<S, C> gs[L]) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int c = 0; c < C; ++c) top = fmaxf(top, fabsf(gs[i].get(c)));
+    return __all(top <= kMild);
+}
+// Nothing that was made of a chunk's rows before the ways part is kept beside them.
+template <class S, int C>
+__device__ __forceinline__ void forget_rows(Pack<S, C> rows[L]) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) forget(rows[i]);
+}
+
 // What the length leaves of a chunk: all of it in all lanes, or something in some.
 struct Part {
     int count, inside;                // positions of the segment, positions that count
@@ -139,7 +176,7 @@ struct Part {
 };
 
 // Forward walk.  SUMMARY: only the segment's product of keeps and what it adds; the last segment needs none.
-template <class S, int C, class Off, bool SUMMARY>
+template <class S, int C, class Off, bool MILD, bool SUMMARY>
 __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
     const Lane<C> l(a);
     if (!l.real) return;
@@ -155,13 +192,21 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
         if (a.starts) read<C>(starts, seg, h);
         else if (a.h0) read<C>(h0, 0, h);
     }
-    const auto walk = [&](auto whole, int64_t t0, const Part& part) {
-        constexpr bool FULL = decltype(whole)::value;
+    struct Chunk {
         Pack<S, C> xs[L], gs[L];
-        if (FULL || part.inside > 0) {
-            x.template load_chunk<FULL>(t0, part.inside, xs);
-            g.template load_chunk<FULL>(t0, part.inside, gs);
-        }
+    };
+    const auto load = [&](auto whole, int64_t t0, int inside, Chunk& to) {
+        constexpr bool FULL = decltype(whole)::value;
+        x.template load_chunk<FULL>(t0, inside, to.xs);
+        g.template load_chunk<FULL>(t0, inside, to.gs);
+    };
+    // FULL: the chunk counts as a whole and, in a MILD kernel, its gates are mild
+    const auto walk = [&](auto whole, int64_t t0, const Part& part, const Chunk& loaded) {
+        constexpr bool FULL = decltype(whole)::value;
+        using Gate = std::conditional_t<FULL && MILD, MildGates, Gates<sizeof(S) == 2>>;
+        Chunk own;
+        if (!MILD && (FULL || part.inside > 0)) load(whole, t0, part.inside, own);
+        const Chunk& rows = MILD ? loaded : own;
         S* const to_row = SUMMARY ? nullptr : out.at(t0);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
@@ -169,8 +214,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
             float shown[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const Gates gate(gs[i].get(c));
-                const float next = gate.step(h[c], xs[i].get(c));
+                const Gate gate(rows.gs[i].get(c));
+                const float next = gate.step(h[c], rows.xs[i].get(c));
                 h[c] = in ? next : h[c];
                 if (SUMMARY) product[c] = in ? gate.keep(product[c]) : product[c];
                 shown[c] = in ? next : 0.0f;
@@ -181,8 +226,17 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
     for (int64_t t0 = from; t0 < to; t0 += L) {
         const Part part(t0, to, end);
         if (!SUMMARY && a.states) write<C>(states, t0 / L, h);
-        if (part.full) walk(std::true_type(), t0, part);
-        else walk(std::false_type(), t0, part);
+        bool whole = part.full;
+        Chunk rows;
+        if (MILD) {
+            if (part.full) load(std::true_type(), t0, L, rows);
+            else if (part.inside > 0) load(std::false_type(), t0, part.inside, rows);
+            whole = part.full && mild<S, C>(rows.gs);
+            forget_rows(rows.gs);
+            forget_rows(rows.xs);
+        }
+        if (whole) walk(std::true_type(), t0, part, rows);
+        else walk(std::false_type(), t0, part, rows);
     }
     if (SUMMARY) {
         write<C>(products, seg, product);
@@ -193,8 +247,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
 }
 
 // Backward walk.  SUMMARY: only the segment's product of keeps and what it sends back; the first segment needs none.
-template <class S, int C, class Off, bool SUMMARY>
-__global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) void scan_backward_kernel(Args a) {
+template <class S, int C, class Off, bool MILD, bool SUMMARY>
+__global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 || MILD ? 3 : 4) void scan_backward_kernel(Args a) {
     const Lane<C> l(a);
     if (!l.real) return;
     const int seg = SUMMARY ? blockIdx.y + 1 : blockIdx.y;
@@ -210,17 +264,24 @@ __global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) voi
         if (a.starts) read<C>(starts, seg, f);
         else if (a.last_grad) read<C>(last_grad, 0, f);
     }
-    const auto walk = [&](auto whole, int64_t t0, const Part& part) {
-        constexpr bool FULL = decltype(whole)::value;
+    struct Chunk {
         Pack<S, C> xs[L], gs[L], ds[L];
+    };
+    const auto load = [&](auto whole, int64_t t0, int inside, Chunk& to) {
+        constexpr bool FULL = decltype(whole)::value;
+        g.template load_chunk<FULL>(t0, inside, to.gs);
+        dh.template load_chunk<FULL>(t0, inside, to.ds);
+        if (!SUMMARY) x.template load_chunk<FULL>(t0, inside, to.xs);
+    };
+    const auto walk = [&](auto whole, int64_t t0, const Part& part, const Chunk& loaded) {
+        constexpr bool FULL = decltype(whole)::value;
+        using Gate = std::conditional_t<FULL && MILD, MildGates, Gates<sizeof(S) == 2>>;
+        Chunk rows;
         float before[L][C], h[C] = {};
+        if (MILD) rows = loaded;
         if (FULL || part.inside > 0) {
-            g.template load_chunk<FULL>(t0, part.inside, gs);
-            dh.template load_chunk<FULL>(t0, part.inside, ds);
-            if (!SUMMARY) {
-                x.template load_chunk<FULL>(t0, part.inside, xs);
-                read<C>(states, t0 / L, h);
-            }
+            if (!MILD) load(whole, t0, part.inside, rows);
+            if (!SUMMARY) read<C>(states, t0 / L, h);
         }
         if (!SUMMARY) {
 #pragma unroll
@@ -228,13 +289,13 @@ __global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) voi
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
                     before[i][c] = h[c];
-                    if (i + 1 < L) h[c] = Gates(gs[i].get(c)).step(h[c], xs[i].get(c));   // of use where position i + 1 counts
+                    if (i + 1 < L) h[c] = Gate(rows.gs[i].get(c)).step(h[c], rows.xs[i].get(c));   // of use where position i + 1 counts
                 }
         }
         // The gates are made again on the way back: kept, a chunk's would take 128 registers and three quarters of the wavefronts.
         if (!SUMMARY) {
 #pragma unroll
-            for (int i = 0; i < L; ++i) forget(gs[i]);
+            for (int i = 0; i < L; ++i) forget(rows.gs[i]);
         }
         S* const dx_row = SUMMARY ? nullptr : dx_out.at(t0);
         S* const dg_row = SUMMARY ? nullptr : dg_out.at(t0);
@@ -244,14 +305,14 @@ __global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) voi
             float dx[C], dg[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const Gates gate(gs[i].get(c));
-                const float lambda = ds[i].get(c) + f[c];
+                const Gate gate(rows.gs[i].get(c));
+                const float lambda = rows.ds[i].get(c) + f[c];
                 f[c] = in ? gate.keep(lambda) : f[c];
                 if (SUMMARY) {
                     product[c] = in ? gate.keep(product[c]) : product[c];
                 } else {
                     dx[c] = in ? gate.take(lambda) : 0.0f;
-                    dg[c] = in ? gate.keep(gate.take(lambda * (before[i][c] - xs[i].get(c)))) : 0.0f;
+                    dg[c] = in ? gate.keep(gate.take(lambda * (before[i][c] - rows.xs[i].get(c)))) : 0.0f;
                 }
             }
             if (!SUMMARY && (FULL || i < part.count)) {
@@ -262,8 +323,19 @@ __global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 ? 3 : 4) voi
     };
     for (int64_t t0 = to > from ? from + (to - from - 1) / L * L : from - L; t0 >= from; t0 -= L) {
         const Part part(t0, to, end);
-        if (part.full) walk(std::true_type(), t0, part);
-        else walk(std::false_type(), t0, part);
+        bool whole = part.full;
+        Chunk rows;
+        if (MILD) {
+            if (part.full) load(std::true_type(), t0, L, rows);
+            else if (part.inside > 0) load(std::false_type(), t0, part.inside, rows);
+            whole = part.full && mild<S, C>(rows.gs);
+            forget_rows(rows.gs);
+            forget_rows(rows.ds);
+            if (!SUMMARY) forget_rows(rows.xs);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (whole) walk(std::true_type(), t0, part, rows);
+        else walk(std::false_type(), t0, part, rows);
     }
     if (SUMMARY) {
         write<C>(products, seg, product);
@@ -357,7 +429,7 @@ Args arguments(const ScanCall& c, const Split& s, int channels) {
     return a;
 }
 
-template <class S, int C, class Off>
+template <class S, int C, class Off, bool MILD>
 hipError_t forward(const ScanCall& c, hipStream_t s) {
     const Split p = split(c.B, c.T, c.D);
     Args a = arguments(c, p, C);
@@ -367,15 +439,15 @@ hipError_t forward(const ScanCall& c, hipStream_t s) {
     const unsigned blocks = (unsigned)((c.B * a.lanes + kThreads - 1) / kThreads);
     const int64_t row = c.B * c.D;
     if (p.segments > 1) {
-        hipLaunchKernelGGL((scan_kernel<S, C, Off, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((scan_kernel<S, C, Off, MILD, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
         hipLaunchKernelGGL((scan_chain_kernel<false>), dim3((unsigned)((row + 63) / 64)), dim3(64 * kParts), 0, s, a.products, a.sums, c.h0,
                            p.segments, row);
     }
-    hipLaunchKernelGGL((scan_kernel<S, C, Off, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((scan_kernel<S, C, Off, MILD, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
-template <class S, int C, class Off>
+template <class S, int C, class Off, bool MILD>
 hipError_t backward(const ScanCall& c, hipStream_t s) {
     const Split p = split(c.B, c.T, c.D);
     Args a = arguments(c, p, C);
@@ -387,11 +459,11 @@ hipError_t backward(const ScanCall& c, hipStream_t s) {
     const unsigned blocks = (unsigned)((c.B * a.lanes + kThreads - 1) / kThreads);
     const int64_t row = c.B * c.D;
     if (p.segments > 1) {
-        hipLaunchKernelGGL((scan_backward_kernel<S, C, Off, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((scan_backward_kernel<S, C, Off, MILD, true>), dim3(blocks, p.segments - 1), dim3(kThreads), 0, s, a);
         hipLaunchKernelGGL((scan_chain_kernel<true>), dim3((unsigned)((row + 63) / 64)), dim3(64 * kParts), 0, s, a.products, a.sums,
                            (const float*)c.last, p.segments, row);
     }
-    hipLaunchKernelGGL((scan_backward_kernel<S, C, Off, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((scan_backward_kernel<S, C, Off, MILD, false>), dim3(blocks, p.segments), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
@@ -412,9 +484,10 @@ hipError_t choose(const ScanCall& c, hipStream_t s) {
     // overwritten it with the last.
     const void *in = BACKWARD ? (const void*)c.last : (const void*)c.h0, *out = BACKWARD ? (const void*)c.grad_h0 : (const void*)c.last;
     const bool in_place = in && in == out;
-    if (c.D == 1 || ((c.D & 1) && in_place)) return BACKWARD ? backward<S, 1, uint64_t>(c, s) : forward<S, 1, uint64_t>(c, s);
-    if (all_near(c, BACKWARD)) return BACKWARD ? backward<S, 2, uint32_t>(c, s) : forward<S, 2, uint32_t>(c, s);
-    return BACKWARD ? backward<S, 2, uint64_t>(c, s) : forward<S, 2, uint64_t>(c, s);
+    if (c.D == 1 || ((c.D & 1) && in_place)) return BACKWARD ? backward<S, 1, uint64_t, false>(c, s) : forward<S, 1, uint64_t, false>(c, s);
+    if (!all_near(c, BACKWARD)) return BACKWARD ? backward<S, 2, uint64_t, false>(c, s) : forward<S, 2, uint64_t, false>(c, s);
+    if constexpr (sizeof(S) == 2) return BACKWARD ? backward<S, 2, uint32_t, true>(c, s) : forward<S, 2, uint32_t, true>(c, s);
+    else return BACKWARD ? backward<S, 2, uint32_t, false>(c, s) : forward<S, 2, uint32_t, false>(c, s);
 }
 
 }  // namespace
