@@ -21,6 +21,9 @@
 #include "cc_internal.h"
 #include "cc_model.h"
 
+// A position gives the same bits whichever walk it is worked in: products and sums are fused where fmaf says so and nowhere else.
+#pragma clang fp contract(off)
+
 namespace cc {
 namespace {
 
@@ -125,7 +128,13 @@ struct Rows {
     __device__ __forceinline__ Pack<S, C> load_own(const S* p, int i) const {      // i differs between lanes
         return load_pack<C>((const S*)((const char*)p + (Off)(lane + (Off)i * ((Off)stride * (Off)sizeof(S)))));
     }
-    __device__ __forceinline__ void store(S* p, int i, const float v[C]) const {
+    // What is stored is a value of 32 bits that is rounded: an instruction that rounds a sum of products to f16 at once, where the
+    // compiler finds its form, would store other bits in one walk than in another.
+    __device__ __forceinline__ void store(S* p, int i, float v[C]) const {
+        if (__is_same(S, _Float16)) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) asm("" : "+v"(v[c]));
+        }
         store_pack((S*)((char*)(p + i * stride) + lane), Pack<S, C>::from(v));
     }
     // A chunk's rows from position t on.  Of a chunk that does not count as a whole, the others' places hold the last row that does.
@@ -143,7 +152,7 @@ __device__ __forceinline__ void read(const Rows<float, C, Off>& r, int64_t t, fl
     for (int c = 0; c < C; ++c) v[c] = p.get(c);
 }
 template <int C, class Off>
-__device__ __forceinline__ void write(const Rows<float, C, Off>& r, int64_t t, const float v[C]) { r.store(r.at(t), 0, v); }
+__device__ __forceinline__ void write(const Rows<float, C, Off>& r, int64_t t, float v[C]) { r.store(r.at(t), 0, v); }
 
 // MILD kernels ask whether a wavefront's gates of a chunk can be MildGates: five operations fewer each, for elements of 16 bits, whose
 // walks wait for operations as much as for memory (32 x 1024 x 1024 bf16, forward and backward: 162 us with Gates alone, 152 so;
