@@ -261,7 +261,10 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
         bool mine, valid;
     };
     const auto stage = [&](const Position& p, int base, RowInfo* info) {
-        Batch r = {};
+        Batch r;                                      // of a row that does not count the vectors are zero, of none they are not looked at
+        r.in = {};
+        r.saved = {};
+        r.slope = r.ref = r.token_logit = 0.0f;
         r.mine = p.mine;
         r.at = p.at;
         r.valid = p.mine && !p.masked && (uint32_t)p.k < (uint32_t)V;
@@ -280,7 +283,11 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
         for (int it = 0; it < ITER; ++it) {
             if (base + it * PER >= slots) break;
             const RowInfo row = info[it * PER + group];
-            if (row.k < 0) continue;
+            if (row.k < 0) {
+#pragma unroll
+                for (int c = 0; c < K; ++c) r.packs[it][c] = Pack<S, VEC>();
+                continue;
+            }
 #pragma unroll
             for (int c = 0; c < K; ++c) r.packs[it][c] = load_pack<VEC>((const S*)a.logits + row.in + min((c * G + lane) * VEC, V - VEC));
         }
@@ -342,6 +349,11 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
         for (int it = 0; it < ITER; ++it) {
             const int at_row = it * PER + group;
             const RowInfo r = info[at_row];
+            if (!__any(r.k >= 0)) {                   // none of the groups has a row that counts
+#pragma unroll
+                for (int i = 0; i < K * VEC; ++i) e[it][i] = 0.0f;
+                continue;
+            }
             if (PLACED && orders > 1) look_up(r.o);
             const float token_logit = own[wave][at_row];
             float m = token_logit;
@@ -376,12 +388,12 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
                 float sum = 0.0f;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) sum += z[i];
-                if (j0 != j) {                        // without what the lane before it has
+                if (j0 != j && j < V) {               // without what the lane before it has
                     sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) sum += j0 + i >= j ? z[i] : 0.0f;
                 }
-                rest += sum;
+                rest += j < V ? sum : 0.0f;
             }
             if (KIND != kTokenBackward) {
                 rest = group_sum<G>(rest);
