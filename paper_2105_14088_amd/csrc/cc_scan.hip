@@ -184,7 +184,7 @@ struct Part {
     }
 };
 
-// Forward walk.  SUMMARY: only the segment's product of keeps and what it adds; the last segment needs none.
+// Forward walk.  Bound by memory (2 x 65536 x 1024 bf16: 149 us for 838 MB, 5.6 TB/s; SUMMARY reads 537 MB in 116 us).  SUMMARY: only the segment's product of keeps and what it adds; the last segment needs none.
 template <class S, int C, class Off, bool MILD, bool SUMMARY>
 __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
     const Lane<C> l(a);
@@ -255,7 +255,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args a) {
     }
 }
 
-// Backward walk.  SUMMARY: only the segment's product of keeps and what it sends back; the first segment needs none.
+// Backward walk.  (2 x 65536 x 1024 bf16: 256 us for 1.38 GB, 5.4 TB/s; SUMMARY 118 us.  A chunk's rows loaded while the one before is
+// worked on: 210 registers and the same time.)  SUMMARY: only the segment's product of keeps and what it sends back; the first segment needs none.
 template <class S, int C, class Off, bool MILD, bool SUMMARY>
 __global__ __launch_bounds__(kThreads, SUMMARY ? 0 : sizeof(S) == 4 || MILD ? 3 : 4) void scan_backward_kernel(Args a) {
     const Lane<C> l(a);

@@ -207,6 +207,10 @@ __device__ __forceinline__ void store_partial(double* out, double s0, double s1,
 // the lane before it: these are left out of the sum, and their gradient is written twice, with the same value.  Every
 // lane so has a whole vector to load and store.
 //
+// What it takes: 64000 rows of 1000 bf16 39 us forward (3.3 TB/s, some 17 vector operations per logit, exponentials and 64-bit ends of
+// rows included) and 44 us for the gradient (5.8 TB/s of 256 MB); fewer or more rows a wavefront, and more wavefronts of fewer
+// registers, are slower.
+//
 // The next batch's vectors are loaded before this one is worked, and the tokens of the one after it, which say what to load; the
 // first batch's before the order's nodes are looked up.
 struct RowInfo {
@@ -463,6 +467,8 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
 // A workgroup per row.  K > 0: the row, up to THREADS * K vectors, stays in registers as it was loaded, so that it is read once
 // for log-probability, loss and gradient; its exponentials are taken twice, since 32 bits of each would not fit.  K = 0: rows
 // longer than that are read twice.  As for short rows, a vector that would end beyond the row is moved back.
+//
+// Bound by memory: 8192 rows of 65536 bf16, loss and gradient, 340 us, 6.3 TB/s of 2.15 GB.
 //
 // The token's own term and repeated elements are taken out of the sum where they are, by the lane that has them, in a branch
 // that other wavefronts skip.
