@@ -143,7 +143,9 @@ __device__ __forceinline__ PolicyInputs policy_inputs(const Args& a, int64_t at,
 __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, const PolicyInputs& in) {
     PolicyTerms r;
     const float ratio = expf((float)(lp - (double)in.old_lp));
-    const float free_gain = ratio * in.advantage, held = fminf(fmaxf(ratio, 1.0f - a.clip_low), 1.0f + a.clip_high) * in.advantage;
+    // a ratio that 32 bits do not hold still has no part where there is no advantage, nor a divergence that counts for nothing
+    const float free_gain = in.advantage == 0.0f ? 0.0f : ratio * in.advantage;
+    const float held = fminf(fmaxf(ratio, 1.0f - a.clip_low), 1.0f + a.clip_high) * in.advantage;
     const bool clipped = held < free_gain;
     r.clipped = clipped ? 1.0f : 0.0f;
     r.loss = -(clipped ? held : free_gain);
@@ -152,8 +154,10 @@ __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, co
     if (a.ref) {
         const float away = (float)((double)in.ref - lp), grown = expm1f(away);
         r.kl = grown - away;
-        r.loss += a.kl_coef * r.kl;
-        r.slope -= a.kl_coef * grown;
+        if (a.kl_coef != 0.0f) {
+            r.loss += a.kl_coef * r.kl;
+            r.slope -= a.kl_coef * grown;
+        }
     }
     return r;
 }
