@@ -49,6 +49,23 @@ def _plain(t: Optional[torch.Tensor], shape, dtype, name: str) -> Optional[int]:
     return _dev(t, dtype, name)
 
 
+# What is made here is not looked at like what is passed in.
+def _rows_out(t: Optional[torch.Tensor], shape, dtype, device, stream, name: str):
+    """A result [A, B, C] of the caller's or made here, and where it lies with its strides."""
+    if t is None:
+        t = _new(shape, dtype, device, stream)
+        return t, (t.data_ptr(), shape[1] * shape[2], shape[2])
+    return t, _strided(t, shape, dtype, name)
+
+
+def _plain_out(t: Optional[torch.Tensor], shape, dtype, device, stream, name: str):
+    """A contiguous result of the caller's or made here, and where it lies."""
+    if t is None:
+        t = _new(shape, dtype, device, stream)
+        return t, t.data_ptr()
+    return t, _plain(t, shape, dtype, name)
+
+
 @functools.lru_cache(maxsize=4096)
 def _scan_bytes(b: int, t: int, d: int) -> int:
     return lib().cc_gated_scan_workspace_bytes(b, t, d)
@@ -145,18 +162,16 @@ def cc_gated_scan(x: torch.Tensor, gate: torch.Tensor, h0: Optional[torch.Tensor
         raise ValueError("x must be [B, T, D]")
     shape, code = x.shape, _dtype(x, "x")
     b, t, d = shape
-    if out is None:
-        out = _new(shape, x.dtype, x.device, stream)
-    if last is None:
-        last = _new((b, d), torch.float32, x.device, stream)
-    kept = (b, (t + CC_SCAN_CHUNK - 1) // CC_SCAN_CHUNK, d)
-    if states is None and save_states:
-        states = _new(kept, torch.float32, x.device, stream)
+    device = x.device
+    out, to = _rows_out(out, shape, x.dtype, device, stream, "out")
+    last, last_to = _plain_out(last, (b, d), torch.float32, device, stream, "last")
+    states_to = None
+    if states is not None or save_states:
+        states, states_to = _plain_out(states, (b, (t + CC_SCAN_CHUNK - 1) // CC_SCAN_CHUNK, d), torch.float32, device, stream, "states")
     L = lib()
     held, ws, nbytes = _workspace(workspace, _scan_bytes(b, t, d), x.device, stream)
     _check(L.cc_gated_scan(*_strided(x, shape, x.dtype, "x"), *_strided(gate, shape, x.dtype, "gate"), code, b, t, d,
-                           _plain(lengths, (b,), torch.int32, "lengths"), _plain(h0, (b, d), torch.float32, "h0"), *_strided(out, shape, x.dtype, "out"),
-                           _plain(last, (b, d), torch.float32, "last"), _plain(states, kept, torch.float32, "states"), ws, nbytes, _stream(stream)),
+                           _plain(lengths, (b,), torch.int32, "lengths"), _plain(h0, (b, d), torch.float32, "h0"), *to, last_to, states_to, ws, nbytes, _stream(stream)),
            "cc_gated_scan")
     return out, last, states
 
@@ -171,20 +186,17 @@ def cc_gated_scan_backward(x: torch.Tensor, gate: torch.Tensor, states: torch.Te
         raise ValueError("x must be [B, T, D]")
     shape, code = x.shape, _dtype(x, "x")
     b, t, d = shape
-    if grad_x is None:
-        grad_x = _new(shape, x.dtype, x.device, stream)
-    if grad_gate is None:
-        grad_gate = _new(shape, x.dtype, x.device, stream)
-    if grad_h0 is None:
-        grad_h0 = _new((b, d), torch.float32, x.device, stream)
+    device = x.device
+    grad_x, x_to = _rows_out(grad_x, shape, x.dtype, device, stream, "grad_x")
+    grad_gate, gate_to = _rows_out(grad_gate, shape, x.dtype, device, stream, "grad_gate")
+    grad_h0, h0_to = _plain_out(grad_h0, (b, d), torch.float32, device, stream, "grad_h0")
     kept = (b, (t + CC_SCAN_CHUNK - 1) // CC_SCAN_CHUNK, d)
     L = lib()
     held, ws, nbytes = _workspace(workspace, _scan_bytes(b, t, d), x.device, stream)
     _check(L.cc_gated_scan_backward(*_strided(x, shape, x.dtype, "x"), *_strided(gate, shape, x.dtype, "gate"), code, b, t, d,
                                     _plain(lengths, (b,), torch.int32, "lengths"), _plain(states, kept, torch.float32, "states"),
                                     *_strided(grad_h, shape, x.dtype, "grad_h"), _plain(grad_last, (b, d), torch.float32, "grad_last"),
-                                    *_strided(grad_x, shape, x.dtype, "grad_x"),
-                                    *_strided(grad_gate, shape, x.dtype, "grad_gate"), _plain(grad_h0, (b, d), torch.float32, "grad_h0"),
+                                    *x_to, *gate_to, h0_to,
                                     ws, nbytes, _stream(stream)), "cc_gated_scan_backward")
     return grad_x, grad_gate, grad_h0
 
@@ -223,9 +235,7 @@ def _logits(logits: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Ten
 
 
 def _gradient(logits: torch.Tensor, grad_logits: Optional[torch.Tensor], stream):
-    if grad_logits is None:
-        grad_logits = _new(logits.shape, logits.dtype, logits.device, stream)
-    return grad_logits, _strided(grad_logits, logits.shape, logits.dtype, "grad_logits")
+    return _rows_out(grad_logits, logits.shape, logits.dtype, logits.device, stream, "grad_logits")
 
 
 def cc_token_logprob(logits: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Tensor] = None, placed: bool = False,
@@ -233,12 +243,9 @@ def cc_token_logprob(logits: torch.Tensor, tokens: torch.Tensor, mask: Optional[
                      stream=None):
     """(logprob float32 [B, T], rows float32 [B, T, 2]); rows is what cc_token_logprob_backward needs."""
     args, positions = _logits(logits, tokens, mask, placed, scale)
-    if logprob is None:
-        logprob = _new(positions, torch.float32, logits.device, stream)
-    if rows is None:
-        rows = _new((*positions, 2), torch.float32, logits.device, stream)
-    _check(lib().cc_token_logprob(*args, _plain(logprob, positions, torch.float32, "logprob"), _plain(rows, (*positions, 2), torch.float32, "rows"),
-                                  _stream(stream)), "cc_token_logprob")
+    logprob, logprob_to = _plain_out(logprob, positions, torch.float32, logits.device, stream, "logprob")
+    rows, rows_to = _plain_out(rows, (*positions, 2), torch.float32, logits.device, stream, "rows")
+    _check(lib().cc_token_logprob(*args, logprob_to, rows_to, _stream(stream)), "cc_token_logprob")
     return logprob, rows
 
 
