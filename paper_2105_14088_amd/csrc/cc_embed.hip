@@ -377,8 +377,8 @@ __device__ __forceinline__ void write_row(GT* row, const Part<VEC>& part, const 
 }
 
 // The sums, bound by the latency of rows in no order (65536 x 1024 bf16, 2048 segments: 50 us, 3.6 TB/s; the next 8 rows on their
-// way while 8 are summed took registers from other wavefronts: 52).  G lanes along a row (and blockIdx.y where a row is longer), a segment each.  keys and pos: sorted, with 8 more than n that
-// may be read.
+// way while 8 are summed took registers from other wavefronts: 52).  G lanes along a row (and blockIdx.y where a row is longer), a
+// segment each.  keys and pos: sorted, with 8 more than n that may be read.
 template <class S, class GT, int VEC, int G>
 __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restrict__ grad, const int32_t* __restrict__ keys,
                                                               const int32_t* __restrict__ pos, GT* __restrict__ out, SumArgs a) {

@@ -34,6 +34,12 @@ def test_runs_over_many_segments(d):
     gradient(40, d, 9000, "f32", "even")
 
 
+@pytest.mark.parametrize("n", [65536, 65537])
+@pytest.mark.parametrize("v", [700, 70000])
+def test_tiles_that_each_workgroup_adds_up_and_more(n, v):
+    gradient(v, 2, n, "f32", "steep")
+
+
 def test_one_run_over_all_segments():
     gradient(3, 2, 140001, "f32", "one")
 
