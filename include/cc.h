@@ -480,7 +480,8 @@ int cc_gated_scan_backward(const void* x, int64_t x_stride_b, int64_t x_stride_t
  *              always a candidate.
  *   logprob    fp32 [B, T]
  *   rows       fp32 [B, T, 2], 8-byte aligned, or NULL: what the backward call needs of each row
- * Where every candidate's logit is minus infinity the log-probability is minus infinity and the gradient zero.
+ * Where every candidate's logit is minus infinity the log-probability is minus infinity and the gradient zero.  Where one is NaN or
+ * plus infinity the log-probability and the candidates' gradient are NaN, and so is a loss that the position counts in.
  */
 int cc_token_logprob(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t,
                      const int32_t* tokens, const uint8_t* mask, int32_t placed, float scale, float* logprob, float* rows,

@@ -81,7 +81,8 @@ struct Row {
 __device__ __forceinline__ Row finish_row(float m, float rest, float token_logit, float scale) {
     Row r;
     r.m = m;
-    r.none = m == -kInf;
+    // The largest logit passes NaN over: nothing is a candidate only if the sum and the token's logit say so too.
+    r.none = m == -kInf && rest == 0.0f && token_logit == -kInf;
     if (r.none) {                     // nothing is probable and nothing has a gradient
         r.own = 0.0f;
         r.total = 1.0f;
@@ -143,8 +144,9 @@ __device__ __forceinline__ PolicyInputs policy_inputs(const Args& a, int64_t at,
 __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, const PolicyInputs& in) {
     PolicyTerms r;
     const float ratio = expf((float)(lp - (double)in.old_lp));
-    // a ratio that 32 bits do not hold still has no part where there is no advantage, nor a divergence that counts for nothing
-    const float free_gain = in.advantage == 0.0f ? 0.0f : ratio * in.advantage;
+    // a ratio that 32 bits do not hold still has no part where there is no advantage, nor a divergence that counts for nothing; that
+    // of an undefined log-probability makes the loss undefined
+    const float free_gain = in.advantage == 0.0f && ratio == ratio ? 0.0f : ratio * in.advantage;
     const float held = fminf(fmaxf(ratio, 1.0f - a.clip_low), 1.0f + a.clip_high) * in.advantage;
     const bool clipped = held < free_gain;
     r.clipped = clipped ? 1.0f : 0.0f;
@@ -451,9 +453,13 @@ __global__ __launch_bounds__(kThreads, KIND == kTokenPolicy ? 3 : 4) void short_
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) g[i] = e[it][c * VEC + i] * pull.x;
                 if (PLACED && !(fabsf(pull.x) < kInf)) {
-                    // what is no candidate has no gradient, whatever the row's others have
+                    // what is no candidate has no gradient, whatever the row's others have: a term of 0, or in an undefined row a place
+                    // that an earlier position has
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) g[i] = e[it][c * VEC + i] == 0.0f ? 0.0f : g[i];
+                    for (int i = 0; i < VEC; ++i) {
+                        const bool out_of_play = pull.x == pull.x ? e[it][c * VEC + i] == 0.0f : first_at[r.o * stride + j0 + i] <= r.t;
+                        g[i] = out_of_play ? 0.0f : g[i];
+                    }
                 }
                 if ((uint32_t)(r.k - j0) < (uint32_t)VEC) {
 #pragma unroll

@@ -350,3 +350,97 @@ def test_preference_gradient_against_differences():
     per_order = (valid * rel).sum(1)
     noise = (0.25 * float((per_order[:3] + per_order[3:]).mean()) + abs(up) * U) / eps
     assert abs((up - down) / (2 * eps) - slope) <= noise + 1e-2 * abs(slope)
+
+
+# ------------------------------------------------------------------------------------------------- undefined logits
+
+
+def undefined_rows(v, dtype):
+    """Orders of five rows: nothing but NaN; NaN beside minus infinity, the token one or the other; minus infinity alone; numbers."""
+    logits, tokens, _ = make(2, 5, v, dtype, v, masked=False)
+    nan, low = float("nan"), float("-inf")
+    logits[0, 0] = nan
+    logits[0, 1] = low
+    logits[0, 1, v // 2] = nan
+    tokens[0, 1] = v // 2
+    logits[0, 2] = nan
+    logits[0, 2, v // 3] = low
+    tokens[0, 2] = v // 3
+    logits[0, 3] = low
+    return logits, tokens
+
+
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [2, 6, 64, 300, 1024, 1025, 5000, 140001])
+def test_undefined_logits_are_not_taken_for_impossible_ones(v, name):
+    say(f"undefined logits v={v} {name}")
+    logits, tokens = undefined_rows(v, DTYPES[name])
+    z, k = dev(logits, tokens)
+    nan_rows = torch.tensor([[True, True, True, False, False], [False] * 5])
+    lp, rows = cc.cc_token_logprob(z, k, None, False, SCALE)
+    assert torch.equal(lp.isnan().cpu(), nan_rows) and float(lp[0, 3]) == float("-inf")
+    clean = z.clone()
+    clean[0, :3] = 1.0
+    same, _ = cc.cc_token_logprob(clean, k, None, False, SCALE)
+    assert torch.equal(lp[0, 3:], same[0, 3:]) and torch.equal(lp[1], same[1])
+    slope = torch.ones(2, 5, device="cuda")
+    grad = cc.cc_token_logprob_backward(z, k, None, False, SCALE, rows, slope)
+    assert grad[0, :3].isnan().all() and (grad[0, 3] == 0).all() and torch.isfinite(grad[1]).all()
+    place = z.clone()
+    cc.cc_token_logprob_backward(place, k, None, False, SCALE, rows, slope, grad_logits=place)
+    assert torch.equal(place.isnan(), grad.isnan()) and torch.equal(place.nan_to_num(), grad.nan_to_num())
+    # no loss of an undefined model is a number, with an advantage or without
+    old = torch.full((2, 5), -1.0, device="cuda")
+    for advantage in (1.0, -1.0, 0.0):
+        res = cc.cc_policy_loss(z, k, old, torch.full((2,), advantage, device="cuda"), scale=SCALE)
+        assert res.stats[0].isnan() and res.grad_logits[0, :3].isnan().all() and torch.isfinite(res.grad_logits[1]).all()
+    res = cc.cc_preference_loss(z, k, old, scale=SCALE)
+    assert res.loss.isnan() and res.margin.isnan().all() and res.grad_logits[0, :3].isnan().all()
+
+
+@pytest.mark.parametrize("v", [1, 8, 65, 1000])
+@pytest.mark.parametrize("orders", [1, 40])
+def test_an_undefined_last_candidate(v, orders):
+    """The last rank of an order has one candidate: undefined, its log-probability and its gradient are, and nothing else is."""
+    logits, tokens, _ = make(orders, v, v, torch.float32, v, placed=True, masked=False)
+    say(f"undefined last candidate v={v} orders={orders}")
+    last = tokens[0, -1].item()
+    logits[0, -1] = float("nan")
+    z, k = dev(logits, tokens)
+    lp, rows = cc.cc_token_logprob(z, k, None, True, SCALE)
+    hit = torch.zeros_like(lp, dtype=torch.bool)
+    hit[0, -1] = True
+    assert torch.equal(lp.isnan(), hit)
+    grad = cc.cc_token_logprob_backward(z, k, None, True, SCALE, rows, torch.ones_like(lp))
+    nan_at = torch.zeros_like(grad, dtype=torch.bool)
+    nan_at[0, -1, last] = True
+    assert torch.equal(grad.isnan(), nan_at) and (grad[0, -1][~nan_at[0, -1]] == 0).all()
+    if v > 1:
+        # two candidates, one of them impossible, the other undefined: both gradients are undefined
+        before = tokens[0, -2].item()
+        z[0, -2] = float("-inf")
+        z[0, -2, last] = float("nan")
+        lp, rows = cc.cc_token_logprob(z, k, None, True, SCALE)
+        grad = cc.cc_token_logprob_backward(z, k, None, True, SCALE, rows, torch.ones_like(lp))
+        nan_at[0, -2, last] = nan_at[0, -2, before] = True
+        assert lp[0, -2].isnan() and torch.equal(grad.isnan(), nan_at)
+
+
+@pytest.mark.parametrize("v,placed", [(6, True), (300, False), (300, True), (5000, False)])
+def test_an_infinite_logit_makes_its_row_undefined(v, placed):
+    say(f"infinite logit v={v} placed={placed}")
+    logits, tokens, _ = make(3, 5, v, torch.float32, v, placed=placed, masked=False)
+    if not placed:
+        tokens[:] = torch.arange(5, dtype=torch.int32)
+    logits[0, 1, tokens[0, 1]] = float("inf")                   # the token's own
+    logits[1, 2, tokens[1, 4]] = float("inf")                   # another candidate's
+    z, k = dev(logits, tokens)
+    lp, rows = cc.cc_token_logprob(z, k, None, placed, SCALE)
+    hit = torch.zeros(3, 5, dtype=torch.bool, device="cuda")
+    hit[0, 1] = hit[1, 2] = True
+    assert torch.equal(lp.isnan(), hit) and torch.isfinite(lp[~hit]).all()
+    grad = cc.cc_token_logprob_backward(z, k, None, placed, SCALE, rows, torch.ones_like(lp))
+    nan_at = hit.unsqueeze(2).expand_as(grad).clone()
+    if placed:
+        nan_at[0, 1, tokens[0, 0]] = nan_at[1, 2, tokens[1, 0]] = nan_at[1, 2, tokens[1, 1]] = False
+    assert torch.equal(grad.isnan(), nan_at)
