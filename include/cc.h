@@ -539,7 +539,9 @@ int cc_policy_loss(const void* logits, int32_t dtype, int64_t B, int64_t T, int6
  *   ref_logprob  fp32 [B, T] or NULL (zero);  0 <= label_smoothing <= 1
  *   loss         fp32 [1];  margin fp32 [B/2];  logprob fp32 [B, T]
  *   grad_logits, grad_scale, workspace as for cc_policy_loss.
- * The sums are held in 64 bits.  With no pairs the loss is zero.
+ * The sums are held in 64 bits.  With no pairs the loss is zero.  An impossible token (log-probability minus infinity) makes its
+ * pair's margin infinite, and the loss where it is the preferred sequence's; a term whose coefficient is zero has no part in the
+ * loss then either.  Where both sequences of a pair hold one, margin and loss are undefined (NaN).
  */
 int cc_preference_loss(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t,
                        const int32_t* tokens, const uint8_t* mask, int32_t placed, float scale, const float* ref_logprob,

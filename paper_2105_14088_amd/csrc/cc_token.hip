@@ -742,7 +742,8 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(const double* _
 // A pair: its margin, its share of the loss, and the slope of its two sequences' log-probabilities.
 __device__ __forceinline__ double finish_pair(double gap, int64_t p, int64_t pairs, float beta, float smoothing, float* __restrict__ margin,
                                               float* __restrict__ slope) {
-    const double m = (double)beta * gap;
+    // A sequence that holds an impossible token makes the margin infinite: what is multiplied by zero then still has no part.
+    const double m = beta == 0.0f && gap == gap ? 0.0 : (double)beta * gap;
     // softplus(x) = max(x, 0) + log1p(exp(-|x|))
     const double small = exp(-fabs(m)), tail = log1p(small), part = small / (1.0 + small);
     const double away = m >= 0.0 ? part : 1.0 - part, by = m >= 0.0 ? 1.0 - part : part;       // sigmoid(-m), sigmoid(m)
@@ -750,7 +751,9 @@ __device__ __forceinline__ double finish_pair(double gap, int64_t p, int64_t pai
     margin[p] = (float)m;
     slope[p] = s;
     slope[p + pairs] = -s;
-    return ((1.0 - (double)smoothing) * (fmax(-m, 0.0) + tail) + (double)smoothing * (fmax(m, 0.0) + tail)) / (double)pairs;
+    const double against = smoothing == 1.0f ? 0.0 * tail : (1.0 - (double)smoothing) * (fmax(-m, 0.0) + tail);
+    const double towards = smoothing == 0.0f ? 0.0 * tail : (double)smoothing * (fmax(m, 0.0) + tail);
+    return (against + towards) / (double)pairs;
 }
 
 // TEAM threads share a pair's positions: one where they are few (a pair's 64-bit functions are then taken for 64 pairs at once), a

@@ -444,3 +444,45 @@ def test_an_infinite_logit_makes_its_row_undefined(v, placed):
     if placed:
         nan_at[0, 1, tokens[0, 0]] = nan_at[1, 2, tokens[1, 0]] = nan_at[1, 2, tokens[1, 1]] = False
     assert torch.equal(grad.isnan(), nan_at)
+
+
+# ---------------------------------------------------------------------------------------- margins that are not finite
+
+
+@pytest.mark.parametrize("pairs,t", [(2, 5), (5, 70), (1100, 3)])
+@pytest.mark.parametrize("smoothing,impossible", [(0.0, "dearer"), (1.0, "cheaper")])
+def test_an_infinite_margin_on_the_right_side_costs_nothing(pairs, t, smoothing, impossible):
+    """A term of the loss whose coefficient is zero has no part in it, whatever the margin."""
+    say(f"preference pairs={pairs} t={t} smoothing={smoothing} impossible={impossible}")
+    v = 9
+    logits, tokens, _ = make(2 * pairs, t, v, torch.float32, pairs, masked=False)
+    order = 1 if impossible == "cheaper" else pairs + 1
+    logits[order, 2, tokens[order, 2]] = float("-inf")
+    z, k = dev(logits, tokens)
+    res = cc.cc_preference_loss(z, k, scale=SCALE, beta=0.5, label_smoothing=smoothing)
+    assert float(res.margin[1]) == float("-inf" if impossible == "cheaper" else "inf")
+    others = [i for i in range(2 * pairs) if i % pairs != 1]
+    rest = cc.cc_preference_loss(z[others].contiguous(), k[others].contiguous(), scale=SCALE, beta=0.5, label_smoothing=smoothing)
+    want = float(rest.loss) * (pairs - 1) / pairs
+    assert abs(float(res.loss) - want) <= 4 * U * want                      # two results' roundings, the product's and the quotient's
+    assert (res.grad_logits[[1, pairs + 1]] == 0).all() and torch.isfinite(res.grad_logits).all()
+
+
+def test_an_infinite_margin_on_the_wrong_side():
+    logits, tokens, _ = make(4, 5, 9, torch.float32, 3, masked=False)
+    logits[1, 2, tokens[1, 2]] = float("-inf")
+    z, k = dev(logits, tokens)
+    for smoothing in (0.0, 0.25):
+        res = cc.cc_preference_loss(z, k, scale=SCALE, beta=0.5, label_smoothing=smoothing)
+        assert float(res.margin[1]) == float("-inf") and float(res.loss) == float("inf") and torch.isfinite(res.grad_logits).all()
+    # a margin that counts for nothing
+    res = cc.cc_preference_loss(z, k, scale=SCALE, beta=0.0)
+    assert (res.margin == 0).all() and abs(float(res.loss) - 0.6931471805599453) <= U and (res.grad_logits == 0).all()
+
+
+def test_two_impossible_sequences_have_no_margin():
+    logits, tokens, _ = make(4, 5, 9, torch.float32, 3, masked=False)
+    logits[1, 2, tokens[1, 2]] = logits[3, 4, tokens[3, 4]] = float("-inf")
+    res = cc.cc_preference_loss(*dev(logits, tokens), scale=SCALE, beta=0.5)
+    assert res.margin[1].isnan() and torch.isfinite(res.margin[0]) and res.loss.isnan()
+    assert torch.isfinite(res.grad_logits[[0, 2]]).all()
