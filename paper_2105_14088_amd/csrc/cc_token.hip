@@ -154,8 +154,11 @@ __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, co
     r.slope = clipped ? 0.0f : -free_gain;
     r.kl = 0.0f;
     if (a.ref) {
-        const float away = (float)((double)in.ref - lp), grown = expm1f(away);
-        r.kl = grown - away;
+        // x = ref - lp is small where the policy is near the one to stay near to, and exp(x) - 1 - x then the square of it, halved: in 64
+        // bits, since the difference loses what 32 bits hold of it.  That of an impossible token is infinite.
+        const double away = (double)in.ref - lp, full = expm1(away);
+        const float grown = (float)full;
+        r.kl = away == (double)kInf ? kInf : (float)(full - away);
         if (a.kl_coef != 0.0f) {
             r.loss += a.kl_coef * r.kl;
             r.slope -= a.kl_coef * grown;

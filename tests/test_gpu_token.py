@@ -486,3 +486,49 @@ def test_two_impossible_sequences_have_no_margin():
     res = cc.cc_preference_loss(*dev(logits, tokens), scale=SCALE, beta=0.5)
     assert res.margin[1].isnan() and torch.isfinite(res.margin[0]) and res.loss.isnan()
     assert torch.isfinite(res.grad_logits[[0, 2]]).all()
+
+
+# ---------------------------------------------------------------------------------------------------- small divergences
+
+
+@pytest.mark.parametrize("v,placed", [(8, False), (8, True), (700, False), (3000, False)])
+@pytest.mark.parametrize("apart", [1e-7, 1e-6, 1e-4, 1e-3, 3e-2, 1.0, 20.0, -1e-6, -1e-3, -0.5, -30.0])
+def test_the_divergence_of_policies_near_each_other(v, placed, apart):
+    """Where all candidates' logits are equal the log-probability is -log of their number, to within 1e-12 (the series of the logarithm
+    5e-13, 64-bit operations), and the divergence exp(x) - 1 - x of x = ref - lp moves by |exp(x) - 1| times that."""
+    say(f"policy v={v} placed={placed} apart={apart}")
+    b, t = 3, 4
+    logits = torch.full((b, t, v), 0.5)
+    tokens = torch.arange(t, dtype=torch.int32).expand(b, t).contiguous()
+    lp = -torch.log(torch.tensor([float(v - (i if placed else 0)) for i in range(t)], dtype=torch.float64)).expand(b, t)
+    other = (lp + apart).float()
+    away = other.double() - lp
+    grown = torch.expm1(away)
+    kl = torch.where(away.abs() < 0.1, away ** 2 * (1 / 2 + away / 6 + away ** 2 / 24 + away ** 3 / 120 + away ** 4 / 720 + away ** 5 / 5040 + away ** 6 / 40320),
+                     grown - away)
+    coef = 1000.0
+    args = dev(logits, tokens, lp.float(), torch.zeros(b), other)
+    res = cc.cc_policy_loss(*args, placed=placed, scale=SCALE, kl_coef=coef)
+    # the mean's weights and terms are rounded to 32 bits (a weight, a divergence, the coefficient's product, the result: 4 u)
+    bound = 4 * U * float(kl.mean()) + float(grown.abs().mean()) * 1e-12
+    assert abs(float(res.stats[1]) - float(kl.mean())) <= bound
+    assert abs(float(res.stats[0]) - coef * float(kl.mean())) <= coef * (bound + 2 * U * float(kl.mean()))
+    # the slope is -coef (exp(x) - 1) / 12, the token's gradient SCALE (1 - p) times that
+    want = -coef * grown / (b * t) * SCALE * (1 - torch.exp(lp))
+    got = res.grad_logits.gather(2, args[1].long().unsqueeze(2)).squeeze(2).cpu().double()
+    err = coef * SCALE / (b * t) * torch.exp(away) * 1e-12 + want.abs() * 16 * U
+    if placed:
+        keep = lp < 0
+        got, want, err = got[keep], want[keep], err[keep]
+    assert ((got - want).abs() <= err).all()
+
+
+@pytest.mark.parametrize("v", [30, 2000])
+def test_the_divergence_of_an_impossible_token_is_infinite(v):
+    logits, tokens, _ = make(2, 4, v, torch.float32, 8, masked=False)
+    logits[0, 2, tokens[0, 2]] = float("-inf")
+    z, k, old = dev(logits, tokens, torch.full((2, 4), -3.0))
+    for coef in (0.0, 0.1):
+        res = cc.cc_policy_loss(z, k, old, torch.ones(2, device="cuda"), old, scale=SCALE, kl_coef=coef)
+        assert float(res.stats[1]) == float("inf")
+        assert float(res.stats[0]) == float("inf") if coef else torch.isfinite(res.stats[0])
