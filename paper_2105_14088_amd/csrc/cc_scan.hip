@@ -477,14 +477,15 @@ hipError_t backward(const ScanCall& c, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Whether a lane's offsets fit 32 bits: sequences and channels of a tensor, and a chunk's rows.
+// Whether a lane's offsets fit 32 bits: sequences and channels of a tensor, and a chunk's rows.  The first and the last state are bounded by
+// themselves: without positions there are no kept states.
 bool near(const Strided& t, const ScanCall& c, int64_t bytes) {
     return (double)bytes * ((double)(c.B > 0 ? c.B - 1 : 0) * (double)t.b + (double)c.D + (double)L * (double)t.t) < 4294967296.0;
 }
 bool all_near(const ScanCall& c, bool backward) {
     const int64_t e = c.dtype == kF32 ? 4 : 2, chunks = (c.T + L - 1) / L;
-    const Strided states = {nullptr, chunks * c.D, c.D};
-    return near(c.x, c, e) && near(c.gate, c, e) && near(c.h, c, e) && near(states, c, 4) &&
+    const Strided states = {nullptr, chunks * c.D, c.D}, ends = {nullptr, c.D, 0};
+    return near(c.x, c, e) && near(c.gate, c, e) && near(c.h, c, e) && near(states, c, 4) && near(ends, c, 4) &&
            (!backward || (near(c.grad_x, c, e) && near(c.grad_gate, c, e)));
 }
 

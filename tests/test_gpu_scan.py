@@ -189,3 +189,16 @@ def test_gradient_against_differences():
     _, _, err, err_last = ref.scan(x, gate, h0, None)
     noise = float((err * gh.abs()).sum() + (err_last * gl.abs()).sum()) * 2 / eps
     assert abs(estimate - slope) <= noise + 2e-4 * abs(far - near) + 1e-3 * abs(slope)
+
+
+def test_states_beyond_32_bits_without_positions():
+    """2^30 channels and no position: the states lie beyond 4 GB where the tensors of 16 bits do not."""
+    b, d = (1 << 30) // 1000 + 7, 1000
+    say("scan: 4.3 GB of states, no positions")
+    h0 = torch.arange(b * d, dtype=torch.int32, device="cuda").view(torch.float32).view(b, d)
+    empty = torch.empty(b, 0, d, dtype=torch.bfloat16, device="cuda")
+    _, last, states = cc.cc_gated_scan(empty, empty, h0, save_states=True)
+    assert torch.equal(last.view(torch.int32), h0.view(torch.int32))
+    last.zero_()
+    _, _, g0 = cc.cc_gated_scan_backward(empty, empty, states, empty, h0, grad_h0=last)
+    assert torch.equal(g0.view(torch.int32), h0.view(torch.int32))
