@@ -55,25 +55,6 @@ __device__ __forceinline__ Pack<S, N> load_pack(const S* p) {
 }
 template <int N, class S>
 __device__ __forceinline__ void store_pack(S* p, const Pack<S, N>& r) { __builtin_memcpy(p, &r, sizeof(r)); }
-// The first `have` of N elements; the others read as zero, and are not written.
-template <int N, class S>
-__device__ __forceinline__ Pack<S, N> load_some(const S* p, int have) {
-    if (have >= N) return load_pack<N>(p);
-    float f[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = i < have ? widen(p[i]) : 0.0f;
-    return Pack<S, N>::from(f);
-}
-template <int N, class S>
-__device__ __forceinline__ void store_some(S* p, const Pack<S, N>& r, int have) {
-    if (have >= N) {
-        store_pack(p, r);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < have) p[i] = r.element(i);
-}
 
 // The largest of N elements (a NaN among them is passed over).
 template <class S, int N>
