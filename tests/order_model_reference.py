@@ -196,3 +196,27 @@ def preference(lp, valid, ref, beta, smoothing):
     loss = ((1 - smoothing) * soft(-m) + smoothing * soft(m)).sum() / max(1, pairs)
     s = beta / max(1, pairs) * (smoothing * torch.sigmoid(m) - (1 - smoothing) * torch.sigmoid(-m))
     return loss, m, torch.cat([s, -s]).unsqueeze(1).expand_as(lp)
+
+
+def rows_at_once(logits, tokens, mask, placed, scale):
+    """What `rows` gives, for all positions together: for many of them."""
+    z = logits.double() * scale
+    b, t, v = z.shape
+    valid = counted(tokens, mask, v)
+    at = torch.arange(t)
+    k = tokens.long().clamp(0, v - 1).unsqueeze(2)
+    if placed:
+        there = (tokens >= 0) & (tokens < v)
+        first = torch.full((b, v), t).scatter_reduce_(1, k.squeeze(2), torch.where(there, at, t), "amin")
+        z = z.masked_fill((first.unsqueeze(1) < at[:, None]).scatter(2, k, False), -math.inf)
+    m = z.amax(2, keepdim=True)
+    none = m == -math.inf
+    e = torch.exp(z - torch.where(none, 0.0, m))
+    own, others = e.gather(2, k), e.scatter(2, k, 0.0).sum(2, keepdim=True)
+    total = torch.where(none, 1.0, others + own)
+    lp = torch.where(others < own, -torch.log1p(others / own), (z.gather(2, k) - m) - torch.log(total))
+    lp = torch.where(none, -math.inf, lp)
+    ok = valid.unsqueeze(2)
+    terms = min(v, max(4, v // 8 if v <= 64 else v // 64 + 64))
+    return (torch.where(ok, e / total, 0.0), torch.where(ok, others / total, 0.0).squeeze(2), torch.where(ok, lp, 0.0).squeeze(2), valid,
+            (1.5 * 40 + terms + 20) * U)

@@ -532,3 +532,87 @@ def test_the_divergence_of_an_impossible_token_is_infinite(v):
         res = cc.cc_policy_loss(z, k, old, torch.ones(2, device="cuda"), old, scale=SCALE, kl_coef=coef)
         assert float(res.stats[1]) == float("inf")
         assert float(res.stats[0]) == float("inf") if coef else torch.isfinite(res.stats[0])
+
+
+# ------------------------------------------------------------------------------- many orders, many pairs, longer rows
+
+# Orders enough that a workgroup's wavefronts take several batches of rows each, and a last one that is not full: batches of 32 rows
+# (up to 8 vectors of logits), 16, 8, 4 (up to 64), 2 and 1, two or four of them.
+BATCHES = [(1024, 130, 3, False, "f32"), (1024, 130, 20, True, "f32"), (1030, 200, 40, False, "bf16"), (600, 270, 50, False, "f32"),
+           (520, 150, 100, True, "f16"), (300, 130, 130, True, "f32"), (256, 150, 200, False, "f32"), (300, 100, 300, True, "bf16"),
+           (520, 150, 120, True, "f32"), (64, 520, 300, False, "f32"), (64, 520, 520, True, "f16"), (32, 520, 600, False, "f32"), (20, 900, 1000, True, "f32")]
+
+
+@pytest.fixture
+def at_once(monkeypatch):
+    """The definition for all positions together."""
+    monkeypatch.setattr(ref, "rows", ref.rows_at_once)
+
+
+def inputs(case):
+    """The case's logits, tokens and mask; orders that are longer than their vocabulary place every node again and again."""
+    b, t, v, placed, name = case
+    logits, tokens, mask = make(b, t, v, DTYPES[name], t + v, placed and v >= t)
+    if placed and v < t:
+        again = [torch.rand(b, v, generator=torch.Generator().manual_seed(i)).argsort(1) for i in range(-(-t // v))]
+        tokens = torch.cat(again, 1)[:, :t].to(torch.int32).contiguous()
+    return logits, tokens, mask
+
+
+@pytest.mark.parametrize("case", BATCHES, ids=str)
+def test_logprob_of_many_batches(case, at_once):
+    say(f"logprob {case}")
+    check_logprob(*inputs(case), case[3])
+
+
+@pytest.mark.parametrize("case", BATCHES, ids=str)
+def test_policy_of_many_batches(case, at_once):
+    say(f"policy {case}")
+    check_policy(*inputs(case), case[3], "tokens" if case[1] % 4 else "orders", per_token=case[0] == 300)
+
+
+@pytest.mark.parametrize("case", BATCHES, ids=str)
+def test_preference_of_many_batches(case, at_once):
+    say(f"preference {case}")
+    check_preference(*inputs(case), case[3])
+
+
+@pytest.mark.parametrize("mean", ["tokens", "orders"])
+@pytest.mark.parametrize("b,t,v", [(1024, 1, 4), (1025, 3, 9), (3100, 5, 7), (1500, 70, 6), (2, 700, 5)])
+def test_policy_of_more_orders_than_are_counted_at_once(b, t, v, mean, at_once):
+    say(f"policy b={b} t={t} v={v} {mean}")
+    check_policy(*make(b, t, v, torch.float32, b, masked=b > 2), False, mean)
+
+
+@pytest.mark.parametrize("pairs,t", [(4, 65), (5, 65), (5, 1000), (64, 300), (4, 2048), (3, 2049), (1024, 64), (1025, 64), (1025, 3), (1300, 65), (66000, 1)])
+def test_preference_of_many_pairs(pairs, t, at_once):
+    say(f"preference pairs={pairs} t={t}")
+    check_preference(*make(2 * pairs, t, 5, torch.float32, pairs + t), False)
+    if pairs < 100:
+        check_preference(*make(2 * pairs, t, 6, torch.bfloat16, pairs + t), False, smoothing=0.0, with_ref=False)
+
+
+@pytest.mark.parametrize("b,t,v,name", [(2, 3, 5000, "bf16"), (2, 3, 9001, "f16"), (2, 3, 9001, "f32"), (2, 2, 20003, "bf16"), (1, 3, 32769, "f32"),
+                                        (1, 3, 65536, "f32"), (2, 2, 65537, "f32"), (1, 3, 100003, "f32"), (2, 2, 65537, "f16"),
+                                        (2, 2, 70001, "bf16"), (1, 3, 131072, "bf16"), (2, 2, 131073, "bf16"), (1, 3, 140007, "f16"),
+                                        (1, 2, 300009, "bf16")])
+def test_policy_of_longer_rows(b, t, v, name, at_once):
+    """On both sides of what each kernel keeps of a row, and rows that none keeps: read again for the gradient, in place too."""
+    say(f"policy b={b} t={t} v={v} {name}")
+    check_policy(*make(b, t, v, DTYPES[name], v, masked=b > 1), False, "tokens")
+
+
+def test_many_long_rows(at_once):
+    """2048 rows and more that are longer than a workgroup's stride are taken by smaller workgroups: the same rows for all orders."""
+    b, t, v = 64, 33, 16401
+    say(f"logprob b={b} t={t} v={v}")
+    logits, tokens, _ = make(1, t, v, torch.float32, 6, masked=False)
+    p, rest, lp, valid, rel = ref.rows(logits, tokens, None, False, SCALE)
+    z, k = logits.cuda().expand(b, t, v), tokens.cuda().expand(b, t).contiguous()
+    got, rows = cc.cc_token_logprob(z, k, None, False, SCALE)
+    within(got, lp.expand(b, t), finish(lp, lp.abs() * U + rel, torch.float32).expand(b, t), "logprob")
+    slope = torch.randn(t, generator=torch.Generator().manual_seed(1))
+    grad = cc.cc_token_logprob_backward(z, k, None, False, SCALE, rows, slope.cuda().expand(b, t).contiguous())
+    want = ref.grad_logits(p, rest, tokens, valid, slope.double() * SCALE)
+    assert torch.equal(grad, grad[:1].expand(b, t, v))
+    within(grad[:1], want, finish(want, want.abs() * (2 * rel + 8 * U), torch.float32), "gradient")

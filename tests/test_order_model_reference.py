@@ -106,3 +106,19 @@ def test_bounds_catch_a_planted_mistake():
         wrong[:, i] = s
     with pytest.raises(AssertionError):
         ref.within(wrong, h, ref.finish(h, err, torch.float32), "h")
+
+
+@pytest.mark.parametrize("placed", [False, True])
+def test_rows_at_once_are_rows(placed):
+    g = torch.Generator().manual_seed(2)
+    logits = 3 * torch.randn(4, 12, 15, generator=g)
+    tokens = torch.randint(-1, 16, (4, 12), generator=g, dtype=torch.int32)
+    mask = torch.rand(4, 12, generator=g) < 0.8
+    logits[0, 1] = float("-inf")
+    logits[1, 2, 3:] = float("-inf")
+    logits[2, 5, 1] = 60.0
+    tokens[2, 5], mask[0, 1], mask[1, 2], mask[2, 5] = 1, True, True, True
+    one, other = ref.rows(logits, tokens, mask, placed, 0.75), ref.rows_at_once(logits, tokens, mask, placed, 0.75)
+    for x, y in zip(one[:3], other[:3]):
+        assert torch.allclose(x, y, rtol=1e-13, atol=1e-300)
+    assert torch.equal(one[3], other[3]) and one[4] == other[4]
