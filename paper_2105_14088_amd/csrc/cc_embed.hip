@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(const int32_t* __res
 // is cut into as many tiles as there are compute units soon enough.
 constexpr int kTile = 1024, kSortWaves = 4, kSortThreads = kSortWaves * 64, kPerThread = kTile / kSortThreads;
 constexpr int kMaxBits = 11;
-constexpr int64_t kColumnsMost = 64;              // see sort_place_kernel
+constexpr int64_t kColumnsMost = 64, kColumnWordsMost = 16384;    // tiles, tiles times digits: see sort_place_kernel
 
 // hist[tile][digit]: how many tokens of the tile have the digit
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t* __restrict__ ids, int64_t n, uint32_t V, int shift,
@@ -217,9 +217,13 @@ __global__ __launch_bounds__(64 * kParts) void sort_columns_kernel(uint32_t* __r
 }
 
 // Places each token behind the tokens of smaller digits, of its digit in earlier tiles, earlier wavefronts of its tile and
-// earlier lanes.  keys_in == ids of the call where pos_in is null (a token's position is then its index).  COLUMNS: of up to
-// kColumnsMost tiles every workgroup adds the counts of all itself, without sort_columns_kernel (64 tiles of 512 digits: 11.6 us against
-// 15.0 for the two; 125 tiles of 1024 digits: 35 against 14.7).
+// earlier lanes.  keys_in == ids of the call where pos_in is null (a token's position is then its index).  COLUMNS: every workgroup adds
+// the counts of all tiles itself, without sort_columns_kernel, where these are few.  What that takes grows with tiles times
+// digits.  The whole gradient in us, with COLUMNS and without, by digits (twice as many passes for 256 of 50001 rows):
+//   256:  16 tiles 34.1, 38.6    64 tiles 45.6, 48.9    111 tiles 59.5, 62.6    128 tiles 61.3, 60.0
+//   512:  16 tiles 19.1, 20.6    31 tiles 20.1, 20.8     47 tiles 23.5, 23.2     64 tiles 24.7, 23.9
+//   1024: 13 tiles 23.7, 24.1    16 tiles 23.7, 23.6     20 tiles 25.6, 23.7     64 tiles 31.2, 26.1
+//   2048:  9 tiles 30.5, 28.1    64 tiles 43.4, 29.3
 template <bool COLUMNS>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t* __restrict__ keys_in, const int32_t* __restrict__ pos_in,
                                                                   int64_t n, uint32_t V, int shift, int bits,
@@ -250,11 +254,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t*
         const int tiles = (int)clear.own;
         for (int d = threadIdx.x; d < digits; d += kSortThreads) {
             uint32_t sum = 0, before = 0;
-#pragma unroll 16
-            for (int t = 0; t < tiles; ++t) {
-                const uint32_t c = hist[((int64_t)t << bits) + d];
-                before += t < (int)blockIdx.x ? c : 0u;
-                sum += c;
+            // 16 at a time, the last of them too: one after the other, they would be waited for one by one
+            for (int t0 = 0; t0 < tiles; t0 += 16) {
+                uint32_t c[16];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) c[u] = hist[((int64_t)min(t0 + u, tiles - 1) << bits) + d];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+                    before += t0 + u < (int)blockIdx.x ? c[u] : 0u;
+                    sum += t0 + u < tiles ? c[u] : 0u;
+                }
             }
             column[d] = sum;
             column[digits + d] = before;
@@ -594,9 +603,9 @@ hipError_t backward(const EmbedCall& c, hipStream_t s) {
         if (blocks > 0)
             hipLaunchKernelGGL(rank_kernel, dim3(blocks), dim3(kRankThreads), 0, s, c.ids, (int)c.n, (uint32_t)c.V, keys[0], pos[0], clear);
     } else {
-        const bool columns = l.tiles <= kColumnsMost;
+        const bool columns = l.tiles <= kColumnsMost && l.tiles << l.bits <= kColumnWordsMost;
         const int digits = 1 << l.bits, each = columns ? 2 : 3, launches = each * l.passes;
-        const size_t lds = sizeof(uint32_t) * (size_t)(kSortWaves + (columns ? 2 : 0)) * digits;   // 32 or 48 KB for 2048 of them
+        const size_t lds = sizeof(uint32_t) * (size_t)(kSortWaves + (columns ? 2 : 0)) * digits;   // 32 KB for 2048 of them; with columns 24 KB for 1024
         const auto place = columns ? sort_place_kernel<true> : sort_place_kernel<false>;
         for (int p = 0; p < l.passes; ++p) {
             const int32_t* in = p == 0 ? c.ids : keys[(p + 1) & 1];

@@ -57,3 +57,10 @@ def test_absent_rows_are_cleared_and_nothing_beside_them(v, d, apart, n, name, w
     within(table, want, finish(want, err, table.dtype), "gradient")
     table.fill_(7.0)
     assert (whole == 7).all()
+
+
+@pytest.mark.parametrize("v,n", [(100, 65536), (200, 65536), (200, 65537), (300, 32768), (300, 32769), (1000, 16384), (1000, 16385), (1500, 8193),
+                                 (50001, 65536), (50001, 65537), (100000, 32768), (100000, 32769), (600000, 16384), (600000, 16385)])
+def test_counts_that_each_workgroup_adds_up_and_more(v, n):
+    """Both sides of the line in tiles times digits, for 128 to 2048 digits and one or two passes."""
+    gradient(v, 2, n, "f32", "steep")
