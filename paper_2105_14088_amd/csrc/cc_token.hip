@@ -966,12 +966,14 @@ hipError_t run(TokenKind kind, const TokenCall& c, hipStream_t s) {
     if (any) launch_rows<S, kTokenForward>(a, c.placed, s);
     double* const losses = (double*)(w + l.losses);
     float* const slopes = (float*)(w + l.counts);
-    if (c.T <= 64 && pairs <= 1024) {
-        // a thread per pair, one workgroup
+    // One workgroup, and no second launch, where it is done in one turn: a thread per pair of few positions, or a quarter of it per
+    // pair of more.  Pairs x positions, one workgroup against two launches: kernels in us, 64 x 64 10.2, 11.3; 256 x 64 15.6, 16.8;
+    // 1024 x 8 9.5, 9.2; 512 x 32 15.8, 13.0; 1024 x 16 15.9, 10.9; 1024 x 64 43.9, 19.3; 1 x 777 8.3, 9.4; 4 x 65 8.8, 8.7; 4 x 2048
+    // 11.0, 9.5; 8 x 65 11.3, 9.0.  A call made from Python is 2.3 us shorter with one launch less: the lines are where that is lost.
+    if (c.T <= 64 && pairs <= 1024 && pairs * c.T <= 16384) {
         hipLaunchKernelGGL((pair_kernel<1024, 1>), dim3(1), dim3(1024), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin, slopes, losses,
                            c.stats);
     } else if (pairs <= 4 && c.T <= 2048) {
-        // 4 x 777 positions: 6.5 us in one workgroup, 9.2 in two launches; 32 x 1000: 18 against 9.3
         hipLaunchKernelGGL((pair_kernel<1024, 256>), dim3(1), dim3(1024), 0, s, a.gaps, pairs, c.T, c.beta, c.smoothing, c.margin, slopes, losses,
                            c.stats);
     } else {

@@ -616,3 +616,9 @@ def test_many_long_rows(at_once):
     want = ref.grad_logits(p, rest, tokens, valid, slope.double() * SCALE)
     assert torch.equal(grad, grad[:1].expand(b, t, v))
     within(grad[:1], want, finish(want, want.abs() * (2 * rel + 8 * U), torch.float32), "gradient")
+
+
+@pytest.mark.parametrize("pairs,t", [(256, 64), (257, 63), (257, 64), (512, 32), (512, 33), (1024, 16), (1024, 17), (1025, 7)])
+def test_preference_of_pairs_on_both_sides_of_one_workgroup(pairs, t, at_once):
+    say(f"preference pairs={pairs} t={t}")
+    check_preference(*make(2 * pairs, t, 5, torch.float32, pairs + t), False)
