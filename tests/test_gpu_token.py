@@ -622,3 +622,19 @@ def test_many_long_rows(at_once):
 def test_preference_of_pairs_on_both_sides_of_one_workgroup(pairs, t, at_once):
     say(f"preference pairs={pairs} t={t}")
     check_preference(*make(2 * pairs, t, 5, torch.float32, pairs + t), False)
+
+
+@pytest.mark.parametrize("b,t,v", [(16, 32, 4096), (16, 32, 4097), (7, 73, 4096), (7, 73, 4097), (16, 32, 32767), (16, 32, 32768), (7, 73, 32767)])
+def test_rows_on_both_sides_of_larger_workgroups(b, t, v, at_once):
+    """512 rows and fewer, about one turn of the larger workgroups and eight: the same logits for all orders."""
+    say(f"logprob b={b} t={t} v={v}")
+    logits, tokens, _ = make(1, t, v, torch.float32, 6, masked=False)
+    p, rest, lp, valid, rel = ref.rows(logits, tokens, None, False, SCALE)
+    z, k = logits.cuda().expand(b, t, v), tokens.cuda().expand(b, t).contiguous()
+    got, rows = cc.cc_token_logprob(z, k, None, False, SCALE)
+    within(got, lp.expand(b, t), finish(lp, lp.abs() * U + rel, torch.float32).expand(b, t), "logprob")
+    slope = torch.randn(t, generator=torch.Generator().manual_seed(1))
+    grad = cc.cc_token_logprob_backward(z, k, None, False, SCALE, rows, slope.cuda().expand(b, t).contiguous())
+    want = ref.grad_logits(p, rest, tokens, valid, slope.double() * SCALE)
+    assert torch.equal(grad, grad[:1].expand(b, t, v))
+    within(grad[:1], want, finish(want, want.abs() * (2 * rel + 8 * U), torch.float32), "gradient")
