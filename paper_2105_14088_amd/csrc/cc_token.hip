@@ -146,7 +146,7 @@ __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, co
     const float ratio = expf((float)(lp - (double)in.old_lp));
     // a ratio that 32 bits do not hold still has no part where there is no advantage, nor a divergence that counts for nothing; that
     // of an undefined log-probability makes the loss undefined
-    const float free_gain = in.advantage == 0.0f && ratio == ratio ? 0.0f : ratio * in.advantage;
+    const float free_gain = in.advantage == 0.0f && lp == lp ? 0.0f : ratio * in.advantage;
     const float held = fminf(fmaxf(ratio, 1.0f - a.clip_low), 1.0f + a.clip_high) * in.advantage;
     const bool clipped = held < free_gain;
     r.clipped = clipped ? 1.0f : 0.0f;

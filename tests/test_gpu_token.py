@@ -638,3 +638,14 @@ def test_rows_on_both_sides_of_larger_workgroups(b, t, v, at_once):
     want = ref.grad_logits(p, rest, tokens, valid, slope.double() * SCALE)
     assert torch.equal(grad, grad[:1].expand(b, t, v))
     within(grad[:1], want, finish(want, want.abs() * (2 * rel + 8 * U), torch.float32), "gradient")
+
+
+@pytest.mark.parametrize("v", [12, 2500])
+def test_no_advantage_and_no_ratio(v):
+    """A token that was impossible when it was drawn, and still is, has no ratio: without an advantage it has no part either."""
+    logits, tokens, _ = make(2, 4, v, torch.float32, v, masked=False)
+    logits[0, 1, tokens[0, 1]] = float("-inf")
+    z, k = dev(logits, tokens)
+    old, _ = cc.cc_token_logprob(z, k, scale=SCALE)
+    res = cc.cc_policy_loss(z, k, old, torch.zeros(2, device="cuda"), scale=SCALE)
+    assert float(old[0, 1]) == float("-inf") and (res.stats == 0).all() and (res.grad_logits == 0).all()
