@@ -124,6 +124,26 @@ __device__ __forceinline__ Row finish_row(float m, float rest, float token_logit
 // towards zero and the rest is positive: for x = -infinity both products are.
 __device__ __forceinline__ float term(const Args& a, float x) { return __builtin_amdgcn_exp2f(fmaf(x, a.scale2, x * a.scale2_rest)); }
 
+// exp(x) - 1 in 64 bits, so that x can be taken from it: x = n ln 2 + r with |r| <= ln 2 / 2 and a little, exp(r) - 1 = r + r^2 (1/2! + r (1/3! + r/4!
+// + ... + r^6/9!)).  What the series leaves out is below 3e-10 of the sum; its inner sum is at most an eighth of 1/2 and is taken in 32 bits,
+// as constants of 64 bits would take registers from other wavefronts: both results are off by less than 2^-25 of themselves.
+// Below -100 it is -1, and where n is held it is more than 32 bits hold.
+__device__ __forceinline__ double grown_by(double x) {
+    const double y = x < -100.0 ? -100.0 : x;             // NaN stays
+    const float n = fminf(rintf((float)y * kLog2e), 250.0f);
+    const double r = y - (double)n * kLn2;
+    const float f = (float)r;
+    float p = 1.0f / 362880;
+    p = fmaf(p, f, 1.0f / 40320);
+    p = fmaf(p, f, 1.0f / 5040);
+    p = fmaf(p, f, 1.0f / 720);
+    p = fmaf(p, f, 1.0f / 120);
+    p = fmaf(p, f, 1.0f / 24);
+    p = fmaf(p, f, 1.0f / 6);
+    const double power = ldexp(1.0, (int)n);
+    return power * (r + r * r * (0.5 + (double)(p * f))) + (power - 1.0);
+}
+
 // What a policy row adds to the loss, the divergence and the clipped share, and its slope.
 struct PolicyTerms {
     float loss, kl, clipped, slope;
@@ -156,7 +176,7 @@ __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, co
     if (a.ref) {
         // x = ref - lp is small where the policy is near the one to stay near to, and exp(x) - 1 - x then the square of it, halved: in 64
         // bits, since the difference loses what 32 bits hold of it.  That of an impossible token is infinite.
-        const double away = (double)in.ref - lp, full = expm1(away);
+        const double away = (double)in.ref - lp, full = grown_by(away);
         const float grown = (float)full;
         r.kl = away == (double)kInf ? kInf : (float)(full - away);
         if (a.kl_coef != 0.0f) {
