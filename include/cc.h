@@ -418,7 +418,8 @@ int cc_embed(const void* table, int32_t dtype, int64_t V, int64_t D, int64_t tab
              float scale, void* out, int64_t out_stride, void* stream);
 
 /*
- * Its gradient: grad_table[v] = scale * (sum of grad[i] over the i with ids[i] = v), added up in 32 bits in the order of i
+ * Its gradient: grad_table[v] = scale * (sum of grad[i] over the i with ids[i] = v), added up in 32 bits: stretches of an id's rows in
+ * the order of i, then the stretches' sums, in an order that depends on the sizes and the ids alone
  * (Section 4.3 scores many orders over the same nodes: every node has as many rows to add as there are orders).
  *   grad        [n, D], rows grad_stride apart, of type dtype
  *   grad_table  [V, D], rows grad_table_stride apart, of type grad_dtype: CC_F32 or dtype.  Written in full; with
@@ -523,6 +524,8 @@ size_t cc_token_workspace_bytes(int64_t B, int64_t T);
  *   logprob       fp32 [B, T]
  *   grad_logits   [B, T, V] of type dtype, or NULL (no gradient); may be the logits' own memory (same strides)
  * Positions that do not count have no part in anything; with none at all stats and gradient are zero.
+ * An advantage of zero has no part either, whatever the ratio, nor has a divergence whose coefficient is zero; that of an impossible
+ * token (log-probability minus infinity) is infinite.
  */
 int cc_policy_loss(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t,
                    const int32_t* tokens, const uint8_t* mask, int32_t placed, float scale, const float* old_logprob,

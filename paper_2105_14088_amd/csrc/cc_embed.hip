@@ -1,6 +1,6 @@
 // Embedding lookup with scaling and its gradient (cc.h: cc_embed, cc_embed_backward).
 //
-//   out[i] = scale * table[ids[i]],     grad_table[v] = scale * (sum of grad[i] over the i with ids[i] = v, in order of i)
+//   out[i] = scale * table[ids[i]],     grad_table[v] = scale * (sum of grad[i] over the i with ids[i] = v)
 //
 // An id outside [0, V) is no token: its output row is zero and its gradient goes nowhere.
 //
@@ -8,9 +8,9 @@
 // would add them in another order on every call.  Tokens are sorted by id instead, stably, so that equal ids keep their order (few
 // by counting for each how many come before it, many by a counting sort).  The sorted list is cut into segments of equal length,
 // and each segment is summed by lanes that lie along a row: frequent tokens are then shared by many segments and rare ones
-// share one, so no distribution of ids leaves a workgroup with more to do than the others.  A run of one id that crosses a
-// border leaves a partial sum on each side of it; a last kernel adds those.  The order of additions depends on sizes and ids
-// alone.
+// share one, so no distribution of ids leaves a workgroup with more to do than the others.  Within a segment an id's rows are added in
+// the order of i.  A run of one id that crosses a border leaves a partial sum on each side of it; a last kernel adds those, every
+// so many of them by a group of lanes and then the groups.  The order of additions depends on sizes and ids alone.
 //
 // Rows of ids that do not occur are zero.  All rows are cleared by additional workgroups of the kernels that sort: these wait for
 // memory and leave its bandwidth unused, and to find the absent rows first took longer than to write the others twice.
@@ -415,7 +415,8 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const S* __restric
         Pack<S, VEC> row[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) key[u] = keys[i + u];
-        // beyond the segment's end, and for what is no token, the segment's first row stands in
+        // beyond the segment's end its first row stands in; the row of what is no token is loaded from its place and summed like others,
+        // and the sum dropped
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int p = i + u < to ? pos[i + u] : pos[from];

@@ -21,7 +21,9 @@
 #include "cc_internal.h"
 #include "cc_model.h"
 
-// A position gives the same bits whichever walk it is worked in: products and sums are fused where fmaf says so and nowhere else.
+// From the same state a position gives the same bits whichever walk it is worked in: products and sums are fused where fmaf says so and
+// nowhere else.  (The state that a segment starts from is chained from rounded products of gates: T steps of one position give the
+// bits of one call where its positions are not cut into segments.)
 #pragma clang fp contract(off)
 
 namespace cc {
@@ -32,7 +34,10 @@ using namespace ccm;
 constexpr int kThreads = 256, L = kScanChunk;
 
 // keep and take from e = exp(-|gate|): 1 / (1 + e) and e / (1 + e), neither of them as one minus the other, so that both keep
-// their relative precision.
+// their relative precision.  In 32 bits: the exponential of a rounded product with log2 e (off by up to 1.5 |gate| 2^-24 and its last
+// bit) and the reciprocal instruction (last bit) without a step to refine it: a step would take three operations of some twenty an
+// element to win the last bit of a gate (1024 x 64 x 128 fp32, forward and backward: 1.40e-7 off the definition, elementary
+// operations in 32 bits 1.24e-7).
 //
 // The smaller one is held as two factors, each with half of the exponential's argument.  What it multiplies is then rounded once
 // where the product is subnormal, and the exponential instruction, which gives 0 for subnormal results, is never asked for

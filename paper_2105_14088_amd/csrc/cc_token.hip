@@ -163,6 +163,8 @@ __device__ __forceinline__ PolicyInputs policy_inputs(const Args& a, int64_t at,
 }
 __device__ __forceinline__ PolicyTerms policy_terms(const Args& a, double lp, const PolicyInputs& in) {
     PolicyTerms r;
+    // of a difference x in 64 bits, rounded: off by |x| 2^-24 and the function's last bit, the result's own rounding where a ratio counts
+    // (|x| < 1; in 64 bits throughout, 8192 rows of 65536 bf16 took 1 % longer)
     const float ratio = expf((float)(lp - (double)in.old_lp));
     // a ratio that 32 bits do not hold still has no part where there is no advantage, nor a divergence that counts for nothing; that
     // of an undefined log-probability makes the loss undefined
