@@ -924,10 +924,11 @@ int64_t launch_rows(Args& a, bool placed, hipStream_t s) {
     } else {
         // 256 threads or 1024 a row, in us of the forward kernel: rows short of a turn of 1024 threads' vectors leave most of these
         // without one (4096 x 5000 bf16: 12.7, 26.4; 4096 x 8192: 14.6, 26.2); fewer rows than two workgroups a compute unit want all
-        // threads they can get (256 x 16384: 4.8, 4.4; 256 x 65536: 10.9, 8.0; 256 x 300007: 40.7, 31.7; but 512 x 33000: 9.4, 10.4);
-        // rows of several turns gain from long runs (2048 x 33000: 28.2, 33.1; 4096 x 50001: 96, 95; 4096 x 65536: 107, 94).
-        const bool few = a.B * a.T < 512;
-        if (V <= 1024 * VEC || (!few && V < 1024 * VEC * 8)) return launch_long<S, 256, 0, KIND>(a, s);
+        // threads they can get (256 x 16384: 4.8, 4.4; 256 x 65536: 10.9, 8.0; 256 x 300007: 40.7, 31.7; but 512 x 16384: 5.6, 6.1); longer
+        // ones want them the sooner the fewer rows there are (1024 x 16384: 8.3, 9.8; 1024 x 32768: 15.1, 15.4; 1024 x 65536: 27.9, 26.5;
+        // 2048 x 33000: 28.2, 33.1; 4096 x 50001: 96, 95; 4096 x 65536: 107, 94).
+        const int64_t rows = a.B * a.T, most = rows < 512 ? 1024 * VEC : rows < 2048 ? 4096 * VEC : 8192 * VEC - 1;
+        if (V <= most) return launch_long<S, 256, 0, KIND>(a, s);
         return launch_long<S, 1024, 0, KIND>(a, s);
     }
 }

@@ -624,9 +624,10 @@ def test_preference_of_pairs_on_both_sides_of_one_workgroup(pairs, t, at_once):
     check_preference(*make(2 * pairs, t, 5, torch.float32, pairs + t), False)
 
 
-@pytest.mark.parametrize("b,t,v", [(16, 32, 4096), (16, 32, 4097), (7, 73, 4096), (7, 73, 4097), (16, 32, 32767), (16, 32, 32768), (7, 73, 32767)])
+@pytest.mark.parametrize("b,t,v", [(16, 32, 4096), (16, 32, 4097), (7, 73, 4096), (7, 73, 4097), (16, 32, 32767), (16, 32, 32768), (7, 73, 32767),
+                                   (16, 32, 16384), (16, 32, 16385), (89, 23, 16385), (64, 32, 16385), (64, 32, 32767), (64, 32, 32768)])
 def test_rows_on_both_sides_of_larger_workgroups(b, t, v, at_once):
-    """512 rows and fewer, about one turn of the larger workgroups and eight: the same logits for all orders."""
+    """About 512 and 2048 rows, of one turn of the larger workgroups, four and eight: the same logits for all orders."""
     say(f"logprob b={b} t={t} v={v}")
     logits, tokens, _ = make(1, t, v, torch.float32, 6, masked=False)
     p, rest, lp, valid, rel = ref.rows(logits, tokens, None, False, SCALE)
