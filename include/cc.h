@@ -391,8 +391,9 @@ int cc_validate_matrix(const int32_t* cost_matrix, int32_t N, int32_t require_sy
  * its own (BCube, double binary tree), orders can be proposed by a policy that learns from the batch calls' costs.  An order is a
  * sequence of tokens: nodes are the vocabulary, rank t is position t, and a node that is placed is not placed again.  The
  * calls below are the parts of such a policy that matrix products do not cover, forward and backward: a table of vectors
- * looked up by node, a recurrence that carries what has been placed, log-probabilities of the orders' nodes, and
- * the losses.  They serve sequences over any vocabulary alike.
+ * looked up by node, a recurrence that carries what has been placed, the norm of a sum of layers, log-probabilities of the
+ * orders' nodes, the losses, and for sampling the product of rows in 8 bits and the shaping of logits.  They serve sequences over any
+ * vocabulary alike.
  *   - Elements are of one of the types below; computation is in 32-bit floating point or wider, each result is rounded once.
  *   - Strides are in elements.  The innermost dimension is contiguous; a matrix or row may start at any element.
  *   - Results do not depend on timing: the same call gives the same bits.
@@ -551,6 +552,107 @@ int cc_preference_loss(const void* logits, int32_t dtype, int64_t B, int64_t T, 
                        float beta, float label_smoothing, float grad_scale, float* loss, float* margin, float* logprob,
                        void* grad_logits, int64_t grad_stride_b, int64_t grad_stride_t, void* workspace,
                        size_t workspace_bytes, void* stream);
+
+/*
+ * The sum of two layers' outputs and its root-mean-square norm (between the layers of a policy that proposes Section 4.3's orders):
+ *     h = x + residual, rounded to an element of dtype;  r = 1 / sqrt(mean of h^2 + eps);  out = h r weight
+ * and, for products in 8 bits (cc_product_i8), the same row as whole numbers with a scale: with u = h weight,
+ *     q = the whole number nearest to 127 u / max|u| (ties to even),  scale = r max|u| / 127:  out is about q scale
+ *   x, residual  [n, D] of type dtype, rows apart as given; residual NULL: h = x
+ *   weight       [D] of type weight_dtype, CC_F32 or dtype, or NULL (ones)
+ *   eps          > 0
+ *   sum          [n, D] of type dtype or NULL: h.  May be x's or residual's own memory (same stride).
+ *   out          [n, D] of type dtype or NULL
+ *   q, scale     int8 [n, D] and fp32 [n], both or neither
+ *   rstd         fp32 [n] or NULL: r, what the backward call needs
+ * A row of zeros has q and scale zero; one whose u holds an infinite or undefined element has q zero and scale NaN, so that
+ * products with it are undefined.  Squares are summed in 64 bits.
+ */
+int cc_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, int32_t dtype, int64_t n,
+                int64_t D, const void* weight, int32_t weight_dtype, float eps, void* sum, int64_t sum_stride, void* out,
+                int64_t out_stride, int8_t* q, int64_t q_stride, float* scale, float* rstd, void* stream);
+
+/*
+ * Its gradient (of `out`; trained beside the rest of the policy that stands in for Section 4.3's search): with g = grad_out weight,
+ *     grad_h = r (g - h r mean(g h r)) + grad_sum,  grad_weight = sum over rows of grad_out h r
+ * grad_h is the gradient of x and of residual alike.
+ *   h            [n, D] of type dtype: the forward call's sum (x without a residual);  rstd fp32 [n]
+ *   grad_sum     [n, D] of type dtype or NULL (zero): the gradient that reaches h past the norm
+ *   grad_h       [n, D] of type dtype; may be grad_out's or grad_sum's own memory (same stride)
+ *   grad_weight  [D] of type grad_weight_dtype, CC_F32 or weight_dtype, or NULL; with accumulate != 0 the sum is added to what
+ *                is there.  It is summed in 32 bits, in an order that depends on the sizes alone.
+ * Workspace: cc_rms_norm_workspace_bytes(n, D), only for grad_weight.
+ */
+size_t cc_rms_norm_workspace_bytes(int64_t n, int64_t D);
+int cc_rms_norm_backward(const void* grad_out, int64_t grad_out_stride, const void* h, int64_t h_stride, int32_t dtype, int64_t n,
+                         int64_t D, const void* weight, int32_t weight_dtype, const float* rstd, const void* grad_sum,
+                         int64_t grad_sum_stride, void* grad_h, int64_t grad_h_stride, void* grad_weight,
+                         int32_t grad_weight_dtype, int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rows as whole numbers of 8 bits with a scale each (the weights of a policy from which many of Section 4.3's orders are sampled, once, and
+ * activations that no norm precedes): q = the whole number nearest to 127 x / max|x| (ties to even), scale = max|x| / 127.
+ *   x [n, D] of type dtype;  q int8 [n, D];  scale fp32 [n].  Rows of zeros and undefined rows as for cc_rms_norm.
+ */
+int cc_quantize_rows(const void* x, int64_t x_stride, int32_t dtype, int64_t n, int64_t D, int8_t* q, int64_t q_stride,
+                     float* scale, void* stream);
+
+/*
+ * Product of rows in 8 bits with a scale for each row and each channel (a sampling policy's layers, and its logits over
+ * Section 4.3's nodes):
+ *     out[m, n] = x_scale[m] w_scale[n] (sum over k of x[m, k] w[n, k]) + bias[n]
+ *   x    int8 [M, K], rows x_stride apart;  x_scale fp32 [M]: of cc_rms_norm or cc_quantize_rows
+ *   w    int8 [N, K], rows w_stride apart;  w_scale fp32 [N]: a layer's weights, a row for each channel
+ *   bias fp32 [N] or NULL
+ *   out  [M, N] of type dtype, rows out_stride apart
+ * The sum is exact (all values of int8 are served), so K is at most CC_PRODUCT_MAX_K; what follows is computed in 32 bits.
+ * K = 0 gives the bias.  out has at most 2^40 elements.
+ * Workspace: cc_product_i8_workspace_bytes(M, N, K), which may be 0.
+ */
+#define CC_PRODUCT_MAX_K ((1 << 17) - 1)
+size_t cc_product_i8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int cc_product_i8(const int8_t* x, int64_t x_stride, const float* x_scale, const int8_t* w, int64_t w_stride, const float* w_scale,
+                  const float* bias, int64_t M, int64_t N, int64_t K, void* out, int64_t out_stride, int32_t dtype,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Logits shaped before a token is drawn from them or its log-probability taken.  Row (b, t) looks back on the first
+ * lengths[b] + t entries of history[b, :] (at most L); a token j that is among them is seen, and counts as often as it is among those from
+ * starts[b] on.  With (r, p, f) = penalties[b, :], every logit z_j becomes
+ *     z_j > 0 ? z_j / r : z_j r      where j is seen
+ *     less p + f count_j             where count_j > 0
+ *     plus bias_j
+ *   and minus infinity, whatever it is (NaN and infinities included), where it is forbidden: its bit of `allowed` is 0, its bias is minus
+ *   infinity, or count_j > 0 and p or f is plus infinity.  (1, infinity, 0) forbids the nodes that an order has placed (Section 4.3).
+ *   logits     [B, T, V] of type dtype
+ *   history    int32 [B, L], rows history_stride apart, or NULL (L = 0); entries outside [0, V) are no token
+ *   lengths    int32 [B] or NULL (zero).  While sampling, T = 1 and lengths[b] is what there is before the token; where the
+ *              tokens [B, T] of whole orders are the history, row t sees the t tokens before it.
+ *   starts     int32 [B] or NULL (zero): where what is not the prompt begins
+ *   penalties  fp32 [B, 3] or NULL (1, 0, 0)
+ *   bias       fp32 [V], bias_stride 0, or one of each sequence, [B, V], bias_stride apart, or NULL.  It is a constant.
+ *   allowed    uint32 [B, T, ceil(V / 32)], strides as given (0: shared), or NULL: bit j % 32 of word j / 32 allows j
+ *   out        [B, T, V] of type dtype; may be the logits' own memory (same strides)
+ * Computed in 32 bits from z_j on, rounded once.  A row that nothing is left of is minus infinity throughout.
+ */
+int cc_shape_logits(const void* logits, int32_t dtype, int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t,
+                    const int32_t* history, int64_t L, int64_t history_stride, const int32_t* lengths, const int32_t* starts,
+                    const float* penalties, const float* bias, int64_t bias_stride, const uint32_t* allowed,
+                    int64_t allowed_stride_b, int64_t allowed_stride_t, void* out, int64_t out_stride_b, int64_t out_stride_t,
+                    void* stream);
+
+/*
+ * Its gradient, for a policy trained on the distribution that Section 4.3's orders are sampled from: that of `out` divided by r
+ * where j is seen and z_j > 0, times r where it is seen and z_j is not, and zero, whatever grad_out holds, where j is forbidden.
+ * The arguments in common are the forward call's (the logits as they were before it).
+ *   grad_out     [B, T, V] of type dtype
+ *   grad_logits  [B, T, V] of type dtype; may be grad_out's own memory (same strides)
+ */
+int cc_shape_logits_backward(const void* grad_out, int64_t grad_stride_b, int64_t grad_stride_t, const void* logits, int32_t dtype,
+                             int64_t B, int64_t T, int64_t V, int64_t stride_b, int64_t stride_t, const int32_t* history, int64_t L,
+                             int64_t history_stride, const int32_t* lengths, const int32_t* starts, const float* penalties,
+                             const float* bias, int64_t bias_stride, const uint32_t* allowed, int64_t allowed_stride_b,
+                             int64_t allowed_stride_t, void* grad_logits, int64_t out_stride_b, int64_t out_stride_t, void* stream);
 
 /* Static, human-readable text for a cc_status value (host pointer, never freed). */
 const char* cc_status_string(int status);

@@ -29,7 +29,8 @@ EXPORTS = ["cc_ring_cost_batch", "cc_ring_cost_batch_u8", "cc_ring_cost_batch_u1
            "cc_sa_rd_search_ex", "cc_init_tours", "cc_cost_matrix_from_probes", "cc_validate_matrix",
            "cc_embed", "cc_embed_workspace_bytes", "cc_embed_backward", "cc_gated_scan", "cc_gated_scan_workspace_bytes",
            "cc_gated_scan_backward", "cc_token_logprob", "cc_token_logprob_backward", "cc_token_workspace_bytes", "cc_policy_loss",
-           "cc_preference_loss",
+           "cc_preference_loss", "cc_rms_norm", "cc_rms_norm_workspace_bytes", "cc_rms_norm_backward", "cc_quantize_rows",
+           "cc_product_i8", "cc_product_i8_workspace_bytes", "cc_shape_logits", "cc_shape_logits_backward",
            "cc_status_string", "cc_last_hip_error", "cc_version"]
 
 
@@ -135,6 +136,23 @@ def lib() -> ctypes.CDLL:
         L.cc_policy_loss.argtypes = logits + [p, p, p, i32, f, f, f, i32, f, p, p, p, i64, i64, p, sz, p]
         L.cc_preference_loss.restype = ctypes.c_int
         L.cc_preference_loss.argtypes = logits + [p, f, f, f, p, p, p, p, i64, i64, p, sz, p]
+        L.cc_rms_norm.restype = ctypes.c_int
+        L.cc_rms_norm.argtypes = [p, i64, p, i64, i32, i64, i64, p, i32, f, p, i64, p, i64, p, i64, p, p, p]
+        L.cc_rms_norm_workspace_bytes.restype = sz
+        L.cc_rms_norm_workspace_bytes.argtypes = [i64, i64]
+        L.cc_rms_norm_backward.restype = ctypes.c_int
+        L.cc_rms_norm_backward.argtypes = [p, i64, p, i64, i32, i64, i64, p, i32, p, p, i64, p, i64, p, i32, i32, p, sz, p]
+        L.cc_quantize_rows.restype = ctypes.c_int
+        L.cc_quantize_rows.argtypes = [p, i64, i32, i64, i64, p, i64, p, p]
+        L.cc_product_i8_workspace_bytes.restype = sz
+        L.cc_product_i8_workspace_bytes.argtypes = [i64, i64, i64]
+        L.cc_product_i8.restype = ctypes.c_int
+        L.cc_product_i8.argtypes = [p, i64, p, p, i64, p, p, i64, i64, i64, p, i64, i32, p, sz, p]
+        shaped = [p, i32, i64, i64, i64, i64, i64, p, i64, i64, p, p, p, p, i64, p, i64, i64, p, i64, i64, p]
+        L.cc_shape_logits.restype = ctypes.c_int
+        L.cc_shape_logits.argtypes = shaped
+        L.cc_shape_logits_backward.restype = ctypes.c_int
+        L.cc_shape_logits_backward.argtypes = [p, i64, i64] + shaped
         L.cc_status_string.restype = ctypes.c_char_p
         L.cc_status_string.argtypes = [ctypes.c_int]
         L.cc_last_hip_error.restype = ctypes.c_int

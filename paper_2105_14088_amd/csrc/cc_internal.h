@@ -139,7 +139,8 @@ hipError_t launch_rdswap(const int32_t* c, int N, int restarts, uint64_t seed, b
 hipError_t launch_best_restart(const int64_t* costs, const int32_t* tours, int N, int restarts, int32_t* best_perm,
                                int64_t* best_cost, int32_t* best_restart, hipStream_t s);
 
-// ---- The order model (cc_model_api.hip checks; cc_embed.hip, cc_scan.hip, cc_token.hip compute).  Element types: cc.h, cc_dtype.
+// ---- The order model (cc_model_api.hip checks; cc_embed.hip, cc_scan.hip, cc_token.hip, cc_norm.hip, cc_product.hip, cc_shape.hip
+// compute).  Element types: cc.h, cc_dtype.
 constexpr int kF32 = 0, kF16 = 1, kBF16 = 2;
 
 struct EmbedCall {
@@ -200,5 +201,55 @@ struct TokenCall {
 };
 size_t token_workspace_bytes(int64_t B, int64_t T);
 hipError_t launch_token(TokenKind kind, const TokenCall& c, hipStream_t s);
+
+struct NormCall {
+    const void *x, *residual, *weight;   // the last two or null
+    int dtype, weight_dtype;
+    int64_t n, D, x_stride, residual_stride, sum_stride, out_stride, q_stride;
+    double eps;
+    void *sum, *out;              // or null
+    int8_t* q;                    // or null, with scale
+    float *scale, *rstd;
+};
+hipError_t launch_norm(const NormCall& c, hipStream_t s);
+hipError_t launch_quantize(const NormCall& c, hipStream_t s);    // x, q and scale alone
+
+struct NormBackwardCall {
+    const void *grad, *h, *weight, *grad_sum;   // the last two or null
+    const float* rstd;
+    int dtype, weight_dtype, grad_weight_dtype;
+    int64_t n, D, grad_stride, h_stride, grad_sum_stride, grad_h_stride;
+    void *grad_h, *grad_weight;   // the latter or null
+    bool accumulate;
+    void* workspace;
+};
+size_t norm_workspace_bytes(int64_t n, int64_t D);
+hipError_t launch_norm_backward(const NormBackwardCall& c, hipStream_t s);
+
+struct ProductCall {
+    const int8_t *x, *w;
+    const float *x_scale, *w_scale, *bias;      // bias or null
+    int64_t M, N, K, x_stride, w_stride, out_stride;
+    void* out;
+    int dtype;
+    void* workspace;
+};
+size_t product_workspace_bytes(int64_t M, int64_t N, int64_t K);
+hipError_t launch_product(const ProductCall& c, hipStream_t s);
+
+struct ShapeCall {
+    const void *logits, *grad;    // forward: grad null
+    int dtype;
+    int64_t B, T, V, stride_b, stride_t, grad_stride_b, grad_stride_t, out_stride_b, out_stride_t;
+    const int32_t* history;       // or null: nothing is looked back on
+    int64_t L, history_stride;
+    const int32_t *lengths, *starts;
+    const float *penalties, *bias;
+    int64_t bias_stride;
+    const uint32_t* allowed;
+    int64_t allowed_stride_b, allowed_stride_t;
+    void* out;                    // the shaped logits, or the logits' gradient
+};
+hipError_t launch_shape(const ShapeCall& c, hipStream_t s);
 
 }  // namespace cc

@@ -1,0 +1,383 @@
+// Product of rows in 8 bits with a scale for each row and each channel (cc.h: cc_product_i8).
+//
+//   out[m, n] = x_scale[m] w_scale[n] (sum over k of x[m, k] w[n, k]) + bias[n]
+//
+// The sum is one of whole numbers in 32 bits: at most 131071 terms of at most 2^14, so it is exact and does not depend on
+// how it is cut.  Terms beyond K are zeros that are put where a tile ends inside a row; nothing beyond a row is read.
+//
+// tile_kernel: a workgroup has a tile of the result and goes along K in steps of 128 bytes.  Both operands come to LDS in pieces of 16
+// bytes, straight from memory where rows allow it (16-byte alignment), through registers else.  In LDS a row has 8 such pieces,
+// and piece c lies at place c ^ (row % 8): the lanes that read the same piece of 8 rows then use all banks once.  Two tiles are held:
+// while one is multiplied, the next is on its way.  The last quarter of a tile's products is done behind the barrier that
+// ends it, so that the first operands of the next tile are read while the matrix cores are busy.
+//
+// few_kernel: up to 32 rows, where reading the weights is what takes time: they go from memory to registers, each once; several
+// wavefronts share a channel's K where there are few channels.
+#include <hip/hip_runtime.h>
+
+#include "cc_internal.h"
+#include "cc_model.h"
+
+namespace cc {
+namespace {
+
+using namespace ccm;
+
+typedef int Int4 __attribute__((ext_vector_type(4)));
+typedef int Int16 __attribute__((ext_vector_type(16)));
+
+constexpr int kStep = 128;               // bytes of K in a tile
+constexpr int kPiece = 16;
+
+struct Args {
+    const int8_t *x, *w;
+    const float *x_scale, *w_scale, *bias;
+    int64_t M, x_stride, w_stride, out_stride;
+    int N, K;
+    void* out;
+    int tiles_m, tiles_n;
+};
+
+// 16 bytes of a row from k on; what lies beyond K is zero and not read.
+__device__ __forceinline__ Int4 load_piece(const int8_t* row, int k, int K) {
+    Int4 v = {0, 0, 0, 0};
+    if (k + kPiece <= K) {
+        __builtin_memcpy(&v, row + k, kPiece);
+    } else if (k < K) {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i)
+            if (k + i < K) w[i / 4] |= (uint32_t)(uint8_t)row[k + i] << (8 * (i % 4));
+        v = Int4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+    }
+    return v;
+}
+
+// From the exact sum on in 32 bits: it is rounded, and so is each product and the sum with the bias.
+__device__ __forceinline__ float scaled(int sum, float xs, float ws, float bias) { return (float)sum * xs * ws + bias; }
+
+template <class S>
+__device__ __forceinline__ void store_few(S* p, const S* from, int count) {
+    for (int i = 0; i < count; ++i) p[i] = from[i];
+}
+
+// Workgroups of one XCD (every eighth) get neighbouring tiles, and those in blocks of 8 rows of tiles, so that what they read at the
+// same time is shared in its L2.
+__device__ __forceinline__ void tile_of(uint32_t id, int tiles_m, int tiles_n, int& tm, int& tn) {
+    const uint32_t count = (uint32_t)tiles_m * tiles_n, xcd = id % 8, each = count / 8, more = count % 8;
+    const uint32_t at = xcd * each + min(xcd, more) + id / 8;
+    constexpr uint32_t kGroup = 8;
+    const uint32_t group = at / (kGroup * tiles_n), first = group * kGroup, rows = min(kGroup, (uint32_t)tiles_m - first);
+    const uint32_t in = at - group * kGroup * tiles_n;
+    tm = __builtin_amdgcn_readfirstlane((int)(first + in % rows));
+    tn = __builtin_amdgcn_readfirstlane((int)(in / rows));
+}
+
+template <class S, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const Args a) {
+    constexpr int THREADS = (BM / WM) * (BN / WN) * 64, WAVES = THREADS / 64;
+    constexpr int MT = WM / 32, NT = WN / 32;
+    constexpr int XBYTES = BM * kStep, WBYTES = BN * kStep, BYTES = XBYTES + WBYTES;
+    constexpr int PIECES = BYTES / (THREADS * kPiece), XPIECES = XBYTES / (THREADS * kPiece);
+    static_assert(XBYTES % (THREADS * kPiece) == 0 && WBYTES % (THREADS * kPiece) == 0, "every load of a workgroup is of one operand");
+    constexpr int STRIP = WN * (int)sizeof(S) + 16;                 // a row of the result's strip in LDS
+    static_assert(WAVES * 32 * STRIP <= 2 * BYTES, "the strips lie where the operands were");
+    __shared__ __attribute__((aligned(128))) char lds[2 * BYTES];
+    __shared__ __attribute__((aligned(16))) float channel[2][BN];   // scales and biases
+
+    const int thread = threadIdx.x, lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64);
+    const int wm = wave / (BN / WN), wn = wave % (BN / WN);
+    int tm, tn;
+    tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * BM;
+    const int n0 = tn * BN;
+    const int8_t* const xbase = a.x + m0 * a.x_stride;
+    const int8_t* const wbase = a.w + (int64_t)n0 * a.w_stride;
+    const int last_m = (int)min((int64_t)BM, a.M - m0) - 1, last_n = min(BN, a.N - n0) - 1;
+
+    for (int i = thread; i < BN; i += THREADS) {
+        const int n = n0 + min(i, last_n);
+        channel[0][i] = a.w_scale[n];
+        channel[1][i] = a.bias ? a.bias[n] : 0.0f;
+    }
+
+    // Where this thread's pieces come from: rows beyond the last are the last again, their results are not stored.
+    // Piece p of wavefront `wave` fills LDS from (p * THREADS + wave * 64) * 16 on, 8 rows.
+    const int in_row = (lane % 8) ^ ((lane / 8) % 8);
+    const auto row_of = [&](int p) {
+        const int row = ((p < XPIECES ? p : p - XPIECES) * THREADS + wave * 64 + lane) / 8;
+        return min(row, p < XPIECES ? last_m : last_n);
+    };
+    uint32_t from[DIRECT ? PIECES : 1];
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) from[p] = (uint32_t)row_of(p) * (uint32_t)(p < XPIECES ? a.x_stride : a.w_stride) + in_row * kPiece;
+    }
+    Int4 held[DIRECT ? 1 : PIECES];
+    const auto piece = [&](int p, int tile) {
+        const int8_t* const row = p < XPIECES ? xbase + row_of(p) * a.x_stride : wbase + row_of(p) * a.w_stride;
+        return load_piece(row, tile * kStep + in_row * kPiece, a.K);
+    };
+    const auto put = [&](int p, int buffer, const Int4& v) { *(Int4*)(lds + buffer * BYTES + (p * THREADS + thread) * kPiece) = v; };
+    const int tiles = (a.K + kStep - 1) / kStep;
+    const auto fetch = [&](int tile, int buffer) {
+        if (tile >= tiles) return;
+        if constexpr (DIRECT) {
+            if ((tile + 1) * kStep <= a.K) {
+                const int8_t *xk = xbase + (int64_t)tile * kStep, *wk = wbase + (int64_t)tile * kStep;
+                const uint32_t to = (uint32_t)(uintptr_t)(lds + buffer * BYTES) + wave * 1024;
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                                 :
+                                 : "s"(to + p * THREADS * kPiece), "v"(from[p]), "s"(p < XPIECES ? xk : wk)
+                                 : "memory");
+            } else {
+                // the row's end, once: not unrolled, its addresses would take registers throughout
+#pragma nounroll
+                for (int p = 0; p < PIECES; ++p) put(p, buffer, piece(p, tile));
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) held[p] = piece(p, tile);
+        }
+    };
+    // What was fetched is in LDS, for every wavefront, and nobody reads what lay there before.
+    const auto arrive = [&](int tile, int buffer) {
+        if constexpr (!DIRECT) {
+            if (tile < tiles) {
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) put(p, buffer, held[p]);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+
+    Int16 sum[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[i][j][r] = 0;
+    Int4 xf[2][MT], wf[2][NT];
+    const char* const xrow = lds + (wm * WM + lane % 32) * kStep;
+    const char* const wrow = lds + XBYTES + (wn * WN + lane % 32) * kStep;
+    const auto read = [&](int buffer, int s, int set) {
+        const int at = buffer * BYTES + ((2 * s + lane / 32) ^ (lane % 8)) * kPiece;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xf[set][i] = *(const Int4*)(xrow + at + i * 32 * kStep);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) wf[set][j] = *(const Int4*)(wrow + at + j * 32 * kStep);
+    };
+    const auto multiply = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[set][j], xf[set][i], sum[i][j], 0, 0, 0);
+    };
+
+    if (tiles == 0) {
+        __syncthreads();
+    } else {
+        fetch(0, 0);
+        arrive(0, 0);
+        fetch(1, 1);
+        read(0, 0, 0);
+        for (int t = 0; t < tiles; ++t) {
+            const int now = t & 1;
+            read(now, 1, 1);
+            multiply(0);
+            read(now, 2, 0);
+            multiply(1);
+            read(now, 3, 1);
+            multiply(0);
+            arrive(t + 1, now ^ 1);
+            fetch(t + 2, now);
+            if (t + 1 < tiles) read(now ^ 1, 0, 0);
+            multiply(1);
+        }
+    }
+
+    // A lane has channels 8 g + 4 (lane / 32) .. + 3 of row lane % 32: strips of 32 rows go through LDS, each wavefront's its
+    // own, so that rows are stored in vectors of 16 bytes side by side.
+    char* const strip = lds + wave * 32 * STRIP;
+    constexpr int VEC = 16 / sizeof(S), LANES = WN / VEC, ROWS = 64 / LANES;
+    const int nw = n0 + wn * WN;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t mw = m0 + wm * WM + i * 32;
+        const float xs = a.x_scale[min(mw + lane % 32, a.M - 1)];
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int in = j * 32 + 8 * g + 4 * (lane / 32);
+                const auto ws = *(const Pack<float, 4>*)&channel[0][wn * WN + in], bias = *(const Pack<float, 4>*)&channel[1][wn * WN + in];
+                float f[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) f[r] = scaled(sum[i][j][4 * g + r], xs, ws.get(r), bias.get(r));
+                *(Pack<S, 4>*)(strip + (lane % 32) * STRIP + in * sizeof(S)) = Pack<S, 4>::from(f);
+            }
+        wave_order();
+#pragma unroll
+        for (int r = 0; r < 32; r += ROWS) {
+            const int row = r + lane / LANES, n = nw + lane % LANES * VEC;
+            const int64_t m = mw + row;
+            if (m < a.M && n < a.N) {
+                const auto v = *(const Pack<S, VEC>*)(strip + row * STRIP + lane % LANES * 16);
+                S* const to = (S*)a.out + m * a.out_stride + n;
+                if (n + VEC <= a.N) {
+                    store_pack(to, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (n + e < a.N) to[e] = v.element(e);
+                }
+            }
+        }
+        wave_order();
+    }
+}
+
+// MT * 16 rows, 16 channels to `share` wavefronts of a workgroup's 8, each of which has a stretch of K.
+constexpr int kFewWaves = 8;
+template <class S, int MT>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int share) {
+    __shared__ Int4 parts[kFewWaves][MT][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t n0 = ((int64_t)blockIdx.x * (kFewWaves / share) + wave / share) * 16;
+    const int steps = (a.K + 63) / 64, each = (steps + share - 1) / share;
+    const int begin = min(wave % share * each, steps), end = min(begin + each, steps);
+    Int4 sum[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sum[i] = Int4{0, 0, 0, 0};
+    if (n0 < a.N) {
+        const int8_t* const wrow = a.w + min(n0 + lane % 16, (int64_t)a.N - 1) * a.w_stride;
+        const int8_t* xrow[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xrow[i] = a.x + min((int64_t)i * 16 + lane % 16, a.M - 1) * a.x_stride;
+        const int in = lane / 16 * kPiece;
+        constexpr int U = 8;
+        int s = begin;
+        for (; s + U <= end && (s + U) * 64 <= a.K; s += U) {
+            Int4 w[U], x[U][MT];
+#pragma unroll
+            for (int u = 0; u < U; ++u) __builtin_memcpy(&w[u], wrow + (s + u) * 64 + in, kPiece);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) __builtin_memcpy(&x[u][i], xrow[i] + (s + u) * 64 + in, kPiece);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) sum[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], x[u][i], sum[i], 0, 0, 0);
+        }
+        for (; s < end; ++s) {
+            const Int4 w = load_piece(wrow, s * 64 + in, a.K);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sum[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, load_piece(xrow[i], s * 64 + in, a.K), sum[i], 0, 0, 0);
+        }
+    }
+    if (share > 1) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) parts[wave][i][lane] = sum[i];
+        __syncthreads();
+        if (wave % share != 0) return;
+        for (int p = 1; p < share; ++p)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sum[i] += parts[wave + p][i][lane];
+    }
+    // a lane has channels 4 (lane / 16) .. + 3 of row lane % 16
+    const int64_t n = n0 + lane / 16 * 4;
+    if (n >= a.N) return;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = i * 16 + lane % 16;
+        if (m >= a.M) continue;
+        const float xs = a.x_scale[m];
+        S* const to = (S*)a.out + m * a.out_stride + n;
+        float f[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t c = min(n + r, (int64_t)a.N - 1);
+            f[r] = scaled(sum[i][r], xs, a.w_scale[c], a.bias ? a.bias[c] : 0.0f);
+        }
+        if (n + 4 <= a.N) {
+            store_pack(to, Pack<S, 4>::from(f));
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (n + r < a.N) to[r] = narrow<S>(f[r]);
+        }
+    }
+}
+
+template <class S, int BM, int BN, int WM, int WN>
+void launch_tiles(Args a, bool direct, hipStream_t s) {
+    a.tiles_m = (int)((a.M + BM - 1) / BM);
+    a.tiles_n = (a.N + BN - 1) / BN;
+    const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n)), block((BM / WM) * (BN / WN) * 64);
+    if (direct) {
+        hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, true>), grid, block, 0, s, a);
+    } else if constexpr (BM < 256) {
+        hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, false>), grid, block, 0, s, a);
+    }
+}
+
+bool rows_at_16(const void* p, int64_t stride) {
+    // rows of a tile are addressed by 32 bits from its first
+    return ((uintptr_t)p & 15) == 0 && stride % 16 == 0 && stride < (1 << 24);
+}
+
+template <class S>
+void run(const Args& a, hipStream_t s) {
+    const bool direct = rows_at_16(a.x, a.x_stride) && rows_at_16(a.w, a.w_stride);
+    const auto tiles = [&](int64_t bm, int64_t bn) { return ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
+    if (a.M <= 32) {
+        const int64_t stretches = (a.N + 15) / 16;
+        int share = 1;
+        while (share < kFewWaves && stretches * share < 2048 && a.K > 512 * share) share *= 2;
+        const int64_t per = kFewWaves / share;
+        const dim3 grid((unsigned)((stretches + per - 1) / per));
+        if (a.M <= 16) hipLaunchKernelGGL((few_kernel<S, 1>), grid, dim3(kFewWaves * 64), 0, s, a, share);
+        else hipLaunchKernelGGL((few_kernel<S, 2>), grid, dim3(kFewWaves * 64), 0, s, a, share);
+    } else if (direct && tiles(256, 256) >= 192) {
+        launch_tiles<S, 256, 256, 128, 128>(a, direct, s);
+    } else if (tiles(128, 128) >= 192) {
+        launch_tiles<S, 128, 128, 64, 64>(a, direct, s);
+    } else {
+        launch_tiles<S, 64, 64, 32, 32>(a, direct, s);
+    }
+}
+
+}  // namespace
+
+size_t product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    (void)M;
+    (void)N;
+    (void)K;
+    return 0;
+}
+
+hipError_t launch_product(const ProductCall& c, hipStream_t s) {
+    Args a = {};
+    a.x = c.x;
+    a.w = c.w;
+    a.x_scale = c.x_scale;
+    a.w_scale = c.w_scale;
+    a.bias = c.bias;
+    a.M = c.M;
+    a.N = (int)c.N;
+    a.K = (int)c.K;
+    a.x_stride = c.x_stride;
+    a.w_stride = c.w_stride;
+    a.out_stride = c.out_stride;
+    a.out = c.out;
+    if (c.dtype == kF32) run<float>(a, s);
+    else if (c.dtype == kF16) run<_Float16>(a, s);
+    else run<__bf16>(a, s);
+    return hipGetLastError();
+}
+
+}  // namespace cc

@@ -1,5 +1,6 @@
 """Binding of the order model's calls (include/cc.h, from cc_embed on): embedding lookup and gradient, gated recurrence and
-gradient, log-probabilities, policy loss, preference loss.
+gradient, log-probabilities, policy loss, preference loss, norm of a sum and gradient, rows and products in 8 bits, shaped logits and
+gradient.
 
 As in binding.py, only arguments are marshalled here: device tensors in, device tensors out, on the current stream or the
 one given.  Tensors may be strided as long as their last dimension is contiguous; a tensor made here is contiguous."""
@@ -311,3 +312,227 @@ def cc_preference_loss(logits: torch.Tensor, tokens: torch.Tensor, ref_logprob: 
                                 loss.data_ptr(), margin.data_ptr(), logprob.data_ptr(), *to, ws, nbytes, _stream(stream)),
            "cc_preference_loss")
     return PreferenceLoss(loss, margin, logprob, grad_logits if grad else None)
+
+
+# ------------------------------------------------------------------------------------------ norm, rows and products in 8 bits
+
+
+class RmsNorm(NamedTuple):
+    """out: the normalised rows, or None; sum: x + residual (x itself without one); q int8 and scale float32, or None; rstd
+    float32, or None.  All of x's shape, scale and rstd without its last dimension."""
+    out: Optional[torch.Tensor]
+    sum: torch.Tensor
+    q: Optional[torch.Tensor]
+    scale: Optional[torch.Tensor]
+    rstd: Optional[torch.Tensor]
+
+
+def _rows(t: torch.Tensor, shape, dtype, name: str):
+    """Where the rows of a tensor [..., D] lie, and how far apart: contiguous, or [n, D] with rows apart."""
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    if t.is_cuda and t.dtype is dtype and t.shape == shape and len(shape) != 2:
+        raise ValueError(f"{name} must be contiguous, or [n, D] with rows apart")
+    return _strided(t, shape, dtype, name)
+
+
+def _rows_new(t: Optional[torch.Tensor], shape, dtype, device, stream, name: str):
+    if t is None:
+        t = _new(shape, dtype, device, stream)
+        return t, (t.data_ptr(), shape[-1])
+    return t, _rows(t, shape, dtype, name)
+
+
+_NOWHERE = (None, 0)
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_bytes(n: int, d: int) -> int:
+    return lib().cc_rms_norm_workspace_bytes(n, d)
+
+
+@functools.lru_cache(maxsize=4096)
+def _product_bytes(m: int, n: int, k: int) -> int:
+    return lib().cc_product_i8_workspace_bytes(m, n, k)
+
+
+def cc_rms_norm_workspace_bytes(n: int, d: int) -> int:
+    return int(lib().cc_rms_norm_workspace_bytes(n, d))
+
+
+def cc_product_i8_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(lib().cc_product_i8_workspace_bytes(m, n, k))
+
+
+def _weight(weight: Optional[torch.Tensor], d: int, dtype, name: str):
+    """Where a weight lies and its type's code."""
+    if weight is None:
+        return None, _DTYPES[dtype]
+    if weight.dtype is not torch.float32 and weight.dtype is not dtype:
+        raise ValueError(f"{name} must be float32 or {dtype}")
+    return _plain(weight, (d,), weight.dtype, name), _DTYPES[weight.dtype]
+
+
+def cc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                normed: bool = True, quantized: bool = False, save_rstd: bool = False, out: Optional[torch.Tensor] = None,
+                sum: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                rstd: Optional[torch.Tensor] = None, stream=None) -> RmsNorm:
+    """The norm of x + residual, [..., D]; `sum` may be x or residual itself.  normed: the rows in x's type; quantized: as int8
+    with a scale each, for cc_product_i8; save_rstd: with what cc_rms_norm_backward needs."""
+    shape, dtype, device = x.shape, x.dtype, x.device
+    code = _dtype(x, "x")
+    if not shape:
+        raise ValueError("x must be [..., D]")
+    d, lead = shape[-1], shape[:-1]
+    n = x.numel() // d if d else 0
+    x_at = _rows(x, shape, dtype, "x")
+    residual_at = sum_to = out_to = q_to = _NOWHERE
+    if residual is not None:
+        residual_at = _rows(residual, shape, dtype, "residual")
+    if residual is not None or sum is not None:
+        sum, sum_to = _rows_new(sum, shape, dtype, device, stream, "sum")
+    if normed or out is not None:
+        out, out_to = _rows_new(out, shape, dtype, device, stream, "out")
+    scale_to = rstd_to = None
+    if quantized or q is not None:
+        q, q_to = _rows_new(q, shape, torch.int8, device, stream, "q")
+        scale, scale_to = _plain_out(scale, lead, torch.float32, device, stream, "scale")
+    elif scale is not None:
+        raise ValueError("scale goes with quantized rows")
+    if save_rstd or rstd is not None:
+        rstd, rstd_to = _plain_out(rstd, lead, torch.float32, device, stream, "rstd")
+    _check(lib().cc_rms_norm(*x_at, *residual_at, code, n, d, *_weight(weight, d, dtype, "weight"), eps, *sum_to, *out_to, *q_to,
+                             scale_to, rstd_to, _stream(stream)), "cc_rms_norm")
+    return RmsNorm(out, x if sum is None else sum, q, scale, rstd)
+
+
+def cc_rms_norm_backward(grad_out: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                         grad_sum: Optional[torch.Tensor] = None, grad_h: Optional[torch.Tensor] = None,
+                         grad_weight: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None,
+                         workspace: Optional[torch.Tensor] = None):
+    """(grad_h, grad_weight): h and rstd are cc_rms_norm's sum and rstd, grad_sum the gradient that reaches the sum past the norm.
+    grad_h, the gradient of x and of residual alike, may be grad_out or grad_sum itself.  grad_weight (None without a weight) is of
+    the weight's type if made here, float32 or the weight's type if the caller's; with accumulate it is added to the caller's."""
+    shape, dtype, device = h.shape, h.dtype, h.device
+    code = _dtype(h, "h")
+    if not shape:
+        raise ValueError("h must be [..., D]")
+    d = shape[-1]
+    n = h.numel() // d if d else 0
+    h_at, grad_at = _rows(h, shape, dtype, "h"), _rows(grad_out, shape, dtype, "grad_out")
+    sum_at = _NOWHERE if grad_sum is None else _rows(grad_sum, shape, dtype, "grad_sum")
+    grad_h, grad_h_to = _rows_new(grad_h, shape, dtype, device, stream, "grad_h")
+    to, to_code, held, ws, nbytes = None, code, None, None, 0
+    if weight is None:
+        if grad_weight is not None:
+            raise ValueError("grad_weight goes with a weight")
+    else:
+        if grad_weight is None:
+            if accumulate:
+                raise ValueError("accumulate needs a grad_weight to add to")
+            grad_weight = _new((d,), weight.dtype, device, stream)
+        to, to_code = _plain(grad_weight, (d,), grad_weight.dtype, "grad_weight"), _dtype(grad_weight, "grad_weight")
+        held, ws, nbytes = _workspace(workspace, _norm_bytes(n, d), device, stream)
+    _check(lib().cc_rms_norm_backward(*grad_at, *h_at, code, n, d, *_weight(weight, d, dtype, "weight"),
+                                      _plain(rstd, shape[:-1], torch.float32, "rstd"), *sum_at, *grad_h_to, to, to_code,
+                                      1 if accumulate else 0, ws, nbytes, _stream(stream)), "cc_rms_norm_backward")
+    return grad_h, grad_weight
+
+
+def cc_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, stream=None):
+    """(q int8 [..., D], scale float32 [...]) of x [..., D]: about q * scale."""
+    shape, code = x.shape, _dtype(x, "x")
+    if not shape:
+        raise ValueError("x must be [..., D]")
+    d = shape[-1]
+    x_at = _rows(x, shape, x.dtype, "x")
+    q, q_to = _rows_new(q, shape, torch.int8, x.device, stream, "q")
+    scale, scale_to = _plain_out(scale, shape[:-1], torch.float32, x.device, stream, "scale")
+    _check(lib().cc_quantize_rows(*x_at, code, x.numel() // d if d else 0, d, *q_to, scale_to, _stream(stream)), "cc_quantize_rows")
+    return q, scale
+
+
+def cc_product_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                  dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None,
+                  workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [..., K] times the rows of w [N, K], both int8, with a scale for each row of x and of w: [..., N] of type dtype, or of
+    out's if that is given.  bias: float32 [N]."""
+    if w.dim() != 2 or not x.shape:
+        raise ValueError("x must be [..., K] and w [N, K]")
+    shape, (n, k) = x.shape, w.shape
+    if shape[-1] != k:
+        raise ValueError("x and w must have rows of one length")
+    lead = shape[:-1]
+    if out is not None:
+        dtype = out.dtype
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError("dtype must be float32, float16 or bfloat16")
+    x_at, w_at = _rows(x, shape, torch.int8, "x"), _rows(w, (n, k), torch.int8, "w")
+    m = lead.numel()
+    out, out_to = _rows_new(out, (*lead, n), dtype, x.device, stream, "out")
+    L = lib()
+    held, ws, nbytes = _workspace(workspace, _product_bytes(m, n, k), x.device, stream)
+    _check(L.cc_product_i8(*x_at, _plain(x_scale, lead, torch.float32, "x_scale"), *w_at, _plain(w_scale, (n,), torch.float32, "w_scale"),
+                           _plain(bias, (n,), torch.float32, "bias"), m, n, k, *out_to, code, ws, nbytes, _stream(stream)),
+           "cc_product_i8")
+    return out
+
+
+# -------------------------------------------------------------------------------------------------------- shaped logits
+
+
+def _shape_args(logits: torch.Tensor, history, lengths, penalties, starts, bias, allowed):
+    """The arguments that cc_shape_logits and its gradient share."""
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, T, V]")
+    shape, code = logits.shape, _dtype(logits, "logits")
+    b, t, v = shape
+    where, sb, st = _strided(logits, shape, logits.dtype, "logits")
+    history_at, length, apart = None, 0, 0
+    if history is not None:
+        if history.dim() != 2 or history.shape[0] != b:
+            raise ValueError("history must be [B, L]")
+        if t == 1 and lengths is None:
+            raise ValueError("a single position's history needs lengths")
+        length = history.shape[1]
+        history_at, apart = _strided(history, (b, length), torch.int32, "history")
+    bias_at, bias_apart = None, 0
+    if bias is not None:
+        if bias.shape == (v,):
+            bias_at = _plain(bias, (v,), torch.float32, "bias")
+        else:
+            bias_at, bias_apart = _strided(bias, (b, v), torch.float32, "bias")
+    allowed_at = (None, 0, 0)
+    if allowed is not None:
+        allowed_at = _strided(allowed, (b, t, (v + 31) // 32), torch.int32, "allowed")
+    return (where, code, b, t, v, sb, st, history_at, length, apart, _plain(lengths, (b,), torch.int32, "lengths"),
+            _plain(starts, (b,), torch.int32, "starts"), _plain(penalties, (b, 3), torch.float32, "penalties"), bias_at, bias_apart,
+            *allowed_at)
+
+
+def cc_shape_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                    penalties: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                    allowed: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Logits [B, T, V] with penalties float32 [B, 3] (repetition, presence, frequency) on the tokens of history int32 [B, L] that a row
+    looks back on, bias float32 [V] or [B, V], and allowed int32 [B, T, ceil(V / 32)], a bit for each token.  Row t looks
+    back on the first lengths[b] + t entries; without lengths on the first t, as when the history is the orders themselves.
+    `out` may be the logits."""
+    args = _shape_args(logits, history, lengths, penalties, starts, bias, allowed)
+    out, to = _rows_out(out, logits.shape, logits.dtype, logits.device, stream, "out")
+    _check(lib().cc_shape_logits(*args, *to, _stream(stream)), "cc_shape_logits")
+    return out
+
+
+def cc_shape_logits_backward(grad_out: torch.Tensor, logits: torch.Tensor, history: Optional[torch.Tensor] = None,
+                             lengths: Optional[torch.Tensor] = None, penalties: Optional[torch.Tensor] = None,
+                             starts: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                             allowed: Optional[torch.Tensor] = None, grad_logits: Optional[torch.Tensor] = None,
+                             stream=None) -> torch.Tensor:
+    """The gradient of the logits from that of cc_shape_logits's result, whose arguments the others are.  `grad_logits` may be
+    grad_out."""
+    args = _shape_args(logits, history, lengths, penalties, starts, bias, allowed)
+    grad_logits, to = _rows_out(grad_logits, logits.shape, logits.dtype, logits.device, stream, "grad_logits")
+    _check(lib().cc_shape_logits_backward(*_strided(grad_out, logits.shape, logits.dtype, "grad_out"), *args, *to, _stream(stream)),
+           "cc_shape_logits_backward")
+    return grad_logits
