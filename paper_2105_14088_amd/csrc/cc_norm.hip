@@ -24,14 +24,15 @@ namespace {
 
 using namespace ccm;
 
-constexpr int kBlock = 256;              // threads of a workgroup whose teams are smaller than it
+constexpr int kBlock = 256;              // threads of a workgroup of several teams
+constexpr int threads_of(int team) { return team > 64 ? team : kBlock; }
 constexpr int kLongBlock = 1024;
 
 struct Args {
     const void *x, *residual, *weight;   // residual and weight may be null
     int64_t n, x_stride, residual_stride, sum_stride, out_stride, q_stride;
     int D;
-    double eps;
+    double eps, per_element;             // 1 / D
     void *sum, *out;                     // either may be null
     int8_t* q;
     float *scale, *rstd;
@@ -50,6 +51,9 @@ struct Sum64 {
 };
 struct Max64 {
     __device__ __forceinline__ double operator()(double a, double b) const { return __builtin_fmax(a, b); }
+};
+struct MaxBits {
+    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
 };
 template <int BIT>
 __device__ __forceinline__ double other_lane64(double v) {
@@ -81,39 +85,67 @@ __device__ __forceinline__ double group_reduce64(double v, Op op) {
 }
 // Over a team.  One of several wavefronts is the whole workgroup and uses LDS; `slot` alternates between calls, so that one barrier
 // a call is enough: a wavefront that is a call ahead writes elsewhere.
-template <int TEAM, class Op>
-__device__ __forceinline__ double team_reduce(double v, Op op, double (*lds)[TEAM > 64 ? TEAM / 64 : 1], int slot) {
-    if constexpr (TEAM <= 64) {
-        return group_reduce64<TEAM>(v, op);
-    } else {
-        v = group_reduce64<64>(v, op);
-        if (threadIdx.x % 64 == 0) lds[slot][threadIdx.x / 64] = v;
+template <int TEAM, class V, class Op>
+__device__ __forceinline__ V team_reduce(V v, Op op, double (*lds)[TEAM > 64 ? TEAM / 64 : 1], int slot) {
+    constexpr int G = TEAM < 64 ? TEAM : 64;
+    if constexpr (sizeof(V) == 8) v = group_reduce64<G>(v, op);
+    else v = group_reduce<G>(v, op);
+    if constexpr (TEAM > 64) {
+        V* const to = (V*)lds[slot];
+        if (threadIdx.x % 64 == 0) to[threadIdx.x / 64] = v;
         __syncthreads();
-        v = lds[slot][0];
+        v = to[0];
 #pragma unroll
-        for (int i = 1; i < TEAM / 64; ++i) v = op(v, lds[slot][i]);
-        return v;
+        for (int i = 1; i < TEAM / 64; ++i) v = op(v, to[i]);
     }
+    return v;
 }
 
-// What a row's sums say about it.  `check` is the sum of 0 u: undefined if an element of u is infinite or undefined.
+// 1 / sqrt(v) to some 2^-44: the instruction's 2^-23, made better in one step.
+__device__ __forceinline__ double inverse_root(double v) {
+    const double y = __builtin_amdgcn_rsq(v), e = __builtin_fma(-v * y, y, 1.0);
+    return v == __builtin_inf() ? 0.0 : __builtin_fma(y * e, 0.5 + 0.375 * e, y);
+}
+
+// What a row's largest element says about it.
 struct RowScale {
     double most;                         // 0: nothing to divide by
-    float inverse;                       // 127 / most, where 32 bits hold it
+    float inverse;                       // 127 / most, or NaN where 32 bits might not hold it or its products
     bool defined;
-    __device__ __forceinline__ RowScale(double largest, double check) : most(largest), inverse((float)(127.0 / largest)), defined(check == 0.0) {}
+    __device__ __forceinline__ RowScale(double largest, bool finite) : most(largest), defined(finite) {
+        const float m = (float)largest;
+        inverse = finite && m > 0x1p-100f && m < 0x1p100f ? 127.0f * __builtin_amdgcn_rcpf(m) : __builtin_nanf("");
+    }
     // s: what the row was not multiplied by
-    __device__ __forceinline__ float scale(double s) const { return defined ? (float)(most * s / 127.0) : __builtin_nanf(""); }
-    // The whole number nearest to 127 u / most, ties to even.  In 32 bits the quotient is off by less than 127 * 2^-22 (u,
-    // the inverse and their product are rounded); where that reaches a border, and where 32 bits do not hold
-    // the inverse, it is taken in 64.
-    template <class U>
-    __device__ __forceinline__ int nearest(float u, U exact) const {
-        if (!defined || most == 0.0) return 0;
-        const float t = u * inverse;
-        float r = __builtin_rintf(t);
-        if (!(__builtin_fabsf(t - r) < 0.4999f)) r = (float)__builtin_rint(127.0 * exact() / most);
-        return (int)r;
+    __device__ __forceinline__ float scale(double s) const { return defined ? (float)(most * s * (1.0 / 127.0)) : __builtin_nanf(""); }
+    // The whole numbers nearest to 127 u / most, ties to even.  In 32 bits a quotient is off by at most 127 * 6 * 2^-24 = 2^-14.4 (u, most, its
+    // reciprocal, 127 times that and the product are rounded, the reciprocal to a whole step).  Where that reaches a border, what 127 u has
+    // beyond r most says on which side of it the quotient lies: one operation, exact as long as 127 u is, in 64 bits or, where u has at most
+    // 16 (R is float then: 127 u and r most have 23, and no bit of either lies below 2^-24 most unless r = 0), in 32.  An element of some
+    // 5000 is so near; of bf16 ones one of 500, since half of the largest is a border, and then half of all
+    // vectors have one (65536 x 1024: 49 us with a division in 64 bits there, 43 with this in 64, 38 in 32).
+    template <class R, int N, class Exact>
+    __device__ __forceinline__ void nearest(const float (&u)[N], Exact exact, int (&q)[N]) const {
+        float worst = 0.0f, r[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float t = u[i] * inverse;
+            r[i] = __builtin_rintf(t);
+            worst = fmaxf(worst, __builtin_fabsf(t - r[i]));
+        }
+        if (__ballot(inverse != inverse) != 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) r[i] = defined && most > 0.0 ? (float)__builtin_rint(127.0 * exact(i) / most) : 0.0f;
+        } else if (__ballot(!(worst < 0.4999f)) != 0) {
+            const R m = (R)most, half = (R)0.5 * m;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const R top = (R)127 * (R)exact(i), beyond = __builtin_elementwise_fma(-(R)r[i], m, top), size = __builtin_elementwise_abs(beyond);
+                if (size > half || (size == half && ((int)r[i] & 1))) r[i] += beyond > (R)0 ? 1.0f : -1.0f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[i] = (int)r[i];
     }
 };
 
@@ -146,19 +178,47 @@ __device__ __forceinline__ Pack<W, VEC> weights(const void* weight, int64_t at) 
     return Pack<W, VEC>::from(one);
 }
 
-// A row's sums over some of its elements, from the element `skip` on.
-template <bool NORM, bool QUANT, class S, class W, int VEC>
-__device__ __forceinline__ void add_sums(const Pack<S, VEC>& h, const Pack<W, VEC>& w, int skip, double& squares, double& most, double& check) {
+// What is found out about a row on the way through it.
+template <bool NORM, bool QUANT>
+struct Sums {
+    double squares = 0.0;                // of h: neither infinite nor undefined as long as no element is
+    double most = 0.0;                   // |u|: a product of finite 32-bit elements is finite in 64
+    uint32_t bits = 0;                   // without a norm: the largest |x| by its bits, which infinite and undefined ones exceed
+    // Some elements; those before `skip` have been added by another thread.
+    template <class S, class W, int VEC>
+    __device__ __forceinline__ void add(const Pack<S, VEC>& h, const Pack<W, VEC>& w, int skip) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        const double v = (double)h.get(i);
-        if constexpr (NORM) squares = __builtin_fma(i < skip ? 0.0 : v, v, squares);
-        if constexpr (QUANT) {
-            const double u = NORM ? v * (double)w.get(i) : v;
-            most = __builtin_fmax(most, __builtin_fabs(u));
-            check = __builtin_fma(u, 0.0, check);
+        for (int i = 0; i < VEC; ++i) {
+            if constexpr (NORM) {
+                const double v = (double)h.get(i);
+                squares = __builtin_fma(i < skip ? 0.0 : v, v, squares);
+                if constexpr (QUANT) most = __builtin_fmax(most, __builtin_fabs(v * (double)w.get(i)));
+            } else {
+                bits = max(bits, __builtin_bit_cast(uint32_t, h.get(i)) & 0x7fffffffu);
+            }
         }
     }
+    // The row's factor and scale, once all threads of a team have added theirs.
+    template <int TEAM>
+    __device__ __forceinline__ RowScale joined(const Args& a, double (*lds)[TEAM > 64 ? TEAM / 64 : 1], int slot, double& s) {
+        s = 1.0;
+        if constexpr (NORM) {
+            squares = team_reduce<TEAM>(squares, Sum64(), lds, slot);
+            s = inverse_root(__builtin_fma(squares, a.per_element, a.eps));
+            if constexpr (QUANT) most = team_reduce<TEAM>(most, Max64(), lds, 2 + slot);
+            return RowScale(most, squares < __builtin_inf() && most < __builtin_inf());
+        } else {
+            bits = team_reduce<TEAM>(bits, MaxBits(), lds, slot);
+            return RowScale((double)__builtin_bit_cast(float, bits), bits < 0x7f800000u);
+        }
+    }
+};
+template <class W, int VEC>
+__device__ __forceinline__ bool finite(const Pack<W, VEC>& w) {
+    bool all = true;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) all = all && __builtin_fabsf(w.get(i)) < __builtin_inff();
+    return all;
 }
 template <bool NORM, bool QUANT, class S, class W, int VEC>
 __device__ __forceinline__ void store_row(const Args& a, int64_t row, int at, const Pack<S, VEC>& h, const Pack<W, VEC>& w, float s,
@@ -174,69 +234,78 @@ __device__ __forceinline__ void store_row(const Args& a, int64_t row, int at, co
     }
     if constexpr (QUANT) {
         int q[VEC];
+        float u[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float v = h.get(i), f = w.get(i);
-            q[i] = r.nearest(NORM ? v * f : v, [=] { return NORM ? (double)v * (double)f : (double)v; });
-        }
+        for (int i = 0; i < VEC; ++i) u[i] = NORM ? h.get(i) * w.get(i) : h.get(i);
+        using R = std::conditional_t<(sizeof(S) == 2 && !NORM) || (std::is_same_v<S, __bf16> && std::is_same_v<W, __bf16>), float, double>;
+        r.template nearest<R>(u, [&](int i) { return NORM ? (double)h.get(i) * (double)w.get(i) : (double)h.get(i); }, q);
         store_bytes(a.q + row * a.q_stride + at, q);
     }
 }
 
-// A team per row.  A thread holds K vectors of VEC elements; a vector that would end beyond the row is moved back to end
-// with it, and the elements that it then shares with the one before have no second part in the sum of squares.
-// Everything is stored behind the row's sums: by then all of the row has been read, and the sum may be stored where x was.
-template <class S, class W, int VEC, int TEAM, int K, bool NORM, bool QUANT>
-__global__ __launch_bounds__(TEAM > kBlock ? TEAM : kBlock) void norm_kernel(const Args a) {
-    constexpr int TEAMS = TEAM > kBlock ? 1 : kBlock / TEAM;
-    __shared__ double lds[2 * (1 + QUANT * 2)][TEAM > 64 ? TEAM / 64 : 1];
-    const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+// Where a thread's vectors of a row lie.  One that would end beyond the row is moved back to end with it: its first `skip` elements are
+// another's too.  All are loaded, at any length, so that a row's loads are in flight together; one that has no elements of its own
+// (skip = VEC) is not stored.
+template <int VEC, int TEAM, int K>
+struct Place {
     int at[K], skip[K];
-    Pack<W, VEC> w[K];
+    bool uneven[K];                      // of the wavefront: some lane has elements to skip
+    __device__ __forceinline__ Place(int lane, int D) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int i = (k * TEAM + lane) * VEC;
-        at[k] = i < a.D ? min(i, a.D - VEC) : -1;
-        skip[k] = i - at[k];
-        if constexpr (NORM) w[k] = at[k] >= 0 ? weights<W, VEC>(a.weight, at[k]) : Pack<W, VEC>();
+        for (int k = 0; k < K; ++k) {
+            const int i = (k * TEAM + lane) * VEC;
+            at[k] = min(i, D - VEC);
+            skip[k] = min(i - at[k], VEC);
+            uneven[k] = __ballot(skip[k] > 0) != 0;
+        }
+    }
+};
+
+// A team per row.  A thread holds K vectors of VEC elements.  Everything is stored behind the row's
+// sums: by then all of the row has been read, and the sum may be stored where x was.  A team without a row of its own reads the last
+// one and drops it.
+template <class S, class W, int VEC, int TEAM, int K, bool NORM, bool QUANT>
+__global__ __launch_bounds__(threads_of(TEAM)) void norm_kernel(const Args a) {
+    constexpr int TEAMS = threads_of(TEAM) / TEAM;
+    __shared__ double lds[NORM && QUANT ? 4 : 2][TEAM > 64 ? TEAM / 64 : 1];
+    const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+    Place<VEC, TEAM, K> place(lane, a.D);
+    Pack<W, VEC> w[K];
+    if constexpr (NORM) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) w[k] = weights<W, VEC>(a.weight, place.at[k]);
+    }
+    double least = 0.0;                  // an undefined weight makes every row's largest element infinite
+    if constexpr (NORM && QUANT) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (!finite(w[k])) least = __builtin_inf();
     }
     int slot = 0;
     for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.n; first += (int64_t)gridDim.x * TEAMS, slot ^= 1) {
         const int64_t row = first + team;
         const bool live = row < a.n;
+        const int64_t from = live ? row : a.n - 1;
         Pack<S, VEC> h[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            h[k] = Pack<S, VEC>();
-            if (live && at[k] >= 0) h[k] = load_pack<VEC>((const S*)a.x + row * a.x_stride + at[k]);
-        }
+        for (int k = 0; k < K; ++k) h[k] = load_pack<VEC>((const S*)a.x + from * a.x_stride + place.at[k]);
         if constexpr (NORM)
             if (a.residual) {
                 Pack<S, VEC> p[K];
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    p[k] = Pack<S, VEC>();
-                    if (live && at[k] >= 0) p[k] = load_pack<VEC>((const S*)a.residual + row * a.residual_stride + at[k]);
-                }
+                for (int k = 0; k < K; ++k) p[k] = load_pack<VEC>((const S*)a.residual + from * a.residual_stride + place.at[k]);
 #pragma unroll
                 for (int k = 0; k < K; ++k) h[k] = added(h[k], p[k]);
             }
-        double squares = 0, most = 0, check = 0;
+        Sums<NORM, QUANT> sums;
+        sums.most = least;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (at[k] >= 0 && skip[k] > 0) add_sums<NORM, QUANT>(h[k], w[k], skip[k], squares, most, check);
-            else add_sums<NORM, QUANT>(h[k], w[k], 0, squares, most, check);
+            if (place.uneven[k]) sums.add(h[k], w[k], place.skip[k]);
+            else sums.add(h[k], w[k], 0);
         }
-        double s = 1.0;
-        if constexpr (NORM) {
-            squares = team_reduce<TEAM>(squares, Sum64(), lds, slot);
-            s = 1.0 / __builtin_sqrt(squares / a.D + a.eps);
-        }
-        if constexpr (QUANT) {
-            most = team_reduce<TEAM>(most, Max64(), lds, 2 + slot);
-            check = team_reduce<TEAM>(check, Sum64(), lds, 4 + slot);
-        }
-        const RowScale r(most, check);
+        double s;
+        const RowScale r = sums.template joined<TEAM>(a, lds, slot, s);
         if (live) {
             if (lane == 0) {
                 if constexpr (QUANT) a.scale[row] = r.scale(s);
@@ -245,7 +314,7 @@ __global__ __launch_bounds__(TEAM > kBlock ? TEAM : kBlock) void norm_kernel(con
             }
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (at[k] >= 0) store_row<NORM, QUANT>(a, row, at[k], h[k], w[k], (float)s, r);
+                if (place.skip[k] < VEC) store_row<NORM, QUANT>(a, row, place.at[k], h[k], w[k], (float)s, r);
         }
     }
 }
@@ -254,7 +323,7 @@ __global__ __launch_bounds__(TEAM > kBlock ? TEAM : kBlock) void norm_kernel(con
 // as the sum may be stored where x was.
 template <class S, class W, int VEC, bool NORM, bool QUANT>
 __global__ __launch_bounds__(kLongBlock) void norm_long_kernel(const Args a) {
-    __shared__ double lds[2 * (1 + QUANT * 2)][kLongBlock / 64];
+    __shared__ double lds[NORM && QUANT ? 4 : 2][kLongBlock / 64];
     const int whole = a.D - a.D % VEC;
     int slot = 0;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x, slot ^= 1) {
@@ -269,21 +338,16 @@ __global__ __launch_bounds__(kLongBlock) void norm_long_kernel(const Args a) {
             for (int at = threadIdx.x * VEC; at < whole; at += kLongBlock * VEC) body(std::integral_constant<int, VEC>(), at);
             for (int at = whole + threadIdx.x; at < a.D; at += kLongBlock) body(std::integral_constant<int, 1>(), at);
         };
-        double squares = 0, most = 0, check = 0;
+        Sums<NORM, QUANT> sums;
         each([&](auto width, int at) {
             constexpr int N = decltype(width)::value;
-            add_sums<NORM, QUANT>(take(width, at), weights<W, N>(a.weight, at), 0, squares, most, check);
+            const auto w = weights<W, N>(a.weight, at);
+            sums.add(take(width, at), w, 0);
+            if constexpr (NORM && QUANT)
+                if (!finite(w)) sums.most = __builtin_inf();
         });
-        double s = 1.0;
-        if constexpr (NORM) {
-            squares = team_reduce<kLongBlock>(squares, Sum64(), lds, slot);
-            s = 1.0 / __builtin_sqrt(squares / a.D + a.eps);
-        }
-        if constexpr (QUANT) {
-            most = team_reduce<kLongBlock>(most, Max64(), lds, 2 + slot);
-            check = team_reduce<kLongBlock>(check, Sum64(), lds, 4 + slot);
-        }
-        const RowScale r(most, check);
+        double s;
+        const RowScale r = sums.template joined<kLongBlock>(a, lds, slot, s);
         if (threadIdx.x == 0) {
             if constexpr (QUANT) a.scale[row] = r.scale(s);
             if constexpr (NORM)
@@ -299,20 +363,17 @@ __global__ __launch_bounds__(kLongBlock) void norm_long_kernel(const Args a) {
 // The gradient of a row, by a team as above.  Where there is a gradient of weights, a thread sums its columns over the team's rows,
 // then a workgroup's teams are added in their order; norm_weight_kernel adds the workgroups.
 template <class S, class W, int VEC, int TEAM, int K>
-__global__ __launch_bounds__(TEAM > kBlock ? TEAM : kBlock) void norm_backward_kernel(const GradArgs a) {
-    constexpr int TEAMS = TEAM > kBlock ? 1 : kBlock / TEAM, COLUMNS = TEAM * K * VEC;
+__global__ __launch_bounds__(threads_of(TEAM)) void norm_backward_kernel(const GradArgs a) {
+    constexpr int TEAMS = threads_of(TEAM) / TEAM, COLUMNS = TEAM * K * VEC;
     __shared__ double lds[2][TEAM > 64 ? TEAM / 64 : 1];
     __shared__ float sums[TEAMS > 1 ? TEAMS * COLUMNS : 1];
     const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    int at[K], skip[K];
+    const Place<VEC, TEAM, K> place(lane, a.D);
     Pack<W, VEC> w[K];
     float dw[K][VEC];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int i = (k * TEAM + lane) * VEC;
-        at[k] = i < a.D ? min(i, a.D - VEC) : -1;
-        skip[k] = i - at[k];
-        w[k] = at[k] >= 0 ? weights<W, VEC>(a.weight, at[k]) : Pack<W, VEC>();
+        w[k] = weights<W, VEC>(a.weight, place.at[k]);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dw[k][i] = 0.0f;
     }
@@ -320,42 +381,44 @@ __global__ __launch_bounds__(TEAM > kBlock ? TEAM : kBlock) void norm_backward_k
     for (int64_t first = (int64_t)blockIdx.x * TEAMS; first < a.n; first += (int64_t)gridDim.x * TEAMS, slot ^= 1) {
         const int64_t row = first + team;
         const bool live = row < a.n;
-        const float s = live ? a.rstd[row] : 0.0f;
+        const int64_t from = live ? row : a.n - 1;
+        const float s = a.rstd[from];
         Pack<S, VEC> h[K], g[K], more[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            h[k] = Pack<S, VEC>();
-            g[k] = Pack<S, VEC>();
+            h[k] = load_pack<VEC>((const S*)a.h + from * a.h_stride + place.at[k]);
+            g[k] = load_pack<VEC>((const S*)a.grad + from * a.grad_stride + place.at[k]);
             more[k] = Pack<S, VEC>();
-            if (live && at[k] >= 0) {
-                h[k] = load_pack<VEC>((const S*)a.h + row * a.h_stride + at[k]);
-                g[k] = load_pack<VEC>((const S*)a.grad + row * a.grad_stride + at[k]);
-                if (a.grad_sum) more[k] = load_pack<VEC>((const S*)a.grad_sum + row * a.grad_sum_stride + at[k]);
-            }
+        }
+        if (a.grad_sum) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) more[k] = load_pack<VEC>((const S*)a.grad_sum + from * a.grad_sum_stride + place.at[k]);
         }
         float along = 0.0f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float part = 0.0f, shared = 0.0f;
+            float part = 0.0f;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float normed = h[k].get(i) * s, term = g[k].get(i) * normed;
+                const float normed = h[k].get(i) * s;
+                float term = g[k].get(i) * normed;
+                if (!live) term = 0.0f;
                 dw[k][i] += term;
+                if (place.uneven[k] && i < place.skip[k]) term = 0.0f;
                 part = __builtin_fmaf(term, w[k].get(i), part);
-                if (at[k] >= 0 && i < skip[k]) shared = __builtin_fmaf(term, w[k].get(i), shared);
             }
-            along += part - shared;
+            along += part;
         }
         const float mean = (float)(team_reduce<TEAM>((double)along, Sum64(), lds, slot) / a.D);
         if (live) {
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (at[k] >= 0) {
+                if (place.skip[k] < VEC) {
                     float f[VEC];
 #pragma unroll
                     for (int i = 0; i < VEC; ++i)
                         f[i] = __builtin_fmaf(s, __builtin_fmaf(-h[k].get(i) * s, mean, g[k].get(i) * w[k].get(i)), more[k].get(i));
-                    store_pack((S*)a.grad_h + row * a.grad_h_stride + at[k], Pack<S, VEC>::from(f));
+                    store_pack((S*)a.grad_h + row * a.grad_h_stride + place.at[k], Pack<S, VEC>::from(f));
                 }
         }
     }
@@ -364,7 +427,7 @@ __global__ __launch_bounds__(TEAM > kBlock ? TEAM : kBlock) void norm_backward_k
     if constexpr (TEAMS > 1) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (at[k] >= 0) __builtin_memcpy(&sums[team * COLUMNS + (k * TEAM + lane) * VEC], dw[k], sizeof(dw[k]));
+            if (place.skip[k] < VEC) __builtin_memcpy(&sums[team * COLUMNS + (k * TEAM + lane) * VEC], dw[k], sizeof(dw[k]));
         __syncthreads();
         // the last vector's place holds the row's last VEC columns, wherever they begin
         const int last = (a.D - 1) / VEC;
@@ -378,7 +441,7 @@ __global__ __launch_bounds__(TEAM > kBlock ? TEAM : kBlock) void norm_backward_k
         // columns that two threads hold have the same sum in both
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (at[k] >= 0) __builtin_memcpy(to + at[k], dw[k], sizeof(dw[k]));
+            if (place.skip[k] < VEC) __builtin_memcpy(to + place.at[k], dw[k], sizeof(dw[k]));
     }
 }
 
@@ -420,30 +483,61 @@ __global__ __launch_bounds__(kLongBlock) void norm_backward_long_kernel(const Gr
     }
 }
 
-// The weights' gradient of such rows, before grad_h is stored where grad_out may be: a thread has a column of some rows.
+// The weights' gradient of such rows, before grad_h is stored where grad_out may be: a thread has 4 columns of some rows.  The last
+// thread's are moved back to end with the row; the columns that it shares have the same sums in both.
 template <class S>
 __global__ __launch_bounds__(kBlock) void norm_columns_kernel(const GradArgs a, int64_t rows) {
-    const int j = blockIdx.x * kBlock + threadIdx.x;
+    constexpr int N = 4, U = 4;
+    int j = (blockIdx.x * kBlock + threadIdx.x) * N;
     if (j >= a.D) return;
+    j = min(j, a.D - N);
     const int64_t first = (int64_t)blockIdx.y * rows, end = min(first + rows, a.n);
-    float sum = 0.0f;
-    for (int64_t row = first; row < end; ++row)
-        sum += widen(((const S*)a.grad)[row * a.grad_stride + j]) * (widen(((const S*)a.h)[row * a.h_stride + j]) * a.rstd[row]);
-    a.partial[(int64_t)blockIdx.y * a.D + j] = sum;
+    float sum[N] = {};
+    for (int64_t row = first; row < end; row += U) {
+        Pack<S, N> g[U], h[U];
+        float s[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = min(row + u, end - 1);
+            g[u] = load_pack<N>((const S*)a.grad + r * a.grad_stride + j);
+            h[u] = load_pack<N>((const S*)a.h + r * a.h_stride + j);
+            s[u] = a.rstd[r];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (row + u < end) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += g[u].get(i) * (h[u].get(i) * s[u]);
+            }
+    }
+    __builtin_memcpy(a.partial + (int64_t)blockIdx.y * a.D + j, sum, sizeof(sum));
 }
 
-// grad_weight[j] = the sum of `count` partial sums: 64 columns a workgroup, its wavefronts share the sums and are added in order.
+// grad_weight[j] = the sum of `count` partial sums.  16 columns a workgroup; 64 groups of 16 lanes take the sums in turn, eight loads
+// in flight each, and are added in a fixed order.
 template <class W>
 __global__ __launch_bounds__(1024) void norm_weight_kernel(const float* __restrict__ partial, int count, int D, W* grad_weight, int accumulate) {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, j = blockIdx.x * 64 + lane;
+    __shared__ float lds[16][16];
+    const int in = threadIdx.x % 16, group = threadIdx.x / 16, j = blockIdx.x * 16 + in;
     float sum = 0.0f;
-    if (j < D)
-        for (int i = wave; i < count; i += 16) sum += partial[(int64_t)i * D + j];
-    lds[wave][lane] = sum;
+    if (j < D) {
+        int i = group;
+        for (; i + 7 * 64 < count; i += 8 * 64) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = partial[(int64_t)(i + u * 64) * D + j];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += v[u];
+        }
+        for (; i < count; i += 64) sum += partial[(int64_t)i * D + j];
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (threadIdx.x % 64 < 16) lds[threadIdx.x / 64][in] = sum;
     __syncthreads();
-    if (wave == 0 && j < D) {
-        for (int i = 1; i < 16; ++i) sum += lds[i][lane];
+    if (threadIdx.x < 16 && j < D) {
+        sum = lds[0][in];
+        for (int i = 1; i < 16; ++i) sum += lds[i][in];
         if (accumulate) sum += widen(grad_weight[j]);
         grad_weight[j] = narrow<W>(sum);
     }
@@ -467,11 +561,18 @@ void by_length(int64_t D, F f) {
     CC_TEAM(32, 1);
     CC_TEAM(64, 1);
     CC_TEAM(64, 2);
-    CC_TEAM(64, 4);
-    CC_TEAM(256, 2);
-    CC_TEAM(256, 4);
-    CC_TEAM(512, 4);
-    if constexpr (VEC == 4) CC_TEAM(512, 8);
+    if constexpr (VEC == 8) {
+        CC_TEAM(128, 2);
+        CC_TEAM(256, 2);
+        CC_TEAM(512, 2);
+        CC_TEAM(1024, 2);
+    } else {
+        CC_TEAM(64, 4);
+        CC_TEAM(128, 4);
+        CC_TEAM(256, 4);
+        CC_TEAM(512, 4);
+        CC_TEAM(512, 8);
+    }
 #undef CC_TEAM
     f(integral_constant<int, 0>(), integral_constant<int, 0>());
 }
@@ -490,14 +591,14 @@ void launch_rows(const Args& a, hipStream_t s) {
         if constexpr (TEAM == 0) {
             hipLaunchKernelGGL((norm_long_kernel<S, W, VEC, NORM, QUANT>), dim3((unsigned)blocks_for(a.n, 1, kLongBlock)), dim3(kLongBlock), 0, s, a);
         } else {
-            constexpr int threads = TEAM > kBlock ? TEAM : kBlock, teams = threads / TEAM;
+            constexpr int threads = threads_of(TEAM), teams = threads / TEAM;
             hipLaunchKernelGGL((norm_kernel<S, W, VEC, TEAM, K, NORM, QUANT>), dim3((unsigned)blocks_for(a.n, teams, threads)), dim3(threads), 0, s, a);
         }
     });
 }
 
 // Workgroups that sum columns: each leaves a row of partial sums.
-constexpr int64_t kGradBlocks = 1024, kLongParts = 16;
+constexpr int64_t kGradBlocks = 1024, kLongParts = 32;
 int64_t grad_blocks(int64_t n, int teams, int threads) {
     const int64_t need = (n + teams - 1) / teams, most = kGradBlocks * kBlock / threads;
     return need < most ? need : most;
@@ -514,20 +615,21 @@ void launch_backward(GradArgs a, const NormBackwardCall& c, hipStream_t s) {
         by_length<VEC>(a.D, [&](auto team, auto k) {
             constexpr int TEAM = decltype(team)::value, K = decltype(k)::value;
             if constexpr (TEAM == 0) {
-                count = a.n < kLongParts ? a.n : kLongParts;
-                const int64_t rows = (a.n + count - 1) / count;
+                // parts of equal length, none of them empty
+                const int64_t rows = (a.n + kLongParts - 1) / kLongParts, parts = (a.n + rows - 1) / rows;
+                count = parts;
                 if (a.partial)
-                    hipLaunchKernelGGL((norm_columns_kernel<S>), dim3((unsigned)((a.D + kBlock - 1) / kBlock), (unsigned)count), dim3(kBlock), 0, s, a, rows);
+                    hipLaunchKernelGGL((norm_columns_kernel<S>), dim3((unsigned)((a.D + kBlock * 4 - 1) / (kBlock * 4)), (unsigned)parts), dim3(kBlock), 0, s, a, rows);
                 hipLaunchKernelGGL((norm_backward_long_kernel<S, W, VEC>), dim3((unsigned)blocks_for(a.n, 1, kLongBlock)), dim3(kLongBlock), 0, s, a);
             } else {
-                constexpr int threads = TEAM > kBlock ? TEAM : kBlock, teams = threads / TEAM;
+                constexpr int threads = threads_of(TEAM), teams = threads / TEAM;
                 count = grad_blocks(a.n, teams, threads);
                 hipLaunchKernelGGL((norm_backward_kernel<S, W, VEC, TEAM, K>), dim3((unsigned)count), dim3(threads), 0, s, a);
             }
         });
     }
     if (!a.partial) return;
-    const dim3 grid((unsigned)((a.D + 63) / 64));
+    const dim3 grid((unsigned)((a.D + 15) / 16));
     if (c.grad_weight_dtype == kF32)
         hipLaunchKernelGGL((norm_weight_kernel<float>), grid, dim3(1024), 0, s, a.partial, (int)count, a.D, (float*)c.grad_weight, (int)c.accumulate);
     else
@@ -562,6 +664,7 @@ hipError_t launch_norm(const NormCall& c, hipStream_t s) {
     a.q_stride = c.q_stride;
     a.D = (int)c.D;
     a.eps = c.eps;
+    a.per_element = 1.0 / (double)c.D;
     a.sum = c.sum;
     a.out = c.out;
     a.q = c.q;
@@ -589,17 +692,18 @@ hipError_t launch_quantize(const NormCall& c, hipStream_t s) {
     return hipGetLastError();
 }
 
-// A row of partial sums for every workgroup that leaves one: fewer the longer the row, as by_length and grad_blocks have it for
-// the type with the most.
+// A row of partial sums for every workgroup that leaves one: as many as grad_blocks gives for the type with the smaller team.
 size_t norm_workspace_bytes(int64_t n, int64_t D) {
-    const int64_t most = D <= 256 * 4 * 8 ? kGradBlocks : D <= 512 * 4 * 8 ? kGradBlocks * kBlock / 512 : kLongParts;
+    int64_t threads = kBlock;
+    while (threads < 512 && D > threads * 16) threads *= 2;
+    const int64_t most = D > 16384 ? kLongParts : kGradBlocks * kBlock / threads;
     return (size_t)(((n < most ? n : most) * D * 4 + 255) / 256 * 256);
 }
 
 hipError_t launch_norm_backward(const NormBackwardCall& c, hipStream_t s) {
     if (c.n == 0) {
         // nothing to sum: the weights' gradient is cleared
-        const dim3 grid((unsigned)((c.D + 63) / 64));
+        const dim3 grid((unsigned)((c.D + 15) / 16));
         if (c.grad_weight_dtype == kF32)
             hipLaunchKernelGGL((norm_weight_kernel<float>), grid, dim3(1024), 0, s, nullptr, 0, (int)c.D, (float*)c.grad_weight, 0);
         else if (c.grad_weight_dtype == kF16)
