@@ -36,6 +36,7 @@ struct Args {
     int N, K;
     void* out;
     int tiles_m, tiles_n;
+    bool far;                            // rows so far apart that 32 bits do not address a tile's from its first
 };
 
 // 16 bytes of a row from k on; what lies beyond K is zero and not read.
@@ -103,54 +104,53 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 
     // Where this thread's pieces come from: rows beyond the last are the last again, their results are not stored.
     // Piece p of wavefront `wave` fills LDS from (p * THREADS + wave * 64) * 16 on, 8 rows.
-    const int in_row = (lane % 8) ^ ((lane / 8) % 8);
+    const int in_row = (lane % 8) ^ ((wave * 8 + lane / 8) / 2 % 8);
+    static_assert(THREADS / 8 % 16 == 0, "a thread's pieces lie at the same place of their rows");
     const auto row_of = [&](int p) {
         const int row = ((p < XPIECES ? p : p - XPIECES) * THREADS + wave * 64 + lane) / 8;
         return min(row, p < XPIECES ? last_m : last_n);
     };
-    uint32_t from[DIRECT ? PIECES : 1];
-    if constexpr (DIRECT) {
+    uint32_t from[PIECES];
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) from[p] = (uint32_t)row_of(p) * (uint32_t)(p < XPIECES ? a.x_stride : a.w_stride) + in_row * kPiece;
-    }
+    for (int p = 0; p < PIECES; ++p) from[p] = (uint32_t)row_of(p) * (uint32_t)(p < XPIECES ? a.x_stride : a.w_stride) + in_row * kPiece;
     Int4 held[DIRECT ? 1 : PIECES];
-    const auto piece = [&](int p, int tile) {
-        const int8_t* const row = p < XPIECES ? xbase + row_of(p) * a.x_stride : wbase + row_of(p) * a.w_stride;
-        return load_piece(row, tile * kStep + in_row * kPiece, a.K);
-    };
     const auto put = [&](int p, int buffer, const Int4& v) { *(Int4*)(lds + buffer * BYTES + (p * THREADS + thread) * kPiece) = v; };
-    const int tiles = (a.K + kStep - 1) / kStep;
-    const auto fetch = [&](int tile, int buffer) {
-        if (tile >= tiles) return;
+    const int tiles = (a.K + kStep - 1) / kStep, whole = a.far ? 0 : a.K / kStep;
+    // A piece of a tile that has all of its bytes.
+    const auto fetch = [&](int p, int tile, int buffer) {
+        const int8_t* const base = (p < XPIECES ? xbase : wbase) + (int64_t)tile * kStep;
         if constexpr (DIRECT) {
-            if ((tile + 1) * kStep <= a.K) {
-                const int8_t *xk = xbase + (int64_t)tile * kStep, *wk = wbase + (int64_t)tile * kStep;
-                const uint32_t to = (uint32_t)(uintptr_t)(lds + buffer * BYTES) + wave * 1024;
-#pragma unroll
-                for (int p = 0; p < PIECES; ++p)
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                                 :
-                                 : "s"(to + p * THREADS * kPiece), "v"(from[p]), "s"(p < XPIECES ? xk : wk)
-                                 : "memory");
-            } else {
-                // the row's end, once: not unrolled, its addresses would take registers throughout
-#pragma nounroll
-                for (int p = 0; p < PIECES; ++p) put(p, buffer, piece(p, tile));
-            }
+            const uint32_t to = (uint32_t)(uintptr_t)lds + buffer * BYTES + wave * 1024 + p * THREADS * kPiece;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(from[p]), "s"(base) : "memory");
         } else {
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) held[p] = piece(p, tile);
+            __builtin_memcpy(&held[p], base + from[p], kPiece);
+        }
+    };
+    // The last tile, where the rows end inside it, and any tile of rows that are far apart.  Not unrolled: its addresses would take registers
+    // throughout.
+    const auto fetch_end = [&](int tile, int buffer) {
+#pragma nounroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int8_t* const row = p < XPIECES ? xbase + row_of(p) * a.x_stride : wbase + row_of(p) * a.w_stride;
+            put(p, buffer, load_piece(row, tile * kStep + in_row * kPiece, a.K));
         }
     };
     // What was fetched is in LDS, for every wavefront, and nobody reads what lay there before.
     const auto arrive = [&](int tile, int buffer) {
-        if constexpr (!DIRECT) {
-            if (tile < tiles) {
+        if constexpr (!DIRECT)
+            if (tile < whole) {
 #pragma unroll
                 for (int p = 0; p < PIECES; ++p) put(p, buffer, held[p]);
             }
-        }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    const auto fetch_all = [&](int tile, int buffer) {
+        if (tile < whole) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) fetch(p, tile, buffer);
+        } else if (tile < tiles) {
+            fetch_end(tile, buffer);
+        }
     };
 
     Int16 sum[MT][NT];
@@ -160,42 +160,65 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum[i][j][r] = 0;
-    Int4 xf[2][MT], wf[2][NT];
+    Int4 operand[2][MT + NT];
     const char* const xrow = lds + (wm * WM + lane % 32) * kStep;
     const char* const wrow = lds + XBYTES + (wn * WN + lane % 32) * kStep;
-    const auto read = [&](int buffer, int s, int set) {
-        const int at = buffer * BYTES + ((2 * s + lane / 32) ^ (lane % 8)) * kPiece;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) xf[set][i] = *(const Int4*)(xrow + at + i * 32 * kStep);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) wf[set][j] = *(const Int4*)(wrow + at + j * 32 * kStep);
+    // Operand o of a quarter s of a tile, for the next multiplication.
+    const auto read = [&](int o, int buffer, int s) {
+        const int at = buffer * BYTES + ((2 * s + lane / 32) ^ (lane / 2 % 8)) * kPiece;
+        operand[s & 1][o] = *(const Int4*)((o < MT ? xrow + o * 32 * kStep : wrow + (o - MT) * 32 * kStep) + at);
     };
-    const auto multiply = [&](int set) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[set][j], xf[set][i], sum[i][j], 0, 0, 0);
+    // A quarter's products, and between them, in this order, what else is to be issued: a matrix core takes 32 cycles for a product, and a
+    // wavefront has it to itself.
+    constexpr int PRODUCTS = MT * NT;
+    const auto multiply = [&](int set, int q) {
+        const int i = q / NT, j = q % NT;
+        sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(operand[set][MT + j], operand[set][i], sum[i][j], 0, 0, 0);
     };
 
     if (tiles == 0) {
         __syncthreads();
     } else {
-        fetch(0, 0);
+        fetch_all(0, 0);
         arrive(0, 0);
-        fetch(1, 1);
-        read(0, 0, 0);
+        fetch_all(1, 1);
+#pragma unroll
+        for (int o = 0; o < MT + NT; ++o) read(o, 0, 0);
         for (int t = 0; t < tiles; ++t) {
             const int now = t & 1;
-            read(now, 1, 1);
-            multiply(0);
-            read(now, 2, 0);
-            multiply(1);
-            read(now, 3, 1);
-            multiply(0);
+#pragma unroll
+            for (int s = 0; s < 3; ++s)
+#pragma unroll
+                for (int q = 0; q < PRODUCTS; ++q) {
+                    multiply(s & 1, q);
+#pragma unroll
+                    for (int o = 0; o < MT + NT; ++o)
+                        if (o * PRODUCTS / (MT + NT) == q) read(o, now, s + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            // Behind the barrier this tile's place is free.  A quarter of the products goes before it, so that waiting for the others does not
+            // stop the matrix core at once.
+            constexpr int BEFORE = PRODUCTS / 4;
+#pragma unroll
+            for (int q = 0; q < BEFORE; ++q) multiply(1, q);
+            __builtin_amdgcn_sched_barrier(0);
             arrive(t + 1, now ^ 1);
-            fetch(t + 2, now);
-            if (t + 1 < tiles) read(now ^ 1, 0, 0);
-            multiply(1);
+            const bool more = t + 2 < whole;
+#pragma unroll
+            for (int q = BEFORE; q < PRODUCTS; ++q) {
+                multiply(1, q);
+                // read past the last tile too: what is read then is not used
+#pragma unroll
+                for (int o = 0; o < MT + NT; ++o)
+                    if (BEFORE + o * (PRODUCTS - BEFORE) / (MT + NT) == q) read(o, now ^ 1, 0);
+                if (more) {
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p)
+                        if (BEFORE + p * (PRODUCTS - BEFORE) / PIECES == q) fetch(p, t + 2, now);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!more && t + 2 < tiles) fetch_end(t + 2, now);
         }
     }
 
@@ -317,17 +340,14 @@ template <class S, int BM, int BN, int WM, int WN>
 void launch_tiles(Args a, bool direct, hipStream_t s) {
     a.tiles_m = (int)((a.M + BM - 1) / BM);
     a.tiles_n = (a.N + BN - 1) / BN;
+    a.far = a.x_stride >= 1 << 24 || a.w_stride >= 1 << 24;
     const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n)), block((BM / WM) * (BN / WN) * 64);
-    if (direct) {
-        hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, true>), grid, block, 0, s, a);
-    } else if constexpr (BM < 256) {
-        hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, false>), grid, block, 0, s, a);
-    }
+    if (direct) hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, false>), grid, block, 0, s, a);
 }
 
 bool rows_at_16(const void* p, int64_t stride) {
-    // rows of a tile are addressed by 32 bits from its first
-    return ((uintptr_t)p & 15) == 0 && stride % 16 == 0 && stride < (1 << 24);
+    return ((uintptr_t)p & 15) == 0 && stride % 16 == 0;
 }
 
 template <class S>
@@ -342,7 +362,7 @@ void run(const Args& a, hipStream_t s) {
         const dim3 grid((unsigned)((stretches + per - 1) / per));
         if (a.M <= 16) hipLaunchKernelGGL((few_kernel<S, 1>), grid, dim3(kFewWaves * 64), 0, s, a, share);
         else hipLaunchKernelGGL((few_kernel<S, 2>), grid, dim3(kFewWaves * 64), 0, s, a, share);
-    } else if (direct && tiles(256, 256) >= 192) {
+    } else if (tiles(256, 256) >= 192) {
         launch_tiles<S, 256, 256, 128, 128>(a, direct, s);
     } else if (tiles(128, 128) >= 192) {
         launch_tiles<S, 128, 128, 64, 64>(a, direct, s);
