@@ -15,6 +15,8 @@
 // wavefronts share a channel's K where there are few channels.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "cc_internal.h"
 #include "cc_model.h"
 
@@ -36,31 +38,36 @@ struct Args {
     int N, K;
     void* out;
     int tiles_m, tiles_n;
-    bool far;                            // rows so far apart that 32 bits do not address a tile's from its first
 };
 
-// 16 bytes of a row from k on; what lies beyond K is zero and not read.
+// 16 bytes of a row from k on; what lies beyond K is zero and not read.  Where they end beyond the row, its last 16 are read and shifted.
 __device__ __forceinline__ Int4 load_piece(const int8_t* row, int k, int K) {
-    Int4 v = {0, 0, 0, 0};
-    if (k + kPiece <= K) {
-        __builtin_memcpy(&v, row + k, kPiece);
-    } else if (k < K) {
-        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i)
-            if (k + i < K) w[i / 4] |= (uint32_t)(uint8_t)row[k + i] << (8 * (i % 4));
-        v = Int4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+    typedef uint64_t Long2 __attribute__((ext_vector_type(2)));
+    Long2 v = {0, 0};
+    if (K >= kPiece) {
+        const int at = min(k, K - kPiece), beyond = min(k - at, kPiece) * 8;
+        __builtin_memcpy(&v, row + at, kPiece);
+        if (beyond >= 64) v = Long2{v[1], 0};
+        const int shift = beyond & 63;
+        if (beyond == 128) v = Long2{0, 0};
+        else if (shift) v = Long2{v[0] >> shift | v[1] << (64 - shift), v[1] >> shift};
+    } else {
+        for (int i = 0; k + i < K; ++i) {
+            const uint64_t byte = (uint8_t)row[k + i];
+            if (i < 8) v[0] |= byte << (8 * i);
+            else v[1] |= byte << (8 * (i - 8));
+        }
     }
-    return v;
+    return __builtin_bit_cast(Int4, v);
 }
 
 // From the exact sum on in 32 bits: it is rounded, and so is each product and the sum with the bias.
 __device__ __forceinline__ float scaled(int sum, float xs, float ws, float bias) { return (float)sum * xs * ws + bias; }
 
 template <class S>
-__device__ __forceinline__ void store_few(S* p, const S* from, int count) {
-    for (int i = 0; i < count; ++i) p[i] = from[i];
-}
+struct Elements {
+    S v[16 / sizeof(S)];
+};
 
 // Workgroups of one XCD (every eighth) get neighbouring tiles, and those in blocks of 8 rows of tiles, so that what they read at the
 // same time is shared in its L2.
@@ -74,16 +81,23 @@ __device__ __forceinline__ void tile_of(uint32_t id, int tiles_m, int tiles_n, i
     tn = __builtin_amdgcn_readfirstlane((int)(in / rows));
 }
 
-template <class S, int BM, int BN, int WM, int WN, bool DIRECT>
+// How rows come to LDS: straight, through registers, or through registers from addresses that 32 bits do not reach from a tile's first.
+enum RowMode { kRowsDirect, kRowsHeld, kRowsFar };
+
+// RING tiles of the operands are held, so a tile has RING - 1 others' time to arrive.  With more than one workgroup to a tile (gridDim.y) each
+// has a stretch of K, and S is int32: its sums go to a matrix of their own.
+template <class S, int BM, int BN, int WM, int WN, int RING, RowMode MODE>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const Args a) {
     constexpr int THREADS = (BM / WM) * (BN / WN) * 64, WAVES = THREADS / 64;
     constexpr int MT = WM / 32, NT = WN / 32;
     constexpr int XBYTES = BM * kStep, WBYTES = BN * kStep, BYTES = XBYTES + WBYTES;
     constexpr int PIECES = BYTES / (THREADS * kPiece), XPIECES = XBYTES / (THREADS * kPiece);
     static_assert(XBYTES % (THREADS * kPiece) == 0 && WBYTES % (THREADS * kPiece) == 0, "every load of a workgroup is of one operand");
+    static_assert(THREADS / 8 % 16 == 0, "a thread's pieces lie at the same place of their rows");
+    static_assert(MODE == kRowsDirect || RING == 2, "registers hold one tile");
     constexpr int STRIP = WN * (int)sizeof(S) + 16;                 // a row of the result's strip in LDS
-    static_assert(WAVES * 32 * STRIP <= 2 * BYTES, "the strips lie where the operands were");
-    __shared__ __attribute__((aligned(128))) char lds[2 * BYTES];
+    static_assert(WAVES * 32 * STRIP <= RING * BYTES, "the strips lie where the operands were");
+    __shared__ __attribute__((aligned(128))) char lds[RING * BYTES];
     __shared__ __attribute__((aligned(16))) float channel[2][BN];   // scales and biases
 
     const int thread = threadIdx.x, lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64);
@@ -95,71 +109,71 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
     const int8_t* const xbase = a.x + m0 * a.x_stride;
     const int8_t* const wbase = a.w + (int64_t)n0 * a.w_stride;
     const int last_m = (int)min((int64_t)BM, a.M - m0) - 1, last_n = min(BN, a.N - n0) - 1;
-
-    for (int i = thread; i < BN; i += THREADS) {
-        const int n = n0 + min(i, last_n);
-        channel[0][i] = a.w_scale[n];
-        channel[1][i] = a.bias ? a.bias[n] : 0.0f;
-    }
+    if constexpr (!std::is_same_v<S, int32_t>)
+        for (int i = thread; i < BN; i += THREADS) {
+            const int n = n0 + min(i, last_n);
+            channel[0][i] = a.w_scale[n];
+            channel[1][i] = a.bias ? a.bias[n] : 0.0f;
+        }
 
     // Where this thread's pieces come from: rows beyond the last are the last again, their results are not stored.
     // Piece p of wavefront `wave` fills LDS from (p * THREADS + wave * 64) * 16 on, 8 rows.
     const int in_row = (lane % 8) ^ ((wave * 8 + lane / 8) / 2 % 8);
-    static_assert(THREADS / 8 % 16 == 0, "a thread's pieces lie at the same place of their rows");
     const auto row_of = [&](int p) {
         const int row = ((p < XPIECES ? p : p - XPIECES) * THREADS + wave * 64 + lane) / 8;
         return min(row, p < XPIECES ? last_m : last_n);
     };
-    uint32_t from[PIECES];
+    std::conditional_t<MODE == kRowsFar, int64_t, uint32_t> from[PIECES];
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) from[p] = (uint32_t)row_of(p) * (uint32_t)(p < XPIECES ? a.x_stride : a.w_stride) + in_row * kPiece;
-    Int4 held[DIRECT ? 1 : PIECES];
+    for (int p = 0; p < PIECES; ++p)
+        from[p] = (decltype(from[0] + 0))row_of(p) * (decltype(from[0] + 0))(p < XPIECES ? a.x_stride : a.w_stride) + in_row * kPiece;
+    Int4 held[MODE == kRowsDirect ? 1 : PIECES];
     const auto put = [&](int p, int buffer, const Int4& v) { *(Int4*)(lds + buffer * BYTES + (p * THREADS + thread) * kPiece) = v; };
-    const int tiles = (a.K + kStep - 1) / kStep, whole = a.far ? 0 : a.K / kStep;
-    // A piece of a tile that has all of its bytes.
-    const auto fetch = [&](int p, int tile, int buffer) {
-        const int8_t* const base = (p < XPIECES ? xbase : wbase) + (int64_t)tile * kStep;
-        if constexpr (DIRECT) {
+    // The sum does not depend on the order of its terms: where K ends inside a tile, that tile is the first, so that only the start has to
+    // look at where a row ends.
+    const int whole = a.K / kStep, partial = a.K % kStep != 0, all = whole + partial;
+    const int t0 = (int)((int64_t)all * blockIdx.y / gridDim.y), tiles = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y);
+    const auto fetch = [&](int p, int t, int buffer) {
+        const int8_t* const base = (p < XPIECES ? xbase : wbase) + (int64_t)(t - partial) * kStep;
+        if constexpr (MODE == kRowsDirect) {
             const uint32_t to = (uint32_t)(uintptr_t)lds + buffer * BYTES + wave * 1024 + p * THREADS * kPiece;
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(from[p]), "s"(base) : "memory");
         } else {
             __builtin_memcpy(&held[p], base + from[p], kPiece);
         }
     };
-    // The last tile, where the rows end inside it, and any tile of rows that are far apart.  Not unrolled: its addresses would take registers
-    // throughout.
-    const auto fetch_end = [&](int tile, int buffer) {
-#pragma nounroll
-        for (int p = 0; p < PIECES; ++p) {
-            const int8_t* const row = p < XPIECES ? xbase + row_of(p) * a.x_stride : wbase + row_of(p) * a.w_stride;
-            put(p, buffer, load_piece(row, tile * kStep + in_row * kPiece, a.K));
-        }
-    };
-    // What was fetched is in LDS, for every wavefront, and nobody reads what lay there before.
-    const auto arrive = [&](int tile, int buffer) {
-        if constexpr (!DIRECT)
-            if (tile < whole) {
+    const auto fetch_all = [&](int t, int buffer) {
+        if (t >= tiles) return;
 #pragma unroll
-                for (int p = 0; p < PIECES; ++p) put(p, buffer, held[p]);
+        for (int p = 0; p < PIECES; ++p) fetch(p, t, buffer);
+    };
+    const auto fetch_partial = [&] {
+        constexpr int U = PIECES < 8 ? PIECES : 8;
+#pragma unroll
+        for (int p = 0; p < PIECES; p += U) {
+            Int4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int8_t* const row = p + u < XPIECES ? xbase + row_of(p + u) * a.x_stride : wbase + row_of(p + u) * a.w_stride;
+                v[u] = load_piece(row, whole * kStep + in_row * kPiece, a.K);
             }
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    };
-    const auto fetch_all = [&](int tile, int buffer) {
-        if (tile < whole) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) fetch(p, tile, buffer);
-        } else if (tile < tiles) {
-            fetch_end(tile, buffer);
+            for (int u = 0; u < U; ++u) put(p + u, 0, v[u]);
         }
+    };
+    const auto put_held = [&](int buffer) {
+        if constexpr (MODE != kRowsDirect) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) put(p, buffer, held[p]);
+        }
+    };
+    // Tile t + 1 is in LDS, for every wavefront, and nobody reads tile t there any more; the RING - 2 after it may still be on their way.
+    const auto arrive = [&](bool later) {
+        if (RING > 2 && later) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((RING - 2) * PIECES) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
 
     Int16 sum[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sum[i][j][r] = 0;
     Int4 operand[2][MT + NT];
     const char* const xrow = lds + (wm * WM + lane % 32) * kStep;
     const char* const wrow = lds + XBYTES + (wn * WN + lane % 32) * kStep;
@@ -168,24 +182,33 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         const int at = buffer * BYTES + ((2 * s + lane / 32) ^ (lane / 2 % 8)) * kPiece;
         operand[s & 1][o] = *(const Int4*)((o < MT ? xrow + o * 32 * kStep : wrow + (o - MT) * 32 * kStep) + at);
     };
-    // A quarter's products, and between them, in this order, what else is to be issued: a matrix core takes 32 cycles for a product, and a
-    // wavefront has it to itself.
+    // A quarter's products, and between them, in this order, what else is to be issued: a matrix core takes 32 cycles for a product.
     constexpr int PRODUCTS = MT * NT;
     const auto multiply = [&](int set, int q) {
         const int i = q / NT, j = q % NT;
         sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(operand[set][MT + j], operand[set][i], sum[i][j], 0, 0, 0);
     };
 
-    if (tiles == 0) {
-        __syncthreads();
-    } else {
-        fetch_all(0, 0);
-        arrive(0, 0);
-        fetch_all(1, 1);
+    if (t0 < tiles) {
+        if (t0 < partial) fetch_partial();
+        else fetch_all(t0, 0);
+        if (t0 >= partial) put_held(0);
+    }
+    arrive(false);
+#pragma unroll
+    for (int r = 1; r < RING; ++r) fetch_all(t0 + r, r);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[i][j][r] = 0;
+    if (t0 < tiles) {
 #pragma unroll
         for (int o = 0; o < MT + NT; ++o) read(o, 0, 0);
-        for (int t = 0; t < tiles; ++t) {
-            const int now = t & 1;
+        int now = 0;
+        for (int t = t0; t < tiles; ++t) {
+            const int next = now + 1 == RING ? 0 : now + 1;
 #pragma unroll
             for (int s = 0; s < 3; ++s)
 #pragma unroll
@@ -202,23 +225,24 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 #pragma unroll
             for (int q = 0; q < BEFORE; ++q) multiply(1, q);
             __builtin_amdgcn_sched_barrier(0);
-            arrive(t + 1, now ^ 1);
-            const bool more = t + 2 < whole;
+            if (t + 1 < tiles) put_held(next);
+            arrive(t + RING - 1 < tiles);
+            const bool more = t + RING < tiles;
 #pragma unroll
             for (int q = BEFORE; q < PRODUCTS; ++q) {
                 multiply(1, q);
                 // read past the last tile too: what is read then is not used
 #pragma unroll
                 for (int o = 0; o < MT + NT; ++o)
-                    if (BEFORE + o * (PRODUCTS - BEFORE) / (MT + NT) == q) read(o, now ^ 1, 0);
+                    if (BEFORE + o * (PRODUCTS - BEFORE) / (MT + NT) == q) read(o, next, 0);
                 if (more) {
 #pragma unroll
                     for (int p = 0; p < PIECES; ++p)
-                        if (BEFORE + p * (PRODUCTS - BEFORE) / PIECES == q) fetch(p, t + 2, now);
+                        if (BEFORE + p * (PRODUCTS - BEFORE) / PIECES == q) fetch(p, t + RING, now);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (!more && t + 2 < tiles) fetch_end(t + 2, now);
+            now = next;
         }
     }
 
@@ -227,20 +251,26 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
     char* const strip = lds + wave * 32 * STRIP;
     constexpr int VEC = 16 / sizeof(S), LANES = WN / VEC, ROWS = 64 / LANES;
     const int nw = n0 + wn * WN;
+    S* const out = (S*)a.out + (std::is_same_v<S, int32_t> ? blockIdx.y * a.M * a.out_stride : 0);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int64_t mw = m0 + wm * WM + i * 32;
-        const float xs = a.x_scale[min(mw + lane % 32, a.M - 1)];
+        const float xs = std::is_same_v<S, int32_t> ? 0.0f : a.x_scale[min(mw + lane % 32, a.M - 1)];
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int in = j * 32 + 8 * g + 4 * (lane / 32);
-                const auto ws = *(const Pack<float, 4>*)&channel[0][wn * WN + in], bias = *(const Pack<float, 4>*)&channel[1][wn * WN + in];
-                float f[4];
+                char* const to = strip + (lane % 32) * STRIP + in * sizeof(S);
+                if constexpr (std::is_same_v<S, int32_t>) {
+                    *(Int4*)to = Int4{sum[i][j][4 * g], sum[i][j][4 * g + 1], sum[i][j][4 * g + 2], sum[i][j][4 * g + 3]};
+                } else {
+                    const auto ws = *(const Pack<float, 4>*)&channel[0][wn * WN + in], bias = *(const Pack<float, 4>*)&channel[1][wn * WN + in];
+                    float f[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) f[r] = scaled(sum[i][j][4 * g + r], xs, ws.get(r), bias.get(r));
-                *(Pack<S, 4>*)(strip + (lane % 32) * STRIP + in * sizeof(S)) = Pack<S, 4>::from(f);
+                    for (int r = 0; r < 4; ++r) f[r] = scaled(sum[i][j][4 * g + r], xs, ws.get(r), bias.get(r));
+                    *(Pack<S, 4>*)to = Pack<S, 4>::from(f);
+                }
             }
         wave_order();
 #pragma unroll
@@ -248,18 +278,53 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
             const int row = r + lane / LANES, n = nw + lane % LANES * VEC;
             const int64_t m = mw + row;
             if (m < a.M && n < a.N) {
-                const auto v = *(const Pack<S, VEC>*)(strip + row * STRIP + lane % LANES * 16);
-                S* const to = (S*)a.out + m * a.out_stride + n;
+                const Int4 v = *(const Int4*)(strip + row * STRIP + lane % LANES * 16);
+                S* const to = out + m * a.out_stride + n;
                 if (n + VEC <= a.N) {
-                    store_pack(to, v);
+                    __builtin_memcpy(to, &v, sizeof(v));
                 } else {
+                    const auto each = __builtin_bit_cast(Elements<S>, v);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e)
-                        if (n + e < a.N) to[e] = v.element(e);
+                        if (n + e < a.N) to[e] = each.v[e];
                 }
             }
         }
         wave_order();
+    }
+}
+
+// The stretches' sums of an element, and what follows: a thread has N channels of a row.  What would end beyond the row is moved back
+// to end with it and stores what the thread before it stores as well.
+template <class S, int N>
+__global__ __launch_bounds__(256) void join_kernel(const Args a, const int32_t* __restrict__ sums, int stretches) {
+    constexpr int U = 8;                 // loads in flight
+    int n = (int)(blockIdx.x * 256 + threadIdx.x) * N;
+    if (n >= a.N) return;
+    n = min(n, a.N - N);
+    float ws[N], bias[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+        ws[r] = a.w_scale[n + r];
+        bias[r] = a.bias ? a.bias[n + r] : 0.0f;
+    }
+    for (int64_t m = blockIdx.y; m < a.M; m += gridDim.y) {
+        const int32_t* const at = sums + m * a.N + n;
+        int32_t sum[N] = {};
+        for (int i = 0; i < stretches; i += U) {
+            Pack<int32_t, N> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_pack<N>(at + min(i + u, stretches - 1) * a.M * a.N);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int r = 0; r < N; ++r) sum[r] += i + u < stretches ? v[u].v[r] : 0;
+        }
+        const float xs = a.x_scale[m];
+        float f[N];
+#pragma unroll
+        for (int r = 0; r < N; ++r) f[r] = scaled(sum[r], xs, ws[r], bias[r]);
+        store_pack((S*)a.out + m * a.out_stride + n, Pack<S, N>::from(f));
     }
 }
 
@@ -336,48 +401,68 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int s
     }
 }
 
-template <class S, int BM, int BN, int WM, int WN>
-void launch_tiles(Args a, bool direct, hipStream_t s) {
+template <class S, int BM, int BN, int WM, int WN, int RING>
+void launch_tiles(Args a, bool direct, int stretches, hipStream_t s) {
     a.tiles_m = (int)((a.M + BM - 1) / BM);
     a.tiles_n = (a.N + BN - 1) / BN;
-    a.far = a.x_stride >= 1 << 24 || a.w_stride >= 1 << 24;
-    const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n)), block((BM / WM) * (BN / WN) * 64);
-    if (direct) hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, false>), grid, block, 0, s, a);
+    const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n), (unsigned)stretches), block((BM / WM) * (BN / WN) * 64);
+    if (direct) hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, RING, kRowsDirect>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, 2, kRowsHeld>), grid, block, 0, s, a);
 }
 
-bool rows_at_16(const void* p, int64_t stride) {
-    return ((uintptr_t)p & 15) == 0 && stride % 16 == 0;
+bool rows_at_16(const void* p, int64_t stride) { return ((uintptr_t)p & 15) == 0 && stride % 16 == 0; }
+int64_t tiles_of(int64_t M, int64_t N, int64_t side) { return ((M + side - 1) / side) * ((N + side - 1) / side); }
+
+constexpr int64_t kFewRows = 32;
+// Stretches of K for tiles of 64: as many as give every compute unit two workgroups, none shorter than eight tiles of K.
+int stretches_of(int64_t M, int64_t N, int64_t K) {
+    if (M <= kFewRows || tiles_of(M, N, 256) >= 192 || tiles_of(M, N, 128) >= 192) return 1;
+    const int64_t most = K / (8 * kStep), want = 512 / tiles_of(M, N, 64);
+    return (int)(want < 2 || most < 2 ? 1 : want < most ? want : most);
 }
 
 template <class S>
-void run(const Args& a, hipStream_t s) {
-    const bool direct = rows_at_16(a.x, a.x_stride) && rows_at_16(a.w, a.w_stride);
-    const auto tiles = [&](int64_t bm, int64_t bn) { return ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
-    if (a.M <= 32) {
-        const int64_t stretches = (a.N + 15) / 16;
+void run(const Args& a, void* workspace, hipStream_t s) {
+    // of a tile's rows the farthest is addressed by 32 bits from its first
+    const bool far = a.x_stride >= 1 << 24 || a.w_stride >= 1 << 24;
+    const bool direct = !far && rows_at_16(a.x, a.x_stride) && rows_at_16(a.w, a.w_stride);
+    const int stretches = stretches_of(a.M, a.N, a.K);
+    if (a.M <= kFewRows) {
+        const int64_t places = (a.N + 15) / 16;
         int share = 1;
-        while (share < kFewWaves && stretches * share < 2048 && a.K > 512 * share) share *= 2;
+        while (share < kFewWaves && places * share < 2048 && a.K > 512 * share) share *= 2;
         const int64_t per = kFewWaves / share;
-        const dim3 grid((unsigned)((stretches + per - 1) / per));
+        const dim3 grid((unsigned)((places + per - 1) / per));
         if (a.M <= 16) hipLaunchKernelGGL((few_kernel<S, 1>), grid, dim3(kFewWaves * 64), 0, s, a, share);
         else hipLaunchKernelGGL((few_kernel<S, 2>), grid, dim3(kFewWaves * 64), 0, s, a, share);
-    } else if (tiles(256, 256) >= 192) {
-        launch_tiles<S, 256, 256, 128, 128>(a, direct, s);
-    } else if (tiles(128, 128) >= 192) {
-        launch_tiles<S, 128, 128, 64, 64>(a, direct, s);
+    } else if (far) {
+        Args b = a;
+        b.tiles_m = (int)((a.M + 63) / 64);
+        b.tiles_n = (a.N + 63) / 64;
+        hipLaunchKernelGGL((tile_kernel<S, 64, 64, 32, 32, 2, kRowsFar>), dim3((unsigned)((int64_t)b.tiles_m * b.tiles_n)), dim3(256), 0, s, b);
+    } else if (stretches > 1) {
+        Args b = a;
+        b.out = workspace;
+        b.out_stride = a.N;
+        launch_tiles<int32_t, 64, 64, 32, 32, 4>(b, direct, stretches, s);
+        const unsigned rows = (unsigned)(a.M < 16384 ? a.M : 16384);
+        if (a.N >= 4) hipLaunchKernelGGL((join_kernel<S, 4>), dim3((unsigned)((a.N + 1023) / 1024), rows), dim3(256), 0, s, a, (const int32_t*)workspace, stretches);
+        else hipLaunchKernelGGL((join_kernel<S, 1>), dim3(1, rows), dim3(256), 0, s, a, (const int32_t*)workspace, stretches);
+    } else if (tiles_of(a.M, a.N, 256) >= 192) {
+        launch_tiles<S, 256, 256, 128, 128, 2>(a, direct, 1, s);
+    } else if (tiles_of(a.M, a.N, 128) >= 192) {
+        launch_tiles<S, 128, 128, 64, 64, 2>(a, direct, 1, s);
     } else {
-        launch_tiles<S, 64, 64, 32, 32>(a, direct, s);
+        launch_tiles<S, 64, 64, 32, 32, 4>(a, direct, 1, s);
     }
 }
 
 }  // namespace
 
 size_t product_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    (void)M;
-    (void)N;
-    (void)K;
-    return 0;
+    if (M == 0 || N == 0) return 0;
+    const int64_t stretches = stretches_of(M, N, K);
+    return stretches > 1 ? (size_t)((stretches * M * N * 4 + 255) / 256 * 256) : 0;
 }
 
 hipError_t launch_product(const ProductCall& c, hipStream_t s) {
@@ -394,9 +479,9 @@ hipError_t launch_product(const ProductCall& c, hipStream_t s) {
     a.w_stride = c.w_stride;
     a.out_stride = c.out_stride;
     a.out = c.out;
-    if (c.dtype == kF32) run<float>(a, s);
-    else if (c.dtype == kF16) run<_Float16>(a, s);
-    else run<__bf16>(a, s);
+    if (c.dtype == kF32) run<float>(a, c.workspace, s);
+    else if (c.dtype == kF16) run<_Float16>(a, c.workspace, s);
+    else run<__bf16>(a, c.workspace, s);
     return hipGetLastError();
 }
 
