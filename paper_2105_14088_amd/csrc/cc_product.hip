@@ -28,7 +28,6 @@ using namespace ccm;
 typedef int Int4 __attribute__((ext_vector_type(4)));
 typedef int Int16 __attribute__((ext_vector_type(16)));
 
-constexpr int kStep = 128;               // bytes of K in a tile
 constexpr int kPiece = 16;
 
 struct Args {
@@ -86,17 +85,19 @@ enum RowMode { kRowsDirect, kRowsHeld, kRowsFar };
 
 // RING tiles of the operands are held, so a tile has RING - 1 others' time to arrive.  With more than one workgroup to a tile (gridDim.y) each
 // has a stretch of K, and S is int32: its sums go to a matrix of their own.
-template <class S, int BM, int BN, int WM, int WN, int RING, RowMode MODE>
+template <class S, int BM, int BN, int WM, int WN, int STEP, int RING, RowMode MODE>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const Args a) {
     constexpr int THREADS = (BM / WM) * (BN / WN) * 64, WAVES = THREADS / 64;
     constexpr int MT = WM / 32, NT = WN / 32;
-    constexpr int XBYTES = BM * kStep, WBYTES = BN * kStep, BYTES = XBYTES + WBYTES;
+    constexpr int XBYTES = BM * STEP, WBYTES = BN * STEP, BYTES = XBYTES + WBYTES;
+    constexpr int ROW = STEP / kPiece, SHARE = 256 / STEP;          // pieces of a row, rows that share the banks
     constexpr int PIECES = BYTES / (THREADS * kPiece), XPIECES = XBYTES / (THREADS * kPiece);
     static_assert(XBYTES % (THREADS * kPiece) == 0 && WBYTES % (THREADS * kPiece) == 0, "every load of a workgroup is of one operand");
-    static_assert(THREADS / 8 % 16 == 0, "a thread's pieces lie at the same place of their rows");
+    static_assert(THREADS / ROW % (SHARE * ROW) == 0, "a thread's pieces lie at the same place of their rows");
     static_assert(MODE == kRowsDirect || RING == 2, "registers hold one tile");
-    constexpr int STRIP = WN * (int)sizeof(S) + 16;                 // a row of the result's strip in LDS
-    static_assert(WAVES * 32 * STRIP <= RING * BYTES, "the strips lie where the operands were");
+    constexpr int WIDE = WN * sizeof(S) <= 128 ? WN : 128 / sizeof(S);          // channels of the result that a wavefront has in LDS at once
+    constexpr int STRIP = WIDE * (int)sizeof(S) + 16;               // a row of them
+    static_assert(WAVES * WM * STRIP <= RING * BYTES, "they lie where the operands were");
     __shared__ __attribute__((aligned(128))) char lds[RING * BYTES];
     __shared__ __attribute__((aligned(16))) float channel[2][BN];   // scales and biases
 
@@ -117,10 +118,10 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         }
 
     // Where this thread's pieces come from: rows beyond the last are the last again, their results are not stored.
-    // Piece p of wavefront `wave` fills LDS from (p * THREADS + wave * 64) * 16 on, 8 rows.
-    const int in_row = (lane % 8) ^ ((wave * 8 + lane / 8) / 2 % 8);
+    // Piece p of wavefront `wave` fills LDS from (p * THREADS + wave * 64) * 16 on.
+    const int in_row = (lane % ROW) ^ (thread / ROW / SHARE % ROW);
     const auto row_of = [&](int p) {
-        const int row = ((p < XPIECES ? p : p - XPIECES) * THREADS + wave * 64 + lane) / 8;
+        const int row = ((p < XPIECES ? p : p - XPIECES) * THREADS + thread) / ROW;
         return min(row, p < XPIECES ? last_m : last_n);
     };
     std::conditional_t<MODE == kRowsFar, int64_t, uint32_t> from[PIECES];
@@ -131,10 +132,10 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
     const auto put = [&](int p, int buffer, const Int4& v) { *(Int4*)(lds + buffer * BYTES + (p * THREADS + thread) * kPiece) = v; };
     // The sum does not depend on the order of its terms: where K ends inside a tile, that tile is the first, so that only the start has to
     // look at where a row ends.
-    const int whole = a.K / kStep, partial = a.K % kStep != 0, all = whole + partial;
+    const int whole = a.K / STEP, partial = a.K % STEP != 0, all = whole + partial;
     const int t0 = (int)((int64_t)all * blockIdx.y / gridDim.y), tiles = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y);
     const auto fetch = [&](int p, int t, int buffer) {
-        const int8_t* const base = (p < XPIECES ? xbase : wbase) + (int64_t)(t - partial) * kStep;
+        const int8_t* const base = (p < XPIECES ? xbase : wbase) + (int64_t)(t - partial) * STEP;
         if constexpr (MODE == kRowsDirect) {
             const uint32_t to = (uint32_t)(uintptr_t)lds + buffer * BYTES + wave * 1024 + p * THREADS * kPiece;
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(from[p]), "s"(base) : "memory");
@@ -148,14 +149,14 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         for (int p = 0; p < PIECES; ++p) fetch(p, t, buffer);
     };
     const auto fetch_partial = [&] {
-        constexpr int U = PIECES < 8 ? PIECES : 8;
+        constexpr int U = PIECES > 8 ? 4 : PIECES;
 #pragma unroll
         for (int p = 0; p < PIECES; p += U) {
             Int4 v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int8_t* const row = p + u < XPIECES ? xbase + row_of(p + u) * a.x_stride : wbase + row_of(p + u) * a.w_stride;
-                v[u] = load_piece(row, whole * kStep + in_row * kPiece, a.K);
+                v[u] = load_piece(row, whole * STEP + in_row * kPiece, a.K);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) put(p + u, 0, v[u]);
@@ -175,28 +176,33 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 
     Int16 sum[MT][NT];
     Int4 operand[2][MT + NT];
-    const char* const xrow = lds + (wm * WM + lane % 32) * kStep;
-    const char* const wrow = lds + XBYTES + (wn * WN + lane % 32) * kStep;
-    // Operand o of a quarter s of a tile, for the next multiplication.
+    const char* const xrow = lds + (wm * WM + lane % 32) * STEP;
+    const char* const wrow = lds + XBYTES + (wn * WN + lane % 32) * STEP;
+    // Operand o of part s of a tile (32 bytes of K), for the next multiplication.
     const auto read = [&](int o, int buffer, int s) {
-        const int at = buffer * BYTES + ((2 * s + lane / 32) ^ (lane / 2 % 8)) * kPiece;
-        operand[s & 1][o] = *(const Int4*)((o < MT ? xrow + o * 32 * kStep : wrow + (o - MT) * 32 * kStep) + at);
+        const int at = buffer * BYTES + ((2 * s + lane / 32) ^ (lane % 32 / SHARE % ROW)) * kPiece;
+        operand[s & 1][o] = *(const Int4*)((o < MT ? xrow + o * 32 * STEP : wrow + (o - MT) * 32 * STEP) + at);
     };
-    // A quarter's products, and between them, in this order, what else is to be issued: a matrix core takes 32 cycles for a product.
+    constexpr int PARTS = STEP / 32;
+    static_assert(PARTS % 2 == 0, "the next tile's first part is read while this one's last is multiplied");
+    // A part's products, and between them, in this order, what else is to be issued: a matrix core takes 32 cycles for a product.
     constexpr int PRODUCTS = MT * NT;
     const auto multiply = [&](int set, int q) {
         const int i = q / NT, j = q % NT;
         sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(operand[set][MT + j], operand[set][i], sum[i][j], 0, 0, 0);
     };
 
-    if (t0 < tiles) {
-        if (t0 < partial) fetch_partial();
-        else fetch_all(t0, 0);
-        if (t0 >= partial) put_held(0);
+    const bool starts_partial = t0 < partial;
+    if (!starts_partial) {
+        fetch_all(t0, 0);
+        put_held(0);
     }
-    arrive(false);
 #pragma unroll
     for (int r = 1; r < RING; ++r) fetch_all(t0 + r, r);
+    if (starts_partial) fetch_partial();
+    if (MODE == kRowsDirect && !starts_partial && t0 + RING - 1 < tiles)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((RING - 1) * PIECES) : "memory");
+    else arrive(false);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -210,7 +216,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         for (int t = t0; t < tiles; ++t) {
             const int next = now + 1 == RING ? 0 : now + 1;
 #pragma unroll
-            for (int s = 0; s < 3; ++s)
+            for (int s = 0; s < PARTS - 1; ++s)
 #pragma unroll
                 for (int q = 0; q < PRODUCTS; ++q) {
                     multiply(s & 1, q);
@@ -246,36 +252,46 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         }
     }
 
-    // A lane has channels 8 g + 4 (lane / 32) .. + 3 of row lane % 32: strips of 32 rows go through LDS, each wavefront's its
-    // own, so that rows are stored in vectors of 16 bytes side by side.
-    char* const strip = lds + wave * 32 * STRIP;
-    constexpr int VEC = 16 / sizeof(S), LANES = WN / VEC, ROWS = 64 / LANES;
-    const int nw = n0 + wn * WN;
+    // A lane has channels 8 g + 4 (lane / 32) .. + 3 of row lane % 32.  They go through LDS, each wavefront's its own, so that rows are stored in
+    // vectors of 16 bytes side by side, 128 bytes of a row at a time.
+    char* const strip = lds + wave * WM * STRIP;
+    constexpr int VEC = 16 / sizeof(S), LANES = WIDE / VEC, ROWS = 64 / LANES;
+    const int64_t mw = m0 + wm * WM;
     S* const out = (S*)a.out + (std::is_same_v<S, int32_t> ? blockIdx.y * a.M * a.out_stride : 0);
+    float xs[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t mw = m0 + wm * WM + i * 32;
-        const float xs = std::is_same_v<S, int32_t> ? 0.0f : a.x_scale[min(mw + lane % 32, a.M - 1)];
+    for (int i = 0; i < MT; ++i) xs[i] = std::is_same_v<S, int32_t> ? 0.0f : a.x_scale[min(mw + i * 32 + lane % 32, a.M - 1)];
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+    for (int j0 = 0; j0 < NT; j0 += WIDE / 32) {
+        const int nw = wn * WN + j0 * 32;
+#pragma unroll
+        for (int j = 0; j < WIDE / 32; ++j)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int in = j * 32 + 8 * g + 4 * (lane / 32);
-                char* const to = strip + (lane % 32) * STRIP + in * sizeof(S);
-                if constexpr (std::is_same_v<S, int32_t>) {
-                    *(Int4*)to = Int4{sum[i][j][4 * g], sum[i][j][4 * g + 1], sum[i][j][4 * g + 2], sum[i][j][4 * g + 3]};
-                } else {
-                    const auto ws = *(const Pack<float, 4>*)&channel[0][wn * WN + in], bias = *(const Pack<float, 4>*)&channel[1][wn * WN + in];
-                    float f[4];
+                Pack<float, 4> ws = {}, bias = {};
+                if constexpr (!std::is_same_v<S, int32_t>) {
+                    ws = *(const Pack<float, 4>*)&channel[0][nw + in];
+                    bias = *(const Pack<float, 4>*)&channel[1][nw + in];
+                }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) f[r] = scaled(sum[i][j][4 * g + r], xs, ws.get(r), bias.get(r));
-                    *(Pack<S, 4>*)to = Pack<S, 4>::from(f);
+                for (int i = 0; i < MT; ++i) {
+                    char* const to = strip + (i * 32 + lane % 32) * STRIP + in * sizeof(S);
+                    const auto& part = sum[i][j0 + j];
+                    if constexpr (std::is_same_v<S, int32_t>) {
+                        *(Int4*)to = Int4{part[4 * g], part[4 * g + 1], part[4 * g + 2], part[4 * g + 3]};
+                    } else {
+                        float f[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) f[r] = scaled(part[4 * g + r], xs[i], ws.get(r), bias.get(r));
+                        *(Pack<S, 4>*)to = Pack<S, 4>::from(f);
+                    }
                 }
             }
         wave_order();
 #pragma unroll
-        for (int r = 0; r < 32; r += ROWS) {
-            const int row = r + lane / LANES, n = nw + lane % LANES * VEC;
+        for (int r = 0; r < WM; r += ROWS) {
+            const int row = r + lane / LANES, n = n0 + nw + lane % LANES * VEC;
             const int64_t m = mw + row;
             if (m < a.M && n < a.N) {
                 const Int4 v = *(const Int4*)(strip + row * STRIP + lane % LANES * 16);
@@ -328,96 +344,135 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, const int32_t* 
     }
 }
 
-// MT * 16 rows, 16 channels to `share` wavefronts of a workgroup's 8, each of which has a stretch of K.
+// MT * 16 rows; NT * 16 channels to `share` wavefronts of a workgroup's 8, each of which has a stretch of K.  Weights are read once, the rows of x
+// once for every NT * 16 channels.
 constexpr int kFewWaves = 8;
-template <class S, int MT>
+template <class S, int MT, int NT>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int share) {
-    __shared__ Int4 parts[kFewWaves][MT][64];
+    __shared__ Int4 parts[kFewWaves][MT * NT][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int64_t n0 = ((int64_t)blockIdx.x * (kFewWaves / share) + wave / share) * 16;
+    const int64_t n0 = ((int64_t)blockIdx.x * (kFewWaves / share) + wave / share) * 16 * NT;
     const int steps = (a.K + 63) / 64, each = (steps + share - 1) / share;
     const int begin = min(wave % share * each, steps), end = min(begin + each, steps);
-    Int4 sum[MT];
+    Int4 sum[MT][NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) sum[i] = Int4{0, 0, 0, 0};
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sum[i][j] = Int4{0, 0, 0, 0};
     if (n0 < a.N) {
-        const int8_t* const wrow = a.w + min(n0 + lane % 16, (int64_t)a.N - 1) * a.w_stride;
-        const int8_t* xrow[MT];
+        const int8_t *wrow[NT], *xrow[MT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) wrow[j] = a.w + min(n0 + j * 16 + lane % 16, (int64_t)a.N - 1) * a.w_stride;
 #pragma unroll
         for (int i = 0; i < MT; ++i) xrow[i] = a.x + min((int64_t)i * 16 + lane % 16, a.M - 1) * a.x_stride;
         const int in = lane / 16 * kPiece;
-        constexpr int U = 8;
+        constexpr int U = 8 / NT;
+        // U steps' loads in flight; `load` takes pieces that a row has all of, or any
+        const auto batch = [&](int s, int count, auto load) {
+            Int4 w[U][NT], x[U][MT];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) w[u][j] = load(wrow[j], (s + min(u, count - 1)) * 64 + in);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) x[u][i] = load(xrow[i], (s + min(u, count - 1)) * 64 + in);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < count) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][j], x[u][i], sum[i][j], 0, 0, 0);
+                }
+        };
+        const auto all_of = [](const int8_t* row, int k) {
+            Int4 v;
+            __builtin_memcpy(&v, row + k, kPiece);
+            return v;
+        };
         int s = begin;
-        for (; s + U <= end && (s + U) * 64 <= a.K; s += U) {
-            Int4 w[U], x[U][MT];
-#pragma unroll
-            for (int u = 0; u < U; ++u) __builtin_memcpy(&w[u], wrow + (s + u) * 64 + in, kPiece);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < MT; ++i) __builtin_memcpy(&x[u][i], xrow[i] + (s + u) * 64 + in, kPiece);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < MT; ++i) sum[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], x[u][i], sum[i], 0, 0, 0);
-        }
-        for (; s < end; ++s) {
-            const Int4 w = load_piece(wrow, s * 64 + in, a.K);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) sum[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, load_piece(xrow[i], s * 64 + in, a.K), sum[i], 0, 0, 0);
-        }
+        for (; s + U <= end && (s + U) * 64 <= a.K; s += U) batch(s, U, all_of);
+        for (; s < end; s += U) batch(s, min(U, end - s), [&](const int8_t* row, int k) { return load_piece(row, k, a.K); });
     }
     if (share > 1) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) parts[wave][i][lane] = sum[i];
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) parts[wave][i * NT + j][lane] = sum[i][j];
         __syncthreads();
         if (wave % share != 0) return;
         for (int p = 1; p < share; ++p)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) sum[i] += parts[wave + p][i][lane];
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) sum[i][j] += parts[wave + p][i * NT + j][lane];
     }
     // a lane has channels 4 (lane / 16) .. + 3 of row lane % 16
-    const int64_t n = n0 + lane / 16 * 4;
-    if (n >= a.N) return;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t m = i * 16 + lane % 16;
-        if (m >= a.M) continue;
-        const float xs = a.x_scale[m];
-        S* const to = (S*)a.out + m * a.out_stride + n;
-        float f[4];
+    for (int j = 0; j < NT; ++j) {
+        const int64_t n = n0 + j * 16 + lane / 16 * 4;
+        if (n >= a.N) continue;
+        float ws[4], bias[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int64_t c = min(n + r, (int64_t)a.N - 1);
-            f[r] = scaled(sum[i][r], xs, a.w_scale[c], a.bias ? a.bias[c] : 0.0f);
+            ws[r] = a.w_scale[c];
+            bias[r] = a.bias ? a.bias[c] : 0.0f;
         }
-        if (n + 4 <= a.N) {
-            store_pack(to, Pack<S, 4>::from(f));
-        } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (n + r < a.N) to[r] = narrow<S>(f[r]);
+        for (int i = 0; i < MT; ++i) {
+            const int64_t m = i * 16 + lane % 16;
+            if (m >= a.M) continue;
+            const float xs = a.x_scale[m];
+            S* const to = (S*)a.out + m * a.out_stride + n;
+            float f[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) f[r] = scaled(sum[i][j][r], xs, ws[r], bias[r]);
+            if (n + 4 <= a.N) {
+                store_pack(to, Pack<S, 4>::from(f));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (n + r < a.N) to[r] = narrow<S>(f[r]);
+            }
         }
     }
 }
 
-template <class S, int BM, int BN, int WM, int WN, int RING>
+template <class S, int MT, int NT>
+void launch_few(const Args& a, int64_t waves, hipStream_t s) {
+    const int64_t places = (a.N + 16 * NT - 1) / (16 * NT);
+    int share = 1;
+    while (share < kFewWaves && places * share < waves && a.K > 512 / NT * share) share *= 2;
+    const int64_t per = kFewWaves / share;
+    hipLaunchKernelGGL((few_kernel<S, MT, NT>), dim3((unsigned)((places + per - 1) / per)), dim3(kFewWaves * 64), 0, s, a, share);
+}
+
+template <class S, int BM, int BN, int WM, int WN, int STEP, int RING>
 void launch_tiles(Args a, bool direct, int stretches, hipStream_t s) {
     a.tiles_m = (int)((a.M + BM - 1) / BM);
     a.tiles_n = (a.N + BN - 1) / BN;
     const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n), (unsigned)stretches), block((BM / WM) * (BN / WN) * 64);
-    if (direct) hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, RING, kRowsDirect>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, 2, kRowsHeld>), grid, block, 0, s, a);
+    if (direct) hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, STEP, RING, kRowsDirect>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, 128, 2, kRowsHeld>), grid, block, 0, s, a);
 }
 
 bool rows_at_16(const void* p, int64_t stride) { return ((uintptr_t)p & 15) == 0 && stride % 16 == 0; }
 int64_t tiles_of(int64_t M, int64_t N, int64_t side) { return ((M + side - 1) / side) * ((N + side - 1) / side); }
 
 constexpr int64_t kFewRows = 32;
+// A tile of 256 takes a compute unit, which has two of 128 at once; those take 0.6 of its time together (8192 x 8192 x 4096: 269 us in four
+// rounds of the former, 320 in eight of the latter), but leave less of a last round unused (5000 x 5000 x 1024: 46 and 41 us).
+bool large_tiles(int64_t M, int64_t N) {
+    const double small = (double)tiles_of(M, N, 128) / 512;
+    return (double)((tiles_of(M, N, 256) + 255) / 256) <= 0.6 * (small < 1.0 ? 1.0 : small);
+}
 // Stretches of K for tiles of 64: as many as give every compute unit two workgroups, none shorter than eight tiles of K.
 int stretches_of(int64_t M, int64_t N, int64_t K) {
-    if (M <= kFewRows || tiles_of(M, N, 256) >= 192 || tiles_of(M, N, 128) >= 192) return 1;
-    const int64_t most = K / (8 * kStep), want = 512 / tiles_of(M, N, 64);
+    if (M <= kFewRows || tiles_of(M, N, 128) >= 192) return 1;
+    const int64_t most = K / 1024, want = 512 / tiles_of(M, N, 64);
     return (int)(want < 2 || most < 2 ? 1 : want < most ? want : most);
 }
 
@@ -428,32 +483,28 @@ void run(const Args& a, void* workspace, hipStream_t s) {
     const bool direct = !far && rows_at_16(a.x, a.x_stride) && rows_at_16(a.w, a.w_stride);
     const int stretches = stretches_of(a.M, a.N, a.K);
     if (a.M <= kFewRows) {
-        const int64_t places = (a.N + 15) / 16;
-        int share = 1;
-        while (share < kFewWaves && places * share < 2048 && a.K > 512 * share) share *= 2;
-        const int64_t per = kFewWaves / share;
-        const dim3 grid((unsigned)((places + per - 1) / per));
-        if (a.M <= 16) hipLaunchKernelGGL((few_kernel<S, 1>), grid, dim3(kFewWaves * 64), 0, s, a, share);
-        else hipLaunchKernelGGL((few_kernel<S, 2>), grid, dim3(kFewWaves * 64), 0, s, a, share);
+        // 8 x 50001 x 1024: 14.7 us with 32 channels a wavefront, 15.9 with 16; 1 x 512 x 8192: 11.2 and 7.9
+        if (a.N >= 16384) a.M <= 16 ? launch_few<S, 1, 2>(a, 1536, s) : launch_few<S, 2, 2>(a, 1536, s);
+        else a.M <= 16 ? launch_few<S, 1, 1>(a, 2048, s) : launch_few<S, 2, 1>(a, 2048, s);
     } else if (far) {
         Args b = a;
         b.tiles_m = (int)((a.M + 63) / 64);
         b.tiles_n = (a.N + 63) / 64;
-        hipLaunchKernelGGL((tile_kernel<S, 64, 64, 32, 32, 2, kRowsFar>), dim3((unsigned)((int64_t)b.tiles_m * b.tiles_n)), dim3(256), 0, s, b);
+        hipLaunchKernelGGL((tile_kernel<S, 64, 64, 32, 32, 128, 2, kRowsFar>), dim3((unsigned)((int64_t)b.tiles_m * b.tiles_n)), dim3(256), 0, s, b);
     } else if (stretches > 1) {
         Args b = a;
         b.out = workspace;
         b.out_stride = a.N;
-        launch_tiles<int32_t, 64, 64, 32, 32, 4>(b, direct, stretches, s);
+        launch_tiles<int32_t, 64, 64, 32, 32, 128, 4>(b, direct, stretches, s);
         const unsigned rows = (unsigned)(a.M < 16384 ? a.M : 16384);
         if (a.N >= 4) hipLaunchKernelGGL((join_kernel<S, 4>), dim3((unsigned)((a.N + 1023) / 1024), rows), dim3(256), 0, s, a, (const int32_t*)workspace, stretches);
         else hipLaunchKernelGGL((join_kernel<S, 1>), dim3(1, rows), dim3(256), 0, s, a, (const int32_t*)workspace, stretches);
-    } else if (tiles_of(a.M, a.N, 256) >= 192) {
-        launch_tiles<S, 256, 256, 128, 128, 2>(a, direct, 1, s);
+    } else if (tiles_of(a.M, a.N, 256) >= 128 && a.K > 512 && large_tiles(a.M, a.N)) {
+        launch_tiles<S, 256, 256, 128, 128, 128, 2>(a, direct, 1, s);
     } else if (tiles_of(a.M, a.N, 128) >= 192) {
-        launch_tiles<S, 128, 128, 64, 64, 2>(a, direct, 1, s);
+        launch_tiles<S, 128, 128, 64, 64, 128, 2>(a, direct, 1, s);
     } else {
-        launch_tiles<S, 64, 64, 32, 32, 4>(a, direct, 1, s);
+        launch_tiles<S, 64, 64, 32, 32, 128, 4>(a, direct, 1, s);
     }
 }
 

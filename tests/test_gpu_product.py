@@ -46,7 +46,10 @@ def case(m, n, k, dtype=F32, bias=True, full=True, seed=0):
 SIZES = [(1, 1, 1), (1, 16, 64), (2, 17, 15), (3, 5, 16), (8, 64, 130), (16, 100, 512), (16, 1000, 4096), (16, 33, 577), (17, 40, 1000),
          (32, 255, 2048), (31, 513, 100), (33, 64, 128), (33, 1, 7), (64, 64, 128), (65, 66, 129), (64, 64, 256), (100, 130, 384), (128, 128, 400),
          (200, 300, 250), (257, 255, 640), (1024, 64, 128), (777, 1001, 250), (1500, 1700, 96), (2048, 1792, 272), (1800, 2050, 129), (4096, 4096, 640),
-         (4000, 4100, 144), (4100, 3999, 1000), (3840, 4096, 16)]
+         (4000, 4100, 144), (4100, 3999, 1000), (3840, 4096, 16),
+         # stretches of K, of rows that begin anywhere too; wide heads for few rows; tiles of 128 where those of 256 leave a round half empty
+         (64, 64, 2048), (70, 3, 4096), (300, 301, 3001), (40, 700, 9000), (512, 512, 2176), (16, 16384, 200), (9, 20001, 1001), (20, 17000, 640),
+         (5000, 5000, 640), (4500, 4700, 1153), (8192, 2100, 1024)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
