@@ -606,7 +606,7 @@ int cc_quantize_rows(const void* x, int64_t x_stride, int32_t dtype, int64_t n, 
  *   bias fp32 [N] or NULL
  *   out  [M, N] of type dtype, rows out_stride apart
  * The sum is exact (all values of int8 are served), so K is at most CC_PRODUCT_MAX_K; what follows is computed in 32 bits.
- * K = 0 gives the bias.  out has at most 2^40 elements.
+ * K = 0 gives the bias.  out has at most 2^38 elements.
  * Workspace: cc_product_i8_workspace_bytes(M, N, K), which may be 0.
  */
 #define CC_PRODUCT_MAX_K ((1 << 17) - 1)

@@ -17,7 +17,7 @@ namespace {
 static_assert(CC_SCAN_CHUNK == cc::kScanChunk, "the kernels keep states as the header says");
 static_assert(CC_F32 == cc::kF32 && CC_F16 == cc::kF16 && CC_BF16 == cc::kBF16, "element types");
 
-constexpr int64_t kMaxRow = 1 << 24, kMaxRows = 1 << 30, kMaxPositions = (int64_t)1 << 31, kMaxChannels = (int64_t)1 << 32, kMaxProduct = (int64_t)1 << 40;
+constexpr int64_t kMaxRow = 1 << 24, kMaxRows = 1 << 30, kMaxPositions = (int64_t)1 << 31, kMaxChannels = (int64_t)1 << 32, kMaxProduct = (int64_t)1 << 38;
 
 bool is_dtype(int d) { return d == CC_F32 || d == CC_F16 || d == CC_BF16; }
 uintptr_t below(int dtype) { return dtype == CC_F32 ? 3u : 1u; }

@@ -603,28 +603,38 @@ int64_t grad_blocks(int64_t n, int teams, int threads) {
     const int64_t need = (n + teams - 1) / teams, most = kGradBlocks * kBlock / threads;
     return need < most ? need : most;
 }
+// Rows of each part of a long row's sums, so that no part is empty.
+int64_t rows_of_part(int64_t n) { return (n + kLongParts - 1) / kLongParts; }
+// How many partial sums there are of a column.
+template <int VEC>
+int64_t partial_rows(int64_t n, int64_t D) {
+    if (n == 0) return 0;
+    if (D < VEC) return grad_blocks(n, kBlock / 8, kBlock);
+    int64_t count = 0;
+    by_length<VEC>(D, [&](auto team, auto) {
+        constexpr int TEAM = decltype(team)::value;
+        if constexpr (TEAM == 0) count = (n + rows_of_part(n) - 1) / rows_of_part(n);
+        else count = grad_blocks(n, threads_of(TEAM) / TEAM, threads_of(TEAM));
+    });
+    return count;
+}
 
 template <class S, class W>
 void launch_backward(GradArgs a, const NormBackwardCall& c, hipStream_t s) {
     constexpr int VEC = kVec<S>;
-    int64_t count = 0;
+    const int64_t count = partial_rows<VEC>(a.n, a.D);
     if (a.D < VEC) {
-        count = grad_blocks(a.n, kBlock / 8, kBlock);
         hipLaunchKernelGGL((norm_backward_kernel<S, W, 1, 8, 1>), dim3((unsigned)count), dim3(kBlock), 0, s, a);
     } else {
         by_length<VEC>(a.D, [&](auto team, auto k) {
             constexpr int TEAM = decltype(team)::value, K = decltype(k)::value;
             if constexpr (TEAM == 0) {
-                // parts of equal length, none of them empty
-                const int64_t rows = (a.n + kLongParts - 1) / kLongParts, parts = (a.n + rows - 1) / rows;
-                count = parts;
                 if (a.partial)
-                    hipLaunchKernelGGL((norm_columns_kernel<S>), dim3((unsigned)((a.D + kBlock * 4 - 1) / (kBlock * 4)), (unsigned)parts), dim3(kBlock), 0, s, a, rows);
+                    hipLaunchKernelGGL((norm_columns_kernel<S>), dim3((unsigned)((a.D + kBlock * 4 - 1) / (kBlock * 4)), (unsigned)count), dim3(kBlock), 0, s, a,
+                                       rows_of_part(a.n));
                 hipLaunchKernelGGL((norm_backward_long_kernel<S, W, VEC>), dim3((unsigned)blocks_for(a.n, 1, kLongBlock)), dim3(kLongBlock), 0, s, a);
             } else {
-                constexpr int threads = threads_of(TEAM), teams = threads / TEAM;
-                count = grad_blocks(a.n, teams, threads);
-                hipLaunchKernelGGL((norm_backward_kernel<S, W, VEC, TEAM, K>), dim3((unsigned)count), dim3(threads), 0, s, a);
+                hipLaunchKernelGGL((norm_backward_kernel<S, W, VEC, TEAM, K>), dim3((unsigned)count), dim3(threads_of(TEAM)), 0, s, a);
             }
         });
     }
@@ -692,12 +702,10 @@ hipError_t launch_quantize(const NormCall& c, hipStream_t s) {
     return hipGetLastError();
 }
 
-// A row of partial sums for every workgroup that leaves one: as many as grad_blocks gives for the type with the smaller team.
+// A row of partial sums for every workgroup that leaves one; the type is not known here, so for the one that has more.
 size_t norm_workspace_bytes(int64_t n, int64_t D) {
-    int64_t threads = kBlock;
-    while (threads < 512 && D > threads * 16) threads *= 2;
-    const int64_t most = D > 16384 ? kLongParts : kGradBlocks * kBlock / threads;
-    return (size_t)(((n < most ? n : most) * D * 4 + 255) / 256 * 256);
+    const int64_t wide = partial_rows<kVec<_Float16>>(n, D), narrow = partial_rows<kVec<float>>(n, D);
+    return (size_t)(((wide > narrow ? wide : narrow) * D * 4 + 255) / 256 * 256);
 }
 
 hipError_t launch_norm_backward(const NormBackwardCall& c, hipStream_t s) {

@@ -68,6 +68,9 @@ struct Elements {
     S v[16 / sizeof(S)];
 };
 
+// A launch's first dimension holds fewer than 2^32 threads: tiles beyond kAcross go to the third.
+constexpr uint32_t kAcross = 1 << 20;
+
 // Workgroups of one XCD (every eighth) get neighbouring tiles, and those in blocks of 8 rows of tiles, so that what they read at the
 // same time is shared in its L2.
 __device__ __forceinline__ void tile_of(uint32_t id, int tiles_m, int tiles_n, int& tm, int& tn) {
@@ -103,8 +106,10 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 
     const int thread = threadIdx.x, lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64);
     const int wm = wave / (BN / WN), wn = wave % (BN / WN);
+    const uint32_t id = blockIdx.z * kAcross + blockIdx.x;
+    if (id >= (uint32_t)a.tiles_m * a.tiles_n) return;
     int tm, tn;
-    tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
+    tile_of(id, a.tiles_m, a.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * BM;
     const int n0 = tn * BN;
     const int8_t* const xbase = a.x + m0 * a.x_stride;
@@ -450,11 +455,17 @@ void launch_few(const Args& a, int64_t waves, hipStream_t s) {
     hipLaunchKernelGGL((few_kernel<S, MT, NT>), dim3((unsigned)((places + per - 1) / per)), dim3(kFewWaves * 64), 0, s, a, share);
 }
 
+// Counts a result's tiles and gives the grid that has them.
+dim3 tile_grid(Args& a, int bm, int bn, int stretches) {
+    a.tiles_m = (int)((a.M + bm - 1) / bm);
+    a.tiles_n = (a.N + bn - 1) / bn;
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+    return dim3((unsigned)(tiles < kAcross ? tiles : kAcross), (unsigned)stretches, (unsigned)((tiles + kAcross - 1) / kAcross));
+}
+
 template <class S, int BM, int BN, int WM, int WN, int STEP, int RING>
 void launch_tiles(Args a, bool direct, int stretches, hipStream_t s) {
-    a.tiles_m = (int)((a.M + BM - 1) / BM);
-    a.tiles_n = (a.N + BN - 1) / BN;
-    const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n), (unsigned)stretches), block((BM / WM) * (BN / WN) * 64);
+    const dim3 grid = tile_grid(a, BM, BN, stretches), block((BM / WM) * (BN / WN) * 64);
     if (direct) hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, STEP, RING, kRowsDirect>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, 128, 2, kRowsHeld>), grid, block, 0, s, a);
 }
@@ -488,9 +499,8 @@ void run(const Args& a, void* workspace, hipStream_t s) {
         else a.M <= 16 ? launch_few<S, 1, 1>(a, 2048, s) : launch_few<S, 2, 1>(a, 2048, s);
     } else if (far) {
         Args b = a;
-        b.tiles_m = (int)((a.M + 63) / 64);
-        b.tiles_n = (a.N + 63) / 64;
-        hipLaunchKernelGGL((tile_kernel<S, 64, 64, 32, 32, 128, 2, kRowsFar>), dim3((unsigned)((int64_t)b.tiles_m * b.tiles_n)), dim3(256), 0, s, b);
+        const dim3 grid = tile_grid(b, 64, 64, 1);
+        hipLaunchKernelGGL((tile_kernel<S, 64, 64, 32, 32, 128, 2, kRowsFar>), grid, dim3(256), 0, s, b);
     } else if (stretches > 1) {
         Args b = a;
         b.out = workspace;

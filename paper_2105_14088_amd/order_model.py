@@ -11,6 +11,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
+from . import binding as _binding
 from .binding import _check, _dev, _new, _stream, lib
 
 CC_MEAN_TOKENS, CC_MEAN_ORDERS = 0, 1
@@ -87,7 +88,9 @@ def _workspace(workspace: Optional[torch.Tensor], nbytes: int, device, stream):
     if workspace is None:
         if nbytes == 0:
             return None, None, 0
-        workspace = _new(nbytes, torch.uint8, device, stream)
+        workspace = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)     # as _new, and 0.5 us shorter
+        if stream is not None:
+            workspace.record_stream(stream)
         return workspace, workspace.data_ptr(), nbytes
     return workspace, _dev(workspace, torch.uint8, "workspace"), workspace.numel()
 
@@ -377,6 +380,14 @@ def _each_row(t: Optional[torch.Tensor], x: torch.Tensor, stream, name: str):
     return t, _plain(t, x.shape[:-1], torch.float32, name)
 
 
+def _stream_at(t: torch.Tensor, stream) -> int:
+    """The stream's handle.  A kernel is launched on the current device: on a tensor of another it would read what may not be there."""
+    current = torch.cuda.current_device() if _binding._current_device is None else _binding._current_device()
+    if t.get_device() != current:
+        raise ValueError("tensors must be on the current device")
+    return _stream(stream)
+
+
 _NOWHERE = (None, 0)
 
 
@@ -436,7 +447,7 @@ def cc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual
     if save_rstd or rstd is not None:
         rstd, rstd_to = _each_row(rstd, x, stream, "rstd")
     _check(lib().cc_rms_norm(*x_at, *residual_at, code, n, d, *_weight(weight, d, dtype, "weight"), eps, *sum_to, *out_to, *q_to,
-                             scale_to, rstd_to, _stream(stream)), "cc_rms_norm")
+                             scale_to, rstd_to, _stream_at(x, stream)), "cc_rms_norm")
     return RmsNorm(out, x if sum is None else sum, q, scale, rstd)
 
 
@@ -469,7 +480,7 @@ def cc_rms_norm_backward(grad_out: torch.Tensor, h: torch.Tensor, rstd: torch.Te
         held, ws, nbytes = _workspace(workspace, _norm_bytes(n, d), device, stream)
     _check(lib().cc_rms_norm_backward(*grad_at, *h_at, code, n, d, *_weight(weight, d, dtype, "weight"),
                                       _plain(rstd, shape[:-1], torch.float32, "rstd"), *sum_at, *grad_h_to, to, to_code,
-                                      1 if accumulate else 0, ws, nbytes, _stream(stream)), "cc_rms_norm_backward")
+                                      1 if accumulate else 0, ws, nbytes, _stream_at(h, stream)), "cc_rms_norm_backward")
     return grad_h, grad_weight
 
 
@@ -482,7 +493,7 @@ def cc_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: O
     x_at = _rows(x, shape, x.dtype, "x")
     q, q_to = _rows_like(q, x, torch.int8, stream, "q")
     scale, scale_to = _each_row(scale, x, stream, "scale")
-    _check(lib().cc_quantize_rows(*x_at, code, x.numel() // d if d else 0, d, *q_to, scale_to, _stream(stream)), "cc_quantize_rows")
+    _check(lib().cc_quantize_rows(*x_at, code, x.numel() // d if d else 0, d, *q_to, scale_to, _stream_at(x, stream)), "cc_quantize_rows")
     return q, scale
 
 
@@ -514,7 +525,7 @@ def cc_product_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_sca
     L = lib()
     held, ws, nbytes = _workspace(workspace, _product_bytes(m, n, k), x.device, stream)
     _check(L.cc_product_i8(*x_at, _plain(x_scale, lead, torch.float32, "x_scale"), *w_at, _plain(w_scale, (n,), torch.float32, "w_scale"),
-                           _plain(bias, (n,), torch.float32, "bias"), m, n, k, *out_to, code, ws, nbytes, _stream(stream)),
+                           _plain(bias, (n,), torch.float32, "bias"), m, n, k, *out_to, code, ws, nbytes, _stream_at(x, stream)),
            "cc_product_i8")
     return out
 
@@ -568,7 +579,7 @@ def cc_shape_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None
     `out` may be the logits."""
     args = _shape_args(logits, history, lengths, penalties, starts, bias, allowed)
     out, to = _logits_like(out, logits, stream, "out")
-    _check(lib().cc_shape_logits(*args, *to, _stream(stream)), "cc_shape_logits")
+    _check(lib().cc_shape_logits(*args, *to, _stream_at(logits, stream)), "cc_shape_logits")
     return out
 
 
@@ -581,6 +592,6 @@ def cc_shape_logits_backward(grad_out: torch.Tensor, logits: torch.Tensor, histo
     grad_out."""
     args = _shape_args(logits, history, lengths, penalties, starts, bias, allowed)
     grad_logits, to = _logits_like(grad_logits, logits, stream, "grad_logits")
-    _check(lib().cc_shape_logits_backward(*_strided(grad_out, logits.shape, logits.dtype, "grad_out"), *args, *to, _stream(stream)),
+    _check(lib().cc_shape_logits_backward(*_strided(grad_out, logits.shape, logits.dtype, "grad_out"), *args, *to, _stream_at(logits, stream)),
            "cc_shape_logits_backward")
     return grad_logits

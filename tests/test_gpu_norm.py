@@ -256,3 +256,19 @@ def test_the_same_bits_again():
         first = cc.cc_rms_norm_backward(go, x, rstd, w)
         for _ in range(3):
             assert all(torch.equal(a, b) for a, b in zip(first, cc.cc_rms_norm_backward(go, x, rstd, w)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("dim", [5, 64, 513, 1025, 1500, 2048, 2049, 4097, 8193, 16384, 16400])
+def test_a_workspace_is_as_large_as_it_says(dim, dtype):
+    """What lies right behind it stays: with so many rows that every workgroup there can be leaves its sums."""
+    say(f"norm workspace {dim} {dtype}")
+    n = 9000 if dim <= 2049 else 3000
+    h, go, w = made(n, dim, dtype), made(n, dim, dtype, 1), made(1, dim, F32, 2)[0]
+    rstd = cc.cc_rms_norm(h, w, save_rstd=True, normed=False).rstd
+    need = cc.cc_rms_norm_workspace_bytes(n, dim)
+    room = torch.full((need + (32 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+    got = cc.cc_rms_norm_backward(go, h, rstd, w, workspace=room[:need])
+    assert (room[need:] == 0x5A).all()
+    want = cc.cc_rms_norm_backward(go, h, rstd, w)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

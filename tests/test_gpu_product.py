@@ -137,3 +137,16 @@ def test_the_same_bits_again():
         first = cc.cc_product_i8(*args, dtype=F32)
         for _ in range(3):
             assert torch.equal(first, cc.cc_product_i8(*args, dtype=F32))
+
+
+@pytest.mark.parametrize("m,n,k", [(64, 64, 2048), (33, 1000, 4100), (300, 301, 9001)])
+def test_a_workspace_is_as_large_as_it_says(m, n, k):
+    say(f"product workspace {m} {n} {k}")
+    args = case(m, n, k)
+    need = cc.cc_product_i8_workspace_bytes(m, n, k)
+    assert need > 0
+    room = torch.full((need + (16 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+    got = cc.cc_product_i8(*args, workspace=room[:need])
+    assert (room[need:] == 0x5A).all() and torch.equal(got, cc.cc_product_i8(*args))
+    with pytest.raises(cc.CCError):
+        cc.cc_product_i8(*args, workspace=room[:need - 256])

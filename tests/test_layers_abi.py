@@ -138,3 +138,16 @@ def test_binding_refuses_what_it_cannot_describe():
         cc.cc_shape_logits(x)
     with pytest.raises(ValueError, match="GPU"):
         cc.cc_shape_logits(x[None])
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    import types
+
+    from paper_2105_14088_amd import binding, order_model
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_current_raw_stream", lambda device: 100 + device)
+    assert order_model._stream_at(types.SimpleNamespace(get_device=lambda: 0), None) == 100
+    with pytest.raises(ValueError, match="current device"):
+        order_model._stream_at(types.SimpleNamespace(get_device=lambda: 1), None)
+    with pytest.raises(ValueError, match="current device"):
+        order_model._stream_at(types.SimpleNamespace(get_device=lambda: 1), types.SimpleNamespace(cuda_stream=5))
