@@ -26,7 +26,7 @@ constexpr float kInf = __builtin_inff();
 constexpr uint32_t kSeen = 1u << 31;
 constexpr int kShortRow = 2048;
 constexpr int kThreads = 256;
-constexpr int kStretch = 4096;           // 8192 a workgroup or 16384 of 1024 threads: 1 to 4 us more of 23 (128 rows of 131072, 4096 entries)
+constexpr int kEach = 16;                // elements of a thread in a stretch of a long row
 
 struct Args {
     const void *logits, *grad;           // grad: backward only
@@ -257,17 +257,17 @@ __global__ __launch_bounds__(kThreads) void short_kernel(const Args a) {
 }
 
 // A stretch of a row.  A vector that would end beyond the row is taken element by element.
-template <class S, bool BACK, bool COUNT>
-__global__ __launch_bounds__(kThreads) void long_kernel(const Args a) {
-    constexpr int VEC = 16 / sizeof(S), K = kStretch / kThreads / VEC;
-    __shared__ __attribute__((aligned(16))) uint32_t count[COUNT ? kStretch : 1];
+template <class S, int THREADS, bool BACK, bool COUNT>
+__global__ __launch_bounds__(THREADS) void long_kernel(const Args a) {
+    constexpr int VEC = 16 / sizeof(S), K = kEach / VEC, STRETCH = kEach * THREADS;
+    __shared__ __attribute__((aligned(16))) uint32_t count[COUNT ? STRETCH : 1];
     const int64_t unit = workgroup();
     if (unit >= a.units) return;
     const int64_t row = quotient(unit, a.per_row), b = quotient(row, a.T), t = row - b * a.T;
     // Every eighth workgroup is on the same XCD, and the first stretch often has most of a history: rows begin at another each.
     int turned = (int)(unit - row * a.per_row) + (int)((uint32_t)row % (uint32_t)a.per_row);
     if (turned >= a.per_row) turned -= a.per_row;
-    const int from = turned * kStretch, width = min(kStretch, a.V - from);
+    const int from = turned * STRETCH, width = min(STRETCH, a.V - from);
     const float one[3] = {1.0f, 0.0f, 0.0f};
     const Penalties pen(COUNT ? a.penalties + 3 * b : one);
     const bool plain = !COUNT || pen.only;
@@ -278,12 +278,12 @@ __global__ __launch_bounds__(kThreads) void long_kernel(const Args a) {
     const uint32_t* const allowed = a.allowed ? a.allowed + b * a.allowed_sb + t * a.allowed_st + from / 32 : nullptr;
 
     if constexpr (COUNT) {
-        const int words = plain ? kStretch / 32 : kStretch;
-        for (int i = threadIdx.x * 4; i < words; i += kThreads * 4) *(Pack<float, 4>*)(count + i) = Pack<float, 4>();
+        const int words = plain ? STRETCH / 32 : STRETCH;
+        for (int i = threadIdx.x * 4; i < words; i += THREADS * 4) *(Pack<float, 4>*)(count + i) = Pack<float, 4>();
         __syncthreads();
         const int64_t n = (a.lengths ? a.lengths[b] : 0) + t;
         const int start = a.starts ? a.starts[b] : 0;
-        look_back(a.history + b * a.history_stride, (int)min(max(n, (int64_t)0), a.L), start, from, width, threadIdx.x, kThreads, count, plain);
+        look_back(a.history + b * a.history_stride, (int)min(max(n, (int64_t)0), a.L), start, from, width, threadIdx.x, THREADS, count, plain);
         __syncthreads();
     }
     Pack<S, VEC> z[K] = {}, g[K] = {};
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(kThreads) void long_kernel(const Args a) {
     uint32_t live[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int in = (k * kThreads + threadIdx.x) * VEC;
+        const int in = (k * THREADS + threadIdx.x) * VEC;
         live[k] = ~0u;
         if (in + VEC <= width) {
             if (BACK) g[k] = load_pack<VEC>(grow + in);
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void long_kernel(const Args a) {
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int in = (k * kThreads + threadIdx.x) * VEC;
+        const int in = (k * THREADS + threadIdx.x) * VEC;
         if (in + VEC <= width) {
             live[k] &= ~banned(bias[k]);
             if (plain) {
@@ -348,9 +348,16 @@ void launch(Args a, int64_t B, hipStream_t s) {
         else if (a.V <= 256 * VEC) hipLaunchKernelGGL((short_kernel<S, VEC, 4, BACK, COUNT>), grid, dim3(kThreads), 0, s, a);
         else if constexpr (VEC == 4) hipLaunchKernelGGL((short_kernel<S, VEC, 8, BACK, COUNT>), grid, dim3(kThreads), 0, s, a);
     } else {
-        a.per_row = (a.V + kStretch - 1) / kStretch;
+        // Longer stretches go through the history less often, and are more for one workgroup to wait for: 128 rows of 131072 with 4096 entries
+        // 22.3 us with 256 threads, 21.6 with 512, 24 to 28 with 1024.
+        const int threads = COUNT && a.V > 16384 ? 512 : 256;
+        a.per_row = (a.V + kEach * threads - 1) / (kEach * threads);
         a.units = B * a.T * a.per_row;
-        hipLaunchKernelGGL((long_kernel<S, BACK, COUNT>), grid_of(a.units), dim3(kThreads), 0, s, a);
+        if (threads == 512) {
+            if constexpr (COUNT) hipLaunchKernelGGL((long_kernel<S, 512, BACK, COUNT>), grid_of(a.units), dim3(512), 0, s, a);
+        } else {
+            hipLaunchKernelGGL((long_kernel<S, 256, BACK, COUNT>), grid_of(a.units), dim3(256), 0, s, a);
+        }
     }
 }
 
