@@ -102,7 +102,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
     constexpr int STRIP = WIDE * (int)sizeof(S) + 16;               // a row of them
     static_assert(WAVES * WM * STRIP <= RING * BYTES, "they lie where the operands were");
     __shared__ __attribute__((aligned(128))) char lds[RING * BYTES];
-    __shared__ __attribute__((aligned(16))) float channel[2][BN];   // scales and biases
+    __shared__ __attribute__((aligned(16))) float channel[2][BN], row_scale[BM];    // channels' scales and biases, rows' scales
 
     const int thread = threadIdx.x, lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64);
     const int wm = wave / (BN / WN), wn = wave % (BN / WN);
@@ -115,13 +115,6 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
     const int8_t* const xbase = a.x + m0 * a.x_stride;
     const int8_t* const wbase = a.w + (int64_t)n0 * a.w_stride;
     const int last_m = (int)min((int64_t)BM, a.M - m0) - 1, last_n = min(BN, a.N - n0) - 1;
-    if constexpr (!std::is_same_v<S, int32_t>)
-        for (int i = thread; i < BN; i += THREADS) {
-            const int n = n0 + min(i, last_n);
-            channel[0][i] = a.w_scale[n];
-            channel[1][i] = a.bias ? a.bias[n] : 0.0f;
-        }
-
     // Where this thread's pieces come from: rows beyond the last are the last again, their results are not stored.
     // Piece p of wavefront `wave` fills LDS from (p * THREADS + wave * 64) * 16 on.
     const int in_row = (lane % ROW) ^ (thread / ROW / SHARE % ROW);
@@ -205,6 +198,15 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 #pragma unroll
     for (int r = 1; r < RING; ++r) fetch_all(t0 + r, r);
     if (starts_partial) fetch_partial();
+    // behind the first tiles' loads, and not where they are used: each would be waited for by itself
+    if constexpr (!std::is_same_v<S, int32_t>) {
+        for (int i = thread; i < BN; i += THREADS) {
+            const int n = n0 + min(i, last_n);
+            channel[0][i] = a.w_scale[n];
+            channel[1][i] = a.bias ? a.bias[n] : 0.0f;
+        }
+        for (int i = thread; i < BM; i += THREADS) row_scale[i] = a.x_scale[m0 + min(i, last_m)];
+    }
     if (MODE == kRowsDirect && !starts_partial && t0 + RING - 1 < tiles)
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((RING - 1) * PIECES) : "memory");
     else arrive(false);
@@ -265,7 +267,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
     S* const out = (S*)a.out + (std::is_same_v<S, int32_t> ? blockIdx.y * a.M * a.out_stride : 0);
     float xs[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) xs[i] = std::is_same_v<S, int32_t> ? 0.0f : a.x_scale[min(mw + i * 32 + lane % 32, a.M - 1)];
+    for (int i = 0; i < MT; ++i) xs[i] = std::is_same_v<S, int32_t> ? 0.0f : row_scale[wm * WM + i * 32 + lane % 32];
 #pragma unroll
     for (int j0 = 0; j0 < NT; j0 += WIDE / 32) {
         const int nw = wn * WN + j0 * 32;
@@ -364,7 +366,19 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int s
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) sum[i][j] = Int4{0, 0, 0, 0};
+    // A lane has channels 4 (lane / 16) .. + 3 of row lane % 16.  Their scales are on their way while the sums are made.
+    float ws[NT][4], bias[NT][4], xs[MT];
     if (n0 < a.N) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t c = min(n0 + j * 16 + lane / 16 * 4 + r, (int64_t)a.N - 1);
+                ws[j][r] = a.w_scale[c];
+                bias[j][r] = a.bias ? a.bias[c] : 0.0f;
+            }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xs[i] = a.x_scale[min((int64_t)i * 16 + lane % 16, a.M - 1)];
         const int8_t *wrow[NT], *xrow[MT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) wrow[j] = a.w + min(n0 + j * 16 + lane % 16, (int64_t)a.N - 1) * a.w_stride;
@@ -414,27 +428,18 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int s
 #pragma unroll
                 for (int j = 0; j < NT; ++j) sum[i][j] += parts[wave + p][i * NT + j][lane];
     }
-    // a lane has channels 4 (lane / 16) .. + 3 of row lane % 16
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int64_t n = n0 + j * 16 + lane / 16 * 4;
         if (n >= a.N) continue;
-        float ws[4], bias[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t c = min(n + r, (int64_t)a.N - 1);
-            ws[r] = a.w_scale[c];
-            bias[r] = a.bias ? a.bias[c] : 0.0f;
-        }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int64_t m = i * 16 + lane % 16;
             if (m >= a.M) continue;
-            const float xs = a.x_scale[m];
             S* const to = (S*)a.out + m * a.out_stride + n;
             float f[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) f[r] = scaled(sum[i][j][r], xs, ws[r], bias[r]);
+            for (int r = 0; r < 4; ++r) f[r] = scaled(sum[i][j][r], xs[i], ws[j][r], bias[j][r]);
             if (n + 4 <= a.N) {
                 store_pack(to, Pack<S, 4>::from(f));
             } else {

@@ -46,6 +46,8 @@ def _plain(t: Optional[torch.Tensor], shape, dtype, name: str) -> Optional[int]:
     """Where a contiguous tensor lies, or None for none."""
     if t is None:
         return None
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}")
     return _dev(t, dtype, name)
@@ -385,6 +387,8 @@ def _stream_at(t: torch.Tensor, stream) -> int:
     current = torch.cuda.current_device() if _binding._current_device is None else _binding._current_device()
     if t.get_device() != current:
         raise ValueError("tensors must be on the current device")
+    if stream is None and _binding._current_raw_stream is not None:
+        return _binding._current_raw_stream(current)
     return _stream(stream)
 
 
