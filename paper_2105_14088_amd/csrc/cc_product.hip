@@ -146,18 +146,28 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) fetch(p, t, buffer);
     };
+    // The first tile, where K ends inside it: pieces that a row has all of come like others.
     const auto fetch_partial = [&] {
+        const int k = whole * STEP + in_row * kPiece;
         constexpr int U = PIECES > 8 ? 4 : PIECES;
+        if (MODE == kRowsDirect && k + kPiece <= a.K) {
 #pragma unroll
-        for (int p = 0; p < PIECES; p += U) {
-            Int4 v[U];
+            for (int p = 0; p < PIECES; ++p) fetch(p, all, 0);
+        } else if (MODE == kRowsDirect && k >= a.K) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int8_t* const row = p + u < XPIECES ? xbase + row_of(p + u) * a.x_stride : wbase + row_of(p + u) * a.w_stride;
-                v[u] = load_piece(row, whole * STEP + in_row * kPiece, a.K);
+            for (int p = 0; p < PIECES; ++p) put(p, 0, Int4{0, 0, 0, 0});
+        } else {
+#pragma unroll
+            for (int p = 0; p < PIECES; p += U) {
+                Int4 v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int8_t* const row = p + u < XPIECES ? xbase + row_of(p + u) * a.x_stride : wbase + row_of(p + u) * a.w_stride;
+                    v[u] = load_piece(row, k, a.K);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) put(p + u, 0, v[u]);
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u) put(p + u, 0, v[u]);
         }
     };
     const auto put_held = [&](int buffer) {
