@@ -63,6 +63,13 @@ __device__ __forceinline__ Int4 load_piece(const int8_t* row, int k, int K) {
 // From the exact sum on in 32 bits: it is rounded, and so is each product and the sum with the bias.
 __device__ __forceinline__ float scaled(int sum, float xs, float ws, float bias) { return (float)sum * xs * ws + bias; }
 
+// An address that all lanes have, in scalar registers.
+__device__ __forceinline__ const int8_t* scalar(const int8_t* p) {
+    const uint64_t v = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const int8_t*)((uint64_t)hi << 32 | lo);
+}
+
 template <class S>
 struct Elements {
     S v[16 / sizeof(S)];
@@ -126,25 +133,29 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 #pragma unroll
     for (int p = 0; p < PIECES; ++p)
         from[p] = (decltype(from[0] + 0))row_of(p) * (decltype(from[0] + 0))(p < XPIECES ? a.x_stride : a.w_stride) + in_row * kPiece;
-    Int4 held[MODE == kRowsDirect ? 1 : PIECES];
+    // Tiles on their way through registers: two where there is room, as a tile of LDS alone leaves loads too little time.
+    constexpr int HOLD = MODE == kRowsDirect || PIECES > 8 ? 1 : 2;
+    Int4 held[HOLD][MODE == kRowsDirect ? 1 : PIECES];
     const auto put = [&](int p, int buffer, const Int4& v) { *(Int4*)(lds + buffer * BYTES + (p * THREADS + thread) * kPiece) = v; };
     // The sum does not depend on the order of its terms: where K ends inside a tile, that tile is the first, so that only the start has to
     // look at where a row ends.
     const int whole = a.K / STEP, partial = a.K % STEP != 0, all = whole + partial;
     const int t0 = (int)((int64_t)all * blockIdx.y / gridDim.y), tiles = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y);
-    const auto fetch = [&](int p, int t, int buffer) {
+    const auto fetch = [&](int p, int t, int buffer, int set) {
         const int8_t* const base = (p < XPIECES ? xbase : wbase) + (int64_t)(t - partial) * STEP;
         if constexpr (MODE == kRowsDirect) {
             const uint32_t to = (uint32_t)(uintptr_t)lds + buffer * BYTES + wave * 1024 + p * THREADS * kPiece;
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(from[p]), "s"(base) : "memory");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :
+                         : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from[p]), "s"(scalar(base)) : "memory");
         } else {
-            __builtin_memcpy(&held[p], base + from[p], kPiece);
+            __builtin_memcpy(&held[set][p], base + from[p], kPiece);
         }
     };
-    const auto fetch_all = [&](int t, int buffer) {
+    const auto fetch_all = [&](int t, int buffer, int set) {
         if (t >= tiles) return;
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) fetch(p, t, buffer);
+        for (int p = 0; p < PIECES; ++p) fetch(p, t, buffer, set);
     };
     // The first tile, where K ends inside it: pieces that a row has all of come like others.
     const auto fetch_partial = [&] {
@@ -152,7 +163,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         constexpr int U = PIECES > 8 ? 4 : PIECES;
         if (MODE == kRowsDirect && k + kPiece <= a.K) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) fetch(p, all, 0);
+            for (int p = 0; p < PIECES; ++p) fetch(p, all, 0, 0);
         } else if (MODE == kRowsDirect && k >= a.K) {
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) put(p, 0, Int4{0, 0, 0, 0});
@@ -170,16 +181,17 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
             }
         }
     };
-    const auto put_held = [&](int buffer) {
+    const auto put_held = [&](int buffer, int set) {
         if constexpr (MODE != kRowsDirect) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) put(p, buffer, held[p]);
+            for (int p = 0; p < PIECES; ++p) put(p, buffer, held[set][p]);
         }
     };
     // Tile t + 1 is in LDS, for every wavefront, and nobody reads tile t there any more; the RING - 2 after it may still be on their way.
     const auto arrive = [&](bool later) {
         if (RING > 2 && later) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((RING - 2) * PIECES) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else if (MODE == kRowsDirect) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // held tiles stay on their way
     };
 
     Int16 sum[MT][NT];
@@ -200,13 +212,15 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(operand[set][MT + j], operand[set][i], sum[i][j], 0, 0, 0);
     };
 
+    // Tile t0 + r is fetched for buffer r, or into set (r - 1) % HOLD once tile t0 has been put from set 0.
     const bool starts_partial = t0 < partial;
     if (!starts_partial) {
-        fetch_all(t0, 0);
-        put_held(0);
+        fetch_all(t0, 0, 0);
+        put_held(0, 0);
     }
+    constexpr int AHEAD = MODE == kRowsDirect ? RING : HOLD + 1;      // tiles that are in LDS or on their way
 #pragma unroll
-    for (int r = 1; r < RING; ++r) fetch_all(t0 + r, r);
+    for (int r = 1; r < AHEAD; ++r) fetch_all(t0 + r, r, (r - 1) % HOLD);
     if (starts_partial) fetch_partial();
     // behind the first tiles' loads, and not where they are used: each would be waited for by itself
     if constexpr (!std::is_same_v<S, int32_t>) {
@@ -229,8 +243,10 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
     if (t0 < tiles) {
 #pragma unroll
         for (int o = 0; o < MT + NT; ++o) read(o, 0, 0);
-        int now = 0;
-        for (int t = t0; t < tiles; ++t) {
+        // Tile t lies in buffer `now`, the next is put from set `set`.  `steady`: there are AHEAD more.  Asked at every tile, that would be a branch
+        // behind which the compiler waits for all loads where some would do.
+        const auto tile = [&](int t, int now, int set, auto steady) {
+            constexpr bool STEADY = decltype(steady)::value;
             const int next = now + 1 == RING ? 0 : now + 1;
 #pragma unroll
             for (int s = 0; s < PARTS - 1; ++s)
@@ -248,9 +264,9 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
 #pragma unroll
             for (int q = 0; q < BEFORE; ++q) multiply(1, q);
             __builtin_amdgcn_sched_barrier(0);
-            if (t + 1 < tiles) put_held(next);
-            arrive(t + RING - 1 < tiles);
-            const bool more = t + RING < tiles;
+            if (STEADY || t + 1 < tiles) put_held(next, set);
+            arrive(STEADY || t + RING - 1 < tiles);
+            const bool more = STEADY || t + AHEAD < tiles;
 #pragma unroll
             for (int q = BEFORE; q < PRODUCTS; ++q) {
                 multiply(1, q);
@@ -261,11 +277,31 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
                 if (more) {
 #pragma unroll
                     for (int p = 0; p < PIECES; ++p)
-                        if (BEFORE + p * (PRODUCTS - BEFORE) / PIECES == q) fetch(p, t + RING, now);
+                        if (BEFORE + p * (PRODUCTS - BEFORE) / PIECES == q) fetch(p, t + AHEAD, now, set);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            now = next;
+        };
+        int t = t0;
+        if constexpr (HOLD == 2) {
+            for (; t + 1 + AHEAD < tiles; t += 2) {
+                tile(t, 0, 0, std::true_type());
+                tile(t + 1, 1, 1, std::true_type());
+            }
+            for (; t < tiles; t += 2) {
+                tile(t, 0, 0, std::false_type());
+                if (t + 1 < tiles) tile(t + 1, 1, 1, std::false_type());
+            }
+        } else {
+            int now = 0;
+            for (; t + AHEAD < tiles; ++t) {
+                tile(t, now, 0, std::true_type());
+                now = now + 1 == RING ? 0 : now + 1;
+            }
+            for (; t < tiles; ++t) {
+                tile(t, now, 0, std::false_type());
+                now = now + 1 == RING ? 0 : now + 1;
+            }
         }
     }
 
