@@ -542,8 +542,8 @@ int stretches_of(int64_t M, int64_t N, int64_t K) {
 
 template <class S>
 void run(const Args& a, void* workspace, hipStream_t s) {
-    // of a tile's rows the farthest is addressed by 32 bits from its first
-    const bool far = a.x_stride >= 1 << 24 || a.w_stride >= 1 << 24;
+    // of a tile's 256 rows the farthest is addressed by 31 bits from its first
+    const bool far = a.x_stride >= 1 << 23 || a.w_stride >= 1 << 23;
     const bool direct = !far && rows_at_16(a.x, a.x_stride) && rows_at_16(a.w, a.w_stride);
     const int stretches = stretches_of(a.M, a.N, a.K);
     if (a.M <= kFewRows) {

@@ -106,6 +106,20 @@ def test_rows_far_apart():
     assert torch.equal(cc.cc_product_i8(far[:, 16:16 + k], xs, w, ws, b), cc.cc_product_i8(x, xs, w, ws, b))
 
 
+@pytest.mark.parametrize("apart", [(1 << 23) - 16, (1 << 23) - 1, 1 << 23])
+@pytest.mark.parametrize("which", ["x", "w"])
+def test_rows_of_a_large_tile_apart(which, apart):
+    """256 rows of a tile whose offsets just fit into 31 bits, straight and through registers, and those that do not."""
+    say(f"product large tile apart {which} {apart}")
+    m, n, k = (2048, 8192, 640) if which == "x" else (8192, 2048, 640)
+    x, xs, w, ws, b = case(m, n, k)
+    want = cc.cc_product_i8(x, xs, w, ws, b, dtype=BF16)
+    rows = torch.empty(2048 * apart, device="cuda", dtype=torch.int8).view(2048, apart)[:, 16:16 + k]
+    rows.copy_(x if which == "x" else w)
+    got = cc.cc_product_i8(rows, xs, w, ws, b, dtype=BF16) if which == "x" else cc.cc_product_i8(x, xs, rows, ws, b, dtype=BF16)
+    assert torch.equal(got, want)
+
+
 def test_undefined_rows_stay_theirs():
     for m, n, k in ((5, 40, 64), (90, 40, 64)):
         x, xs, w, ws, b = case(m, n, k)
