@@ -6,7 +6,7 @@
 // how it is cut.  Terms beyond K are zeros that are put where a tile ends inside a row; nothing beyond a row is read.
 //
 // tile_kernel: a workgroup has a tile of the result and goes along K in steps of 128 bytes.  Both operands come to LDS in pieces of 16
-// bytes, straight from memory where rows allow it (16-byte alignment), through registers else.  In LDS a row has 8 such pieces,
+// bytes, straight from memory where all rows begin at words of 4 bytes (4096 x 4096 x 4004: 77 us, 90 through registers), through registers else.  In LDS a row has 8 such pieces,
 // and piece c lies at place c ^ (row / 2 % 8): the lanes that read the same piece of 16 rows then use all 64 banks once.  Two to
 // four tiles are held: while one is multiplied, others are on their way.
 //
@@ -36,6 +36,7 @@ struct Args {
     int N, K;
     void* out;
     int tiles_m, tiles_n;
+    bool bytes;                          // some row does not begin at a word of 4 bytes
 };
 
 // 16 bytes of a row from k on; what lies beyond K is zero and not read.  Where they end beyond the row, its last 16 are read and shifted.
@@ -57,6 +58,61 @@ __device__ __forceinline__ Int4 load_piece(const int8_t* row, int k, int K) {
         }
     }
     return __builtin_bit_cast(Int4, v);
+}
+
+// A load of 16 bytes that does not begin at a word takes far longer than one that does (8 x 50001 x 1001: 22 us, x 1004 13): such a piece is read as
+// the five words that it lies in, and `by` bytes of the first are shifted out (16 us).  At a row's ends, where a word has bytes that are not the row's, the piece is read as it lies, by = 0.
+struct Whole {
+    Int4 v;
+    __device__ __forceinline__ Int4 get() const { return v; }
+};
+struct Words {
+    Int4 v;
+    uint32_t next, by;
+    __device__ __forceinline__ Int4 get() const {
+        return Int4{(int)__builtin_amdgcn_alignbyte(v[1], v[0], by), (int)__builtin_amdgcn_alignbyte(v[2], v[1], by),
+                    (int)__builtin_amdgcn_alignbyte(v[3], v[2], by), (int)__builtin_amdgcn_alignbyte(next, v[3], by)};
+    }
+};
+__device__ __forceinline__ uint32_t beyond_word(const void* p) { return (uint32_t)(uintptr_t)p & 3u; }
+// The piece at p, of which `by` bytes are shifted out: 0, or as many as p is beyond a word.  `more`: there is a fifth word to read.
+__device__ __forceinline__ Words load_words(const int8_t* p, uint32_t by, bool more) {
+    Words w;
+    p -= by;
+    __builtin_memcpy(&w.v, p, kPiece);
+    __builtin_memcpy(&w.next, p + (more ? kPiece : kPiece - 4), 4);
+    w.by = by;
+    return w;
+}
+// Any piece of a row, as load_piece, without a branch: K >= 16.
+template <class Part>
+struct Clipped {
+    Part part;
+    int beyond;                          // bytes before the piece, which are shifted out as well
+    __device__ __forceinline__ Int4 get() const {
+        typedef uint64_t Long2 __attribute__((ext_vector_type(2)));
+        Long2 v = __builtin_bit_cast(Long2, part.get());
+        const int shift = (beyond & 7) * 8;
+        if (beyond & 8) v = Long2{v[1], 0};
+        v = Long2{v[0] >> shift | v[1] << 1 << (63 - shift), v[1] >> shift};
+        if (beyond >= kPiece) v = Long2{0, 0};
+        return __builtin_bit_cast(Int4, v);
+    }
+};
+__device__ __forceinline__ Whole load_whole(const int8_t* p) {
+    Whole v;
+    __builtin_memcpy(&v.v, p, kPiece);
+    return v;
+}
+__device__ __forceinline__ Clipped<Whole> load_clipped(const int8_t* row, int k, int K) {
+    const int at = min(k, K - kPiece);
+    return {load_whole(row + at), min(k - at, kPiece)};
+}
+__device__ __forceinline__ Clipped<Words> load_clipped_words(const int8_t* row, int k, int K) {
+    const int at = min(k, K - kPiece);
+    const uint32_t by = beyond_word(row + at);
+    const bool inside = at >= (int)by && at - (int)by + kPiece + 4 <= K;
+    return {load_words(row + at, inside ? by : 0, inside), min(k - at, kPiece)};
 }
 
 // From the exact sum on in 32 bits: it is rounded, and so is each product and the sum with the bias.
@@ -172,14 +228,17 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
         } else {
 #pragma unroll
             for (int p = 0; p < PIECES; p += U) {
-                Int4 v[U];
+                const auto row = [&](int u) { return p + u < XPIECES ? xbase + row_of(p + u) * a.x_stride : wbase + row_of(p + u) * a.w_stride; };
+                if (a.K < kPiece) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int8_t* const row = p + u < XPIECES ? xbase + row_of(p + u) * a.x_stride : wbase + row_of(p + u) * a.w_stride;
-                    v[u] = load_piece(row, k, a.K);
+                    for (int u = 0; u < U; ++u) put(p + u, 0, load_piece(row(u), k, a.K));
+                } else {
+                    Clipped<Words> v[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) v[u] = load_clipped_words(row(u), k, a.K);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) put(p + u, 0, v[u].get());
                 }
-#pragma unroll
-                for (int u = 0; u < U; ++u) put(p + u, 0, v[u]);
             }
         }
     };
@@ -399,7 +458,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, const int32_t* 
     }
 }
 
-// Bound by memory: 8 x 50001 x 1024 13 us, 4.0 TB/s; 8 x 8192 x 8192 16 us, 4.2.  MT * 16 rows; NT * 16 channels to `share` wavefronts of a workgroup's 8, each of which has a stretch of K.  Weights are read once, the rows of x
+// Bound by memory: 8 x 50001 x 1024 13 us, 4.0 TB/s; 8 x 8192 x 8192 16 us, 4.2; with rows at any byte 8 x 50001 x 1001 17 us, 3.0.  MT * 16 rows; NT * 16 channels to `share` wavefronts of a workgroup's 8, each of which has a stretch of K.  Weights are read once, the rows of x
 // once for every NT * 16 channels.
 constexpr int kFewWaves = 8;
 template <class S, int MT, int NT>
@@ -434,9 +493,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int s
         for (int i = 0; i < MT; ++i) xrow[i] = a.x + min((int64_t)i * 16 + lane % 16, a.M - 1) * a.x_stride;
         const int in = lane / 16 * kPiece;
         constexpr int U = 8 / NT;
-        // U steps' loads in flight; `load` takes pieces that a row has all of, or any
-        const auto batch = [&](int s, int count, auto load) {
-            Int4 w[U][NT], x[U][MT];
+        // the loads of at most `most` steps in flight; `load` takes pieces that a row has all of, or any
+        const auto batch = [&](auto most, int s, int count, auto load) __attribute__((always_inline)) {
+            constexpr int U = decltype(most)::value;
+            decltype(load(wrow[0], 0)) w[U][NT], x[U][MT];
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -448,20 +508,43 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int s
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (u < count) {
+                    Int4 wv[NT];
 #pragma unroll
-                    for (int i = 0; i < MT; ++i)
+                    for (int j = 0; j < NT; ++j) wv[j] = w[u][j].get();
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][j], x[u][i], sum[i][j], 0, 0, 0);
+                    for (int i = 0; i < MT; ++i) {
+                        const Int4 xv = x[u][i].get();
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[j], xv, sum[i][j], 0, 0, 0);
+                    }
                 }
         };
-        const auto all_of = [](const int8_t* row, int k) {
-            Int4 v;
-            __builtin_memcpy(&v, row + k, kPiece);
-            return v;
-        };
         int s = begin;
-        for (; s + U <= end && (s + U) * 64 <= a.K; s += U) batch(s, U, all_of);
-        for (; s < end; s += U) batch(s, min(U, end - s), [&](const int8_t* row, int k) { return load_piece(row, k, a.K); });
+        if (a.K < kPiece) {
+            if (s < end) batch(std::integral_constant<int, 1>(), s, 1, [&](const int8_t* row, int k) { return Whole{load_piece(row, k, a.K)}; });
+        } else {
+            constexpr std::integral_constant<int, U> full;
+            // a step too many costs its loads (20 x 1000 x 333, six steps: 12 us with the loads of eight, 8 with those of six)
+            const auto some = [&](int s, int count, auto load) __attribute__((always_inline)) {
+                if (count * 4 <= U) batch(std::integral_constant<int, U / 4>(), s, count, load);
+                else if (count * 2 <= U) batch(std::integral_constant<int, U / 2>(), s, count, load);
+                else if (count * 4 <= U * 3) batch(std::integral_constant<int, U * 3 / 4>(), s, count, load);
+                else batch(full, s, min(count, U), load);
+            };
+            if (a.bytes) {
+                const auto words = [&](const int8_t* row, int k) { return load_clipped_words(row, k, a.K); };
+                if (s == 0) {
+                    some(s, end, words);
+                    s = U;
+                }
+                for (; s + U <= end && (s + U) * 64 + 4 <= a.K; s += U)
+                    batch(full, s, U, [](const int8_t* row, int k) { return load_words(row + k, beyond_word(row), true); });
+                for (; s < end; s += U) some(s, end - s, words);
+            } else {
+                for (; s + U <= end && (s + U) * 64 <= a.K; s += U) batch(full, s, U, [](const int8_t* row, int k) { return load_whole(row + k); });
+                for (; s < end; s += U) some(s, end - s, [&](const int8_t* row, int k) { return load_clipped(row, k, a.K); });
+            }
+        }
     }
     if (share > 1) {
 #pragma unroll
@@ -523,7 +606,6 @@ void launch_tiles(Args a, bool direct, int stretches, hipStream_t s) {
     else hipLaunchKernelGGL((tile_kernel<S, BM, BN, WM, WN, 128, 2, kRowsHeld>), grid, block, 0, s, a);
 }
 
-bool rows_at_16(const void* p, int64_t stride) { return ((uintptr_t)p & 15) == 0 && stride % 16 == 0; }
 int64_t tiles_of(int64_t M, int64_t N, int64_t side) { return ((M + side - 1) / side) * ((N + side - 1) / side); }
 
 constexpr int64_t kFewRows = 32;
@@ -544,7 +626,7 @@ template <class S>
 void run(const Args& a, void* workspace, hipStream_t s) {
     // of a tile's 256 rows the farthest is addressed by 31 bits from its first
     const bool far = a.x_stride >= 1 << 23 || a.w_stride >= 1 << 23;
-    const bool direct = !far && rows_at_16(a.x, a.x_stride) && rows_at_16(a.w, a.w_stride);
+    const bool direct = !far && !a.bytes;
     const int stretches = stretches_of(a.M, a.N, a.K);
     if (a.M <= kFewRows) {
         // 8 x 50001 x 1024: 14.7 us with 32 channels a wavefront, 15.9 with 16; 1 x 512 x 8192: 11.2 and 7.9
@@ -593,6 +675,7 @@ hipError_t launch_product(const ProductCall& c, hipStream_t s) {
     a.w_stride = c.w_stride;
     a.out_stride = c.out_stride;
     a.out = c.out;
+    a.bytes = (((uintptr_t)c.x | (uintptr_t)c.w | (uintptr_t)c.x_stride | (uintptr_t)c.w_stride) & 3) != 0;
     if (c.dtype == kF32) run<float>(a, c.workspace, s);
     else if (c.dtype == kF16) run<_Float16>(a, c.workspace, s);
     else run<__bf16>(a, c.workspace, s);

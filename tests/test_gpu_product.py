@@ -96,6 +96,36 @@ def test_strided_rows(m, n, k, by):
     assert torch.equal(out[:, 3:n + 3], want) and (out[:, :3] == 5).all() and (out[:, n + 3:] == 5).all()
 
 
+@pytest.mark.parametrize("m,n", [(5, 37), (30, 300), (40, 70)])
+def test_ends_of_rows(m, n):
+    """Rows that begin at every byte of a word, of every length near the ends of pieces, words, steps and batches of steps."""
+    for k in (*range(14, 40), *range(60, 70), *range(127, 134), *range(253, 262), *range(509, 517), *range(1020, 1031)):
+        say(f"product ends {m} {n} {k}")
+        args = case(m, n, k, seed=k)
+        check(cc.cc_product_i8(*args, dtype=F32), *args, F32)
+
+
+@pytest.mark.parametrize("m,n,k", [(8, 8000, 4001), (32, 600, 3333), (17, 20000, 1003), (1, 40, 9001)])
+@pytest.mark.parametrize("by", [0, 1, 2, 3, 4])
+def test_few_rows_at_any_byte(m, n, k, by):
+    say(f"product few rows at byte {m} {n} {k} {by}")
+    x, xs, w, ws, b = case(m, n, k)
+    xa, wa = torch.full((m, k + by), 99, device="cuda", dtype=torch.int8), torch.full((n, k + 4), 99, device="cuda", dtype=torch.int8)
+    xa[:, by:], wa[:, 4 - by:k + 4 - by] = x, w
+    check(cc.cc_product_i8(xa[:, by:], xs, wa[:, 4 - by:k + 4 - by], ws, b), x, xs, w, ws, b, F32)
+
+
+@pytest.mark.parametrize("m,n,k", [(40, 60, 68), (64, 64, 2052), (300, 300, 412), (2048, 1792, 276), (4096, 4096, 644), (4000, 4100, 1036)])
+def test_rows_at_words(m, n, k):
+    """Tiles of each size, straight from rows that begin at words of 4 bytes."""
+    say(f"product rows at words {m} {n} {k}")
+    args = case(m, n, k)
+    check(cc.cc_product_i8(*args, dtype=BF16), *args, BF16)
+    rows = torch.full((m, k + 8), 99, device="cuda", dtype=torch.int8)
+    rows[:, 4:k + 4] = args[0]
+    assert torch.equal(cc.cc_product_i8(rows[:, 4:k + 4], *args[1:]), cc.cc_product_i8(*args))
+
+
 def test_rows_far_apart():
     """Rows of a tile more than 2^32 bytes apart from its first."""
     say("product far rows")
