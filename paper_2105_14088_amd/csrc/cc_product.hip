@@ -39,23 +39,14 @@ struct Args {
     bool bytes;                          // some row does not begin at a word of 4 bytes
 };
 
-// 16 bytes of a row from k on; what lies beyond K is zero and not read.  Where they end beyond the row, its last 16 are read and shifted.
-__device__ __forceinline__ Int4 load_piece(const int8_t* row, int k, int K) {
+// 16 bytes from k on of a row of fewer; what lies beyond it is zero and not read.
+__device__ __forceinline__ Int4 load_short(const int8_t* row, int k, int K) {
     typedef uint64_t Long2 __attribute__((ext_vector_type(2)));
     Long2 v = {0, 0};
-    if (K >= kPiece) {
-        const int at = min(k, K - kPiece), beyond = min(k - at, kPiece) * 8;
-        __builtin_memcpy(&v, row + at, kPiece);
-        if (beyond >= 64) v = Long2{v[1], 0};
-        const int shift = beyond & 63;
-        if (beyond == 128) v = Long2{0, 0};
-        else if (shift) v = Long2{v[0] >> shift | v[1] << (64 - shift), v[1] >> shift};
-    } else {
-        for (int i = 0; k + i < K; ++i) {
-            const uint64_t byte = (uint8_t)row[k + i];
-            if (i < 8) v[0] |= byte << (8 * i);
-            else v[1] |= byte << (8 * (i - 8));
-        }
+    for (int i = 0; k + i < K; ++i) {
+        const uint64_t byte = (uint8_t)row[k + i];
+        if (i < 8) v[0] |= byte << (8 * i);
+        else v[1] |= byte << (8 * (i - 8));
     }
     return __builtin_bit_cast(Int4, v);
 }
@@ -84,7 +75,8 @@ __device__ __forceinline__ Words load_words(const int8_t* p, uint32_t by, bool m
     w.by = by;
     return w;
 }
-// Any piece of a row, as load_piece, without a branch: K >= 16.
+// Any piece of a row of at least 16, without a branch: what lies beyond the row is zero, and where a piece ends beyond it, its last 16 bytes are read and
+// shifted.
 template <class Part>
 struct Clipped {
     Part part;
@@ -231,7 +223,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
                 const auto row = [&](int u) { return p + u < XPIECES ? xbase + row_of(p + u) * a.x_stride : wbase + row_of(p + u) * a.w_stride; };
                 if (a.K < kPiece) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) put(p + u, 0, load_piece(row(u), k, a.K));
+                    for (int u = 0; u < U; ++u) put(p + u, 0, load_short(row(u), k, a.K));
                 } else {
                     Clipped<Words> v[U];
 #pragma unroll
@@ -521,7 +513,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int s
         };
         int s = begin;
         if (a.K < kPiece) {
-            if (s < end) batch(std::integral_constant<int, 1>(), s, 1, [&](const int8_t* row, int k) { return Whole{load_piece(row, k, a.K)}; });
+            if (s < end) batch(std::integral_constant<int, 1>(), s, 1, [&](const int8_t* row, int k) { return Whole{load_short(row, k, a.K)}; });
         } else {
             constexpr std::integral_constant<int, U> full;
             // a step too many costs its loads (20 x 1000 x 333, six steps: 12 us with the loads of eight, 8 with those of six)
