@@ -6,8 +6,8 @@
 // how it is cut.  Terms beyond K are zeros that are put where a tile ends inside a row; nothing beyond a row is read.
 //
 // tile_kernel: a workgroup has a tile of the result and goes along K in steps of 128 bytes.  Both operands come to LDS in pieces of 16
-// bytes, straight from memory where all rows begin at words of 4 bytes (4096 x 4096 x 4004: 77 us, 90 through registers), through registers else.  In LDS a row has 8 such pieces,
-// and piece c lies at place c ^ (row / 2 % 8): the lanes that read the same piece of 16 rows then use all 64 banks once.  Two to
+// bytes, straight from memory where all rows begin at words of 4 bytes (4096 x 4096 x 4004: 77 us, 90 through registers), through
+// registers else.  In LDS a row has 8 such pieces, and piece c lies at place c ^ (row / 2 % 8): the lanes that read the same piece of 16 rows then use all 64 banks once.  Two to
 // four tiles are held: while one is multiplied, others are on their way.
 //
 // few_kernel: up to 32 rows, where reading the weights is what takes time: they go from memory to registers, each once; several
@@ -450,14 +450,17 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, const int32_t* 
     }
 }
 
-// Bound by memory: 8 x 50001 x 1024 13 us, 4.0 TB/s; 8 x 8192 x 8192 16 us, 4.2; with rows at any byte 8 x 50001 x 1001 17 us, 3.0.  MT * 16 rows; NT * 16 channels to `share` wavefronts of a workgroup's 8, each of which has a stretch of K.  Weights are read once, the rows of x
-// once for every NT * 16 channels.
+// Bound by memory: 8 x 50001 x 1024 12 us, 4.2 TB/s; 8 x 8192 x 8192 16 us, 4.2; with rows at any byte 8 x 50001 x 1001 16 us, 3.1.  MT * 16 rows;
+// NT * 16 channels to `share` wavefronts of a workgroup (8 at the most), each of which has a stretch of K.  Weights are read once, the rows
+// of x once for every NT * 16 channels.
 constexpr int kFewWaves = 8;
+constexpr int64_t kFullCard = 256 * kFewWaves;
 template <class S, int MT, int NT>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Args a, int share) {
-    __shared__ Int4 parts[kFewWaves][MT * NT][64];
+    extern __shared__ Int4 sums[];                // of wavefronts that share K
+    auto* const parts = (Int4(*)[MT * NT][64])sums;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int64_t n0 = ((int64_t)blockIdx.x * (kFewWaves / share) + wave / share) * 16 * NT;
+    const int64_t n0 = ((int64_t)blockIdx.x * (blockDim.x / 64 / share) + wave / share) * 16 * NT;
     const int steps = (a.K + 63) / 64, each = (steps + share - 1) / share;
     const int begin = min(wave % share * each, steps), end = min(begin + each, steps);
     Int4 sum[MT][NT];
@@ -579,8 +582,12 @@ void launch_few(const Args& a, int64_t waves, hipStream_t s) {
     const int64_t places = (a.N + 16 * NT - 1) / (16 * NT);
     int share = 1;
     while (share < kFewWaves && places * share < waves && a.K > 512 / NT * share) share *= 2;
-    const int64_t per = kFewWaves / share;
-    hipLaunchKernelGGL((few_kernel<S, MT, NT>), dim3((unsigned)((places + per - 1) / per)), dim3(kFewWaves * 64), 0, s, a, share);
+    // A compute unit has one workgroup of eight wavefronts or two: unless those nearly fill the card, wavefronts that share nothing go by
+    // themselves (8 x 90000 x 1024: 20 us, 25 in eights; 1 x 131072 x 1024, where eights fill it twice: 31 and 28).
+    const int64_t all = places * share, rounds = (all + kFullCard - 1) / kFullCard;
+    const int64_t per = all * 10 >= rounds * kFullCard * 9 ? kFewWaves / share : 1;
+    hipLaunchKernelGGL((few_kernel<S, MT, NT>), dim3((unsigned)((places + per - 1) / per)), dim3((unsigned)(per * share * 64)),
+                       share > 1 ? (size_t)(per * share) * MT * NT * 64 * sizeof(Int4) : 0, s, a, share);
 }
 
 // Counts a result's tiles and gives the grid that has them.
