@@ -96,6 +96,14 @@ def test_strided_rows(m, n, k, by):
     assert torch.equal(out[:, 3:n + 3], want) and (out[:, :3] == 5).all() and (out[:, n + 3:] == 5).all()
 
 
+@pytest.mark.parametrize("m,n,k", [(8, 30000, 700), (20, 31007, 513), (3, 60000, 130), (2, 131072, 65), (5, 4000, 1500), (7, 8100, 1100)])
+def test_few_rows_of_wide_heads(m, n, k):
+    """Wavefronts by themselves and in eights, with a channel's K shared and not."""
+    say(f"product wide {m} {n} {k}")
+    args = case(m, n, k)
+    check(cc.cc_product_i8(*args, dtype=F16), *args, F16)
+
+
 @pytest.mark.parametrize("m,n", [(5, 37), (30, 300), (40, 70)])
 def test_ends_of_rows(m, n):
     """Rows that begin at every byte of a word, of every length near the ends of pieces, words, steps and batches of steps."""
