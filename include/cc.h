@@ -566,7 +566,8 @@ int cc_preference_loss(const void* logits, int32_t dtype, int64_t B, int64_t T, 
  *   q, scale     int8 [n, D] and fp32 [n], both or neither
  *   rstd         fp32 [n] or NULL: r, what the backward call needs
  * A row of zeros has q and scale zero; one whose u holds an infinite or undefined element has q zero and scale NaN, so that
- * products with it are undefined.  Squares are summed in 64 bits.
+ * products with it are undefined.  Squares are summed in 64 bits; where an element of h is infinite, r is zero and `out` zero but there,
+ * where it is undefined.
  */
 int cc_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, int32_t dtype, int64_t n,
                 int64_t D, const void* weight, int32_t weight_dtype, float eps, void* sum, int64_t sum_stride, void* out,

@@ -181,7 +181,7 @@ __device__ __forceinline__ Pack<W, VEC> weights(const void* weight, int64_t at) 
 // What is found out about a row on the way through it.
 template <bool NORM, bool QUANT>
 struct Sums {
-    double squares = 0.0;                // of h: neither infinite nor undefined as long as no element is
+    double squares = 0.0;                // of h: infinite where an element is, undefined where one is
     double most = 0.0;                   // |u|: a product of finite 32-bit elements is finite in 64
     uint32_t bits = 0;                   // without a norm: the largest |x| by its bits, which infinite and undefined ones exceed
     // Some elements; those before `skip` have been added by another thread.
@@ -190,8 +190,8 @@ struct Sums {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             if constexpr (NORM) {
-                const double v = (double)h.get(i);
-                squares = __builtin_fma(i < skip ? 0.0 : v, v, squares);
+                const double v = (double)h.get(i), own = i < skip ? 0.0 : v;     // zero times an infinite v would be undefined
+                squares = __builtin_fma(own, own, squares);
                 if constexpr (QUANT) most = __builtin_fmax(most, __builtin_fabs(v * (double)w.get(i)));
             } else {
                 bits = max(bits, __builtin_bit_cast(uint32_t, h.get(i)) & 0x7fffffffu);

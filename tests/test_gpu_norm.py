@@ -272,3 +272,36 @@ def test_a_workspace_is_as_large_as_it_says(dim, dtype):
     assert (room[need:] == 0x5A).all()
     want = cc.cc_rms_norm_backward(go, h, rstd, w)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("dim", [1, 3, 8, 9, 24, 63, 64, 100, 300, 768, 1021, 1024, 1536, 2050, 5120, 8195, 16384, 16387])
+def test_an_infinity_in_any_column(dim, dtype):
+    """r is zero wherever in a row an infinity stands: zeros, undefined at the infinity alone, and the gradient of its column's weight alone."""
+    say(f"norm infinity {dim} {dtype}")
+    columns = sorted({0, dim // 2, *range(max(0, dim - 9), dim)})
+    x, residual, weight = made(len(columns) + 1, dim, dtype), made(len(columns) + 1, dim, dtype, 1), made(1, dim, F32, 2)[0]
+    for i, column in enumerate(columns):
+        if i % 2:
+            x[i, column] = -math.inf
+        else:
+            x[i, column] = residual[i, column] = torch.finfo(dtype).max         # their sum is infinite
+    res = cc.cc_rms_norm(x, weight, residual, quantized=True, save_rstd=True)
+    h = ref.added(x, residual)
+    at = torch.tensor(columns, device="cuda")
+    want = torch.zeros(len(columns), dim, device="cuda", dtype=dtype)
+    want[torch.arange(len(columns), device="cuda"), at] = math.nan
+    assert torch.equal(res.sum, h) and torch.isinf(h[:-1].gather(1, at[:, None])).all()
+    assert (res.rstd[:-1] == 0).all() and torch.equal(torch.isnan(res.out[:-1]), torch.isnan(want)) and torch.equal(res.out[:-1].nan_to_num(), want.nan_to_num())
+    assert (res.q[:-1] == 0).all() and torch.isnan(res.scale[:-1]).all()
+    last, r = ref.norm(h[-1:], weight, 1e-6)
+    near(res.out[-1:], last, ref.rounded(last, dtype, forward_error(h[-1:], weight, last)), "out")
+    near(res.rstd[-1:], r, 1.001 * ref.U24 * r, "rstd")
+    go = made(len(columns) + 1, dim, dtype, 3)
+    grad_weight = cc.cc_rms_norm_backward(go, h, res.rstd, weight)[1]
+    touched = torch.zeros(dim, device="cuda", dtype=torch.bool)
+    touched[at] = True
+    assert torch.equal(torch.isnan(grad_weight), touched)
+    # of the other columns' terms all but the last row's are zero: two roundings
+    want = (go[-1].double() * h[-1].double() * res.rstd[-1].double())[~touched]
+    near(grad_weight[~touched], want, ref.rounded(want, F32, 2.01 * ref.U24 * want.abs()), "grad_weight")
