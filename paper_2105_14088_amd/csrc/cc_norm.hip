@@ -124,7 +124,10 @@ struct RowScale {
     // 16 (R is float then: 127 u and r most have 23, and no bit of either lies below 2^-24 most unless r = 0), in 32.  An element of some
     // 5000 is so near; of bf16 ones one of 500, since half of the largest is a border, and then half of all
     // vectors have one (65536 x 1024: 49 us with a division in 64 bits there, 43 with this in 64, 38 in 32).
-    template <class R, int N, class Exact>
+    // LONG: u is a product of two 32-bit elements and 127 u may have 55 bits.  What its rounding to 53 leaves out is added last.  The rounded one
+    // lies at most some half of most beyond r most, and near a border no bit of it lies below 2^-54 most, so that is exact, and so is how
+    // far it is from half of most (fp32 rows of 65536 x 1024: as long as without).
+    template <class R, bool LONG, int N, class Exact>
     __device__ __forceinline__ void nearest(const float (&u)[N], Exact exact, int (&q)[N]) const {
         float worst = 0.0f, r[N];
 #pragma unroll
@@ -133,16 +136,27 @@ struct RowScale {
             r[i] = __builtin_rintf(t);
             worst = fmaxf(worst, __builtin_fabsf(t - r[i]));
         }
-        if (__ballot(inverse != inverse) != 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) r[i] = defined && most > 0.0 ? (float)__builtin_rint(127.0 * exact(i) / most) : 0.0f;
-        } else if (__ballot(!(worst < 0.4999f)) != 0) {
+        const auto settle = [&] {
             const R m = (R)most, half = (R)0.5 * m;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const R top = (R)127 * (R)exact(i), beyond = __builtin_elementwise_fma(-(R)r[i], m, top), size = __builtin_elementwise_abs(beyond);
-                if (size > half || (size == half && ((int)r[i] & 1))) r[i] += beyond > (R)0 ? 1.0f : -1.0f;
+                const R top = (R)127 * (R)exact(i), beyond = __builtin_elementwise_fma(-(R)r[i], m, top);
+                R over = __builtin_elementwise_abs(beyond) - half;
+                if constexpr (LONG) {
+                    const R rest = __builtin_elementwise_fma((R)127, (R)exact(i), -top);
+                    over += beyond > (R)0 ? rest : -rest;
+                }
+                if (over > (R)0 || (over == (R)0 && ((int)r[i] & 1))) r[i] += beyond > (R)0 ? 1.0f : -1.0f;
             }
+        };
+        if (__ballot(inverse != inverse) != 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) r[i] = defined && most > 0.0 ? (float)__builtin_rint(127.0 * exact(i) / most) : 0.0f;
+            // a quotient of at most 39 and 32 bits is as far from a border as its rounding
+            if constexpr (LONG)
+                if (defined && most > 0.0) settle();
+        } else if (__ballot(!(worst < 0.4999f)) != 0) {
+            settle();
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) q[i] = (int)r[i];
@@ -238,7 +252,8 @@ __device__ __forceinline__ void store_row(const Args& a, int64_t row, int at, co
 #pragma unroll
         for (int i = 0; i < VEC; ++i) u[i] = NORM ? h.get(i) * w.get(i) : h.get(i);
         using R = std::conditional_t<(sizeof(S) == 2 && !NORM) || (std::is_same_v<S, __bf16> && std::is_same_v<W, __bf16>), float, double>;
-        r.template nearest<R>(u, [&](int i) { return NORM ? (double)h.get(i) * (double)w.get(i) : (double)h.get(i); }, q);
+        constexpr bool LONG = NORM && sizeof(S) + sizeof(W) == 8;
+        r.template nearest<R, LONG>(u, [&](int i) { return NORM ? (double)h.get(i) * (double)w.get(i) : (double)h.get(i); }, q);
         store_bytes(a.q + row * a.q_stride + at, q);
     }
 }

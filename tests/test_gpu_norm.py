@@ -305,3 +305,31 @@ def test_an_infinity_in_any_column(dim, dtype):
     # of the other columns' terms all but the last row's are zero: two roundings
     want = (go[-1].double() * h[-1].double() * res.rstd[-1].double())[~touched]
     near(grad_weight[~touched], want, ref.rounded(want, F32, 2.01 * ref.U24 * want.abs()), "grad_weight")
+
+
+# u = c d, the row's largest a b, all four below 2^24; the quotient is so near to a border that 127 u rounded to 64 bits lies on it or beyond
+NEAR_BORDERS = [(12050691, 15466566, 12431225, 16776439), (15058646, 12249475, 13652353, 16264741), (10140597, 9095033, 9117779, 16576039),
+                (13338359, 16422241, 15533163, 15919379), (15910822, 14294319, 14837975, 16567131), (10766781, 10601041, 8729795, 14253061),
+                (13761129, 12186782, 12433791, 14455227), (16383889, 14128151, 14536913, 16643995), (15583471, 14832691, 15567679, 15912765),
+                (9712573, 9416399, 6450767, 14347221), (14478006, 10004271, 9616069, 16562213), (14300846, 10685011, 12676981, 14934845)]
+
+
+def whole_nearest(top, bottom):
+    """The whole number nearest to top / bottom, ties to even, in whole numbers."""
+    low, rest = divmod(top, bottom)
+    return low + (2 * rest > bottom or (2 * rest == bottom and low % 2 == 1))
+
+
+@pytest.mark.parametrize("size", [0, -80, 40], ids=str)
+@pytest.mark.parametrize("numbers", NEAR_BORDERS, ids=lambda n: str(n[0]))
+def test_products_of_32_bits_next_to_borders(numbers, size):
+    """Both signs, and the same smaller and larger by powers of two, where 32 bits do not hold the product."""
+    c, d, a, b = numbers
+    want = whole_nearest(127 * c * d, a * b)
+    for dim in (5, 700, 17000):
+        x, w = torch.zeros(1, dim, device="cuda"), torch.ones(dim, device="cuda")
+        scaled = 2.0 ** size
+        x[0, 0], x[0, 1], x[0, dim - 2] = a * scaled, c * scaled, -c * scaled
+        w[0], w[1], w[dim - 2] = b * scaled, d * scaled, d * scaled
+        q = cc.cc_rms_norm(x, w, normed=False, quantized=True).q[0]
+        assert [int(q[i]) for i in (0, 1, dim - 2, dim - 1)] == [127, want, -want, 0]
