@@ -204,3 +204,61 @@ def test_a_single_position_says_how_much_history_there_is():
     z, history = torch.randn(2, 1, 5, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda")
     with pytest.raises(ValueError, match="lengths"):
         cc.cc_shape_logits(z, history, None, torch.ones(2, 3, device="cuda"))
+
+
+def repeated(z, r):
+    """Logits whose tokens are all seen and do not count, with (r, 0, 0): the arguments behind them."""
+    b, t, v = z.shape
+    history = torch.arange(v, dtype=torch.int32, device="cuda").expand(b, v)
+    lengths = torch.full((b,), v, dtype=torch.int32, device="cuda")
+    return history, lengths, torch.tensor([r, 0.0, 0.0], device="cuda").repeat(b, 1), lengths + t
+
+
+@pytest.mark.parametrize("v", [3, 40, 1000, 5000])
+@pytest.mark.parametrize("r", [1.3, 0.7, 3.0, 1e10, 2.0 ** -130, 2.0 ** -140 * 3, 2.0 ** 127 * 1.7, 1e-30], ids=str)
+def test_a_quotient_is_rounded_once(v, r):
+    """z / r is off by a division's rounding and no more, whatever r is, and so is the gradient."""
+    say(f"shape quotient {v} {r}")
+    g = torch.Generator(device="cuda").manual_seed(v)
+    r32 = float(torch.tensor(r))
+    # quotients and products that a float holds
+    size = min(1.0, r32 * 2.0 ** 120) * min(1e4, max(1.0, r32 * 2.0 ** -120))
+    z = size * torch.randn(3, 2, v, generator=g, device="cuda")
+    if r32 > 1e30:
+        z = z.abs()
+    rest = repeated(z, r)
+    want = torch.where(z > 0, z.double() / r32, z.double() * r32)
+    got = cc.cc_shape_logits(z, *rest)
+    tol = 1.001 * ref.U24 * want.abs() + ref.BELOW[F32]
+    assert ((got.double() - want).abs() <= tol).all(), float(((got.double() - want).abs() / want.abs()).max() / ref.U24)
+    grad = size * torch.randn(3, 2, v, generator=g, device="cuda")
+    want = torch.where(z > 0, grad.double() / r32, grad.double() * r32)
+    held = want.abs() < torch.finfo(F32).max
+    back = cc.cc_shape_logits_backward(grad, z, *rest)
+    tol = 1.001 * ref.U24 * want.abs() + ref.BELOW[F32]
+    assert ((back.double() - want).abs() <= tol)[held].all() and torch.isinf(back[~held]).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("v", [40, 3000])
+def test_quotients_at_the_ends_of_the_range(v, dtype):
+    """Infinities, undefined and the largest quotients, with divisors that have no reciprocal, or none of full length, too."""
+    top = torch.finfo(dtype).max
+    for r in (0.7, 2.0 ** -130, 2.0 ** -149, 2.0 ** 126 * 1.9, 1.5):
+        r32 = float(torch.tensor(r))
+        z = torch.zeros(2, 1, v, dtype=dtype)
+        z[0, 0, :6] = torch.tensor([math.inf, -math.inf, math.nan, top, 1.0, 0.0]).to(dtype)
+        edge = torch.tensor(min(top * r32, top), dtype=torch.float64).to(dtype)
+        while float(edge) / r32 > top:
+            edge = torch.nextafter(edge, torch.zeros((), dtype=dtype))
+        z[0, 0, 6] = edge                                   # the largest with a quotient that the type holds
+        z[1, 0, 0] = torch.finfo(dtype).tiny
+        want = torch.where(z > 0, z.double() / r32, z.double() * r32).to(dtype)
+        rest = repeated(z.cuda(), r)
+        got = cc.cc_shape_logits(z.cuda(), *rest).cpu()
+        back = cc.cc_shape_logits_backward(z.cuda(), z.cuda(), *rest).cpu()
+        for out in (got, back):
+            assert torch.equal(torch.isnan(out), torch.isnan(want)) and torch.equal(torch.isinf(out), torch.isinf(want))
+            held = torch.isfinite(want)
+            exact = torch.where(z > 0, z.double() / r32, z.double() * r32)[held]
+            assert ((out[held].double() - exact).abs() <= ref.rounded(exact, dtype, 2 * ref.U24 * exact.abs())).all()
