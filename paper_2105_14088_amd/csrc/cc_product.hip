@@ -107,8 +107,13 @@ __device__ __forceinline__ Clipped<Words> load_clipped_words(const int8_t* row, 
     return {load_words(row + at, inside ? by : 0, inside), min(k - at, kPiece)};
 }
 
-// From the exact sum on in 32 bits: it is rounded, and so is each product and the sum with the bias.
-__device__ __forceinline__ float scaled(int sum, float xs, float ws, float bias) { return (float)sum * xs * ws + bias; }
+// From the exact sum on in 32 bits: it is rounded, and so is each product and the sum with the bias.  Beyond 2^96 of xs a power of two is left to
+// the last product, so that the first is not infinite where the result is not (that product takes 1 % of 8192 x 8192 x 4096; a choice of the order by
+// row 2 %, and so does a branch around it).
+__device__ __forceinline__ float scaled(int sum, float xs, float ws, float bias) {
+    const bool far = __builtin_fabsf(xs) > 0x1p96f;
+    return (float)sum * (far ? xs * 0x1p-64f : xs) * ws * (far ? 0x1p64f : 1.0f) + bias;
+}
 
 // An address that all lanes have, in scalar registers.
 __device__ __forceinline__ const int8_t* scalar(const int8_t* p) {

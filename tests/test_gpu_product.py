@@ -202,3 +202,17 @@ def test_a_workspace_is_as_large_as_it_says(m, n, k):
     assert (room[need:] == 0x5A).all() and torch.equal(got, cc.cc_product_i8(*args))
     with pytest.raises(cc.CCError):
         cc.cc_product_i8(*args, workspace=room[:need - 256])
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 40, 64), (20, 17000, 130), (64, 64, 2048), (90, 130, 200), (300, 301, 1001), (2000, 2000, 130), (4096, 4096, 640)])
+@pytest.mark.parametrize("large", ["x", "w"])
+def test_scales_that_one_product_does_not_hold(m, n, k, large):
+    """The sum times one scale may lie beyond 32 bits where the result does not: rows of the largest values times channels of the smallest, and
+    the other way round; one row is ordinary."""
+    say(f"product scales {m} {n} {k} {large}")
+    x, xs, w, ws, b = case(m, n, k)
+    up, down = 2.0 ** 124, 2.0 ** -124
+    xs, ws = (xs * up, ws * down) if large == "x" else (xs * down, ws * up)
+    xs[m // 2] = 2.0 ** -24
+    for bias in (None, b):
+        check(cc.cc_product_i8(x, xs, w, ws, bias), x, xs, w, ws, bias, F32)
