@@ -202,7 +202,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void tile_kernel(const 
             const uint32_t to = (uint32_t)(uintptr_t)lds + buffer * BYTES + wave * 1024 + p * THREADS * kPiece;
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                          :
-                         : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from[p]), "s"(scalar(base)) : "memory");
+                         : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from[p]), "s"(scalar(base)) : "memory", "m0");
         } else {
             __builtin_memcpy(&held[set][p], base + from[p], kPiece);
         }

@@ -46,3 +46,15 @@ def test_kernels_that_address_lds_from_an_integer_are_looked_at_by_the_build():
         for at in re.finditer(r"address_space\(3\)\)\)[^;]*\(uintptr_t\)", code_of(path)):
             before = re.findall(r"__global__[^{;]*?\b(\w+)\s*\(\s*const", code_of(path)[: at.start()])
             assert before[-1] in DYNAMIC_LDS_AT_0
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_assembly_names_the_registers_that_it_sets(path):
+    """m0, vcc and exec are the compiler's as well: what it keeps there across a statement that sets one unnamed is lost."""
+    text = code_of(path)
+    for at in re.finditer(r"\basm\s+(?:volatile\s*)?\((.*?)\)\s*;", text, flags=re.S):
+        statement = at.group(1)
+        code, clobbers = " ".join(re.findall(r'"([^"]*)"', statement)), statement.rsplit(":", 1)[-1]
+        for register in ("m0", "vcc", "exec"):
+            if re.search(rf"\b[sv]_\w+ {register}\b\s*,", code):
+                assert f'"{register}"' in clobbers, (register, statement)
