@@ -382,11 +382,24 @@ def _each_row(t: Optional[torch.Tensor], x: torch.Tensor, stream, name: str):
     return t, _plain(t, x.shape[:-1], torch.float32, name)
 
 
-def _stream_at(t: torch.Tensor, stream) -> int:
-    """The stream's handle.  A kernel is launched on the current device: on a tensor of another it would read what may not be there."""
+@functools.lru_cache(maxsize=None)
+def _several_devices() -> bool:
+    """Whether a tensor on the GPU can be on another than the current one: looking at all that a small call takes is 3 % of it."""
+    return torch.cuda.device_count() > 1
+
+
+def _stream_at(t: torch.Tensor, stream, *passed: Optional[torch.Tensor]) -> int:
+    """The stream's handle.  A kernel is launched on the current device: of t and what else was passed in, on a tensor of another it would read
+    what may not be there."""
     current = torch.cuda.current_device() if _binding._current_device is None else _binding._current_device()
     if t.get_device() != current:
         raise ValueError("tensors must be on the current device")
+    if _several_devices():
+        for other in passed:
+            if other is not None and other.get_device() != current:
+                raise ValueError("tensors must be on the current device")
+        if stream is not None and stream.device_index != current:
+            raise ValueError("the stream must be one of the current device")
     if stream is None and _binding._current_raw_stream is not None:
         return _binding._current_raw_stream(current)
     return _stream(stream)
@@ -432,6 +445,7 @@ def cc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual
     code = _dtype(x, "x")
     if not shape:
         raise ValueError("x must be [..., D]")
+    passed = (weight, residual, out, sum, q, scale, rstd)
     d = shape[-1]
     n = x.numel() // d if d else 0
     x_at = _rows(x, shape, dtype, "x")
@@ -451,7 +465,7 @@ def cc_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual
     if save_rstd or rstd is not None:
         rstd, rstd_to = _each_row(rstd, x, stream, "rstd")
     _check(lib().cc_rms_norm(*x_at, *residual_at, code, n, d, *_weight(weight, d, dtype, "weight"), eps, *sum_to, *out_to, *q_to,
-                             scale_to, rstd_to, _stream_at(x, stream)), "cc_rms_norm")
+                             scale_to, rstd_to, _stream_at(x, stream, *passed)), "cc_rms_norm")
     return RmsNorm(out, x if sum is None else sum, q, scale, rstd)
 
 
@@ -466,6 +480,7 @@ def cc_rms_norm_backward(grad_out: torch.Tensor, h: torch.Tensor, rstd: torch.Te
     code = _dtype(h, "h")
     if not shape:
         raise ValueError("h must be [..., D]")
+    passed = (grad_out, rstd, weight, grad_sum, grad_h, grad_weight, workspace)
     d = shape[-1]
     n = h.numel() // d if d else 0
     h_at, grad_at = _rows(h, shape, dtype, "h"), _rows(grad_out, shape, dtype, "grad_out")
@@ -484,7 +499,7 @@ def cc_rms_norm_backward(grad_out: torch.Tensor, h: torch.Tensor, rstd: torch.Te
         held, ws, nbytes = _workspace(workspace, _norm_bytes(n, d), device, stream)
     _check(lib().cc_rms_norm_backward(*grad_at, *h_at, code, n, d, *_weight(weight, d, dtype, "weight"),
                                       _plain(rstd, shape[:-1], torch.float32, "rstd"), *sum_at, *grad_h_to, to, to_code,
-                                      1 if accumulate else 0, ws, nbytes, _stream_at(h, stream)), "cc_rms_norm_backward")
+                                      1 if accumulate else 0, ws, nbytes, _stream_at(h, stream, *passed)), "cc_rms_norm_backward")
     return grad_h, grad_weight
 
 
@@ -493,11 +508,13 @@ def cc_quantize_rows(x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: O
     shape, code = x.shape, _dtype(x, "x")
     if not shape:
         raise ValueError("x must be [..., D]")
+    passed = (q, scale)
     d = shape[-1]
     x_at = _rows(x, shape, x.dtype, "x")
     q, q_to = _rows_like(q, x, torch.int8, stream, "q")
     scale, scale_to = _each_row(scale, x, stream, "scale")
-    _check(lib().cc_quantize_rows(*x_at, code, x.numel() // d if d else 0, d, *q_to, scale_to, _stream_at(x, stream)), "cc_quantize_rows")
+    _check(lib().cc_quantize_rows(*x_at, code, x.numel() // d if d else 0, d, *q_to, scale_to, _stream_at(x, stream, *passed)),
+           "cc_quantize_rows")
     return q, scale
 
 
@@ -511,6 +528,7 @@ def cc_product_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_sca
     shape, (n, k) = x.shape, w.shape
     if shape[-1] != k:
         raise ValueError("x and w must have rows of one length")
+    passed = (x_scale, w, w_scale, bias, out, workspace)
     lead = shape[:-1]
     if out is not None:
         dtype = out.dtype
@@ -529,7 +547,7 @@ def cc_product_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_sca
     L = lib()
     held, ws, nbytes = _workspace(workspace, _product_bytes(m, n, k), x.device, stream)
     _check(L.cc_product_i8(*x_at, _plain(x_scale, lead, torch.float32, "x_scale"), *w_at, _plain(w_scale, (n,), torch.float32, "w_scale"),
-                           _plain(bias, (n,), torch.float32, "bias"), m, n, k, *out_to, code, ws, nbytes, _stream_at(x, stream)),
+                           _plain(bias, (n,), torch.float32, "bias"), m, n, k, *out_to, code, ws, nbytes, _stream_at(x, stream, *passed)),
            "cc_product_i8")
     return out
 
@@ -582,8 +600,9 @@ def cc_shape_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None
     back on the first lengths[b] + t entries; without lengths on the first t, as when the history is the orders themselves.
     `out` may be the logits."""
     args = _shape_args(logits, history, lengths, penalties, starts, bias, allowed)
+    passed = (history, lengths, penalties, starts, bias, allowed, out)
     out, to = _logits_like(out, logits, stream, "out")
-    _check(lib().cc_shape_logits(*args, *to, _stream_at(logits, stream)), "cc_shape_logits")
+    _check(lib().cc_shape_logits(*args, *to, _stream_at(logits, stream, *passed)), "cc_shape_logits")
     return out
 
 
@@ -595,7 +614,8 @@ def cc_shape_logits_backward(grad_out: torch.Tensor, logits: torch.Tensor, histo
     """The gradient of the logits from that of cc_shape_logits's result, whose arguments the others are.  `grad_logits` may be
     grad_out."""
     args = _shape_args(logits, history, lengths, penalties, starts, bias, allowed)
+    passed = (grad_out, history, lengths, penalties, starts, bias, allowed, grad_logits)
     grad_logits, to = _logits_like(grad_logits, logits, stream, "grad_logits")
-    _check(lib().cc_shape_logits_backward(*_strided(grad_out, logits.shape, logits.dtype, "grad_out"), *args, *to, _stream_at(logits, stream)),
-           "cc_shape_logits_backward")
+    _check(lib().cc_shape_logits_backward(*_strided(grad_out, logits.shape, logits.dtype, "grad_out"), *args, *to,
+                                          _stream_at(logits, stream, *passed)), "cc_shape_logits_backward")
     return grad_logits
