@@ -333,3 +333,15 @@ def test_products_of_32_bits_next_to_borders(numbers, size):
         w[0], w[1], w[dim - 2] = b * scaled, d * scaled, d * scaled
         q = cc.cc_rms_norm(x, w, normed=False, quantized=True).q[0]
         assert [int(q[i]) for i in (0, 1, dim - 2, dim - 1)] == [127, want, -want, 0]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("n,dim", [(70001, 40), (40000, 250), (9001, 700), (3001, 2500), (1500, 5000), (1500, 16384), (130, 16400), (1003, 16400)])
+def test_weights_gradient_of_several_rows_a_team(n, dim, dtype):
+    """More rows than the teams of all workgroups: 3 to 10 of each, and of rows that no team holds 5 and 32 of each part.  One after the other are
+    added these, at most 32 teams, 16 partial sums a lane, 2 lanes and 16 wavefronts: no more than check_backward's 128."""
+    say(f"norm backward teams {n} {dim} {dtype}")
+    h, go = made(n, dim, dtype, 0, 3.0), made(n, dim, dtype, 1)
+    # rows that differ, so that one left out or taken twice shows
+    h *= (1 + torch.arange(n, device="cuda") % 7).to(dtype).unsqueeze(1)
+    check_backward(go, h, made(1, dim, F32, 3)[0], 1e-6, None)
