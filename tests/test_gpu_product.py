@@ -216,3 +216,20 @@ def test_scales_that_one_product_does_not_hold(m, n, k, large):
     xs[m // 2] = 2.0 ** -24
     for bias in (None, b):
         check(cc.cc_product_i8(x, xs, w, ws, bias), x, xs, w, ws, bias, F32)
+
+
+@pytest.mark.parametrize("far", ["x", "w", "both"])
+@pytest.mark.parametrize("k,by", [(7, 0), (16, 3), (128, 1), (129, 0), (129, 5), (401, 16), (641, 1), (1153, 4), (1153, 7)])
+def test_rows_far_apart_of_any_length(k, by, far):
+    """Offsets of 64 bits inside a tile: rows shorter than a piece, K that ends inside a tile, several tiles on their way, rows at any byte."""
+    say(f"product far rows {k} {by} {far}")
+    m, n, apart = 70, 65, (1 << 23) + 16 * 3 + by % 2
+    x, xs, w, ws, b = case(m, n, k, seed=k)
+
+    def spread(t):
+        rows = torch.full((t.shape[0] * apart,), 99, device="cuda", dtype=torch.int8).view(t.shape[0], apart)[:, by:by + k]
+        return rows.copy_(t)
+
+    got = cc.cc_product_i8(spread(x) if far != "w" else x, xs, spread(w) if far != "x" else w, ws, b)
+    check(got, x, xs, w, ws, b, F32)
+    assert torch.equal(got, cc.cc_product_i8(x, xs, w, ws, b))
