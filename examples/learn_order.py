@@ -154,7 +154,8 @@ def score(model: str, matrix: torch.Tensor, orders: torch.Tensor) -> torch.Tenso
 
 def learn(matrix: torch.Tensor, model: str, loss: str = "policy", steps: int = 200, batch: int = 1024, rounds: int = 3,
           rate: float = 0.015, seed: int = 1, say=lambda *a: None, layers: int = 1, bits: int = 32):
-    """(best order, its cost, mean cost of the last batch)."""
+    """(best order, its cost, mean cost of the last batch).  The losses compare the policy with itself before the batch's steps, both in 32 bits;
+    with bits=8 the orders come from a policy that differs from that by the roundings to 8 bits, which is not corrected for."""
     n = matrix.shape[0]
     policy = OrderPolicy(n, seed=seed, layers=layers)
     optimiser = torch.optim.Adam(policy.params.values(), lr=rate)

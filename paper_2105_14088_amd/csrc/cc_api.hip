@@ -510,6 +510,6 @@ const char* cc_status_string(int status) {
 
 int cc_last_hip_error(void) { return g_last_hip_error; }
 
-int cc_version(void) { return 600; }
+int cc_version(void) { return 601; }
 
 }  // extern "C"

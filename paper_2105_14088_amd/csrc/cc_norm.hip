@@ -290,7 +290,8 @@ __device__ __forceinline__ void load_row(Pack<S, VEC> (&to)[K], const S* row, co
     }
 }
 
-// Bound by memory: 65536 x 1024 bf16 with a residual 92 us, 5.9 TB/s; the same into 8 bits 95 us, 4.9; rows in 8 bits alone 36 us, 5.6.  A
+// Bound by memory: 65536 x 1024 bf16 with a residual 91 us in a training pass, 5.9 TB/s, and 102 by itself, 5.3; into 8 bits 94 us, 5.0; rows in 8 bits
+// alone 37 us, 5.5.  A
 // team per row, the smallest that holds it: with more than 16 elements a thread registers leave too few wavefronts (2048
 // columns, four vectors of 64 threads or two of 128).  A thread holds K vectors of VEC elements.  Everything is stored behind the row's
 // sums: by then all of the row has been read, and the sum may be stored where x was.
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(threads_of(TEAM)) void norm_kernel(const Args a) {
 }
 
 // Rows that a team's registers do not hold: a workgroup per row reads it twice, the second time out of the caches (8192 x 40000 bf16 with a
-// residual 577 us, 4.5 TB/s of what is read and written once).  Every element is read and written by one thread,
+// residual 580 us, 4.5 TB/s of what is read and written once).  Every element is read and written by one thread,
 // as the sum may be stored where x was.
 template <class S, class W, int VEC, bool NORM, bool QUANT>
 __global__ __launch_bounds__(kLongBlock) void norm_long_kernel(const Args a) {
@@ -389,7 +390,8 @@ __global__ __launch_bounds__(kLongBlock) void norm_long_kernel(const Args a) {
     }
 }
 
-// The gradient of a row, by a team as above, bound by memory: 65536 x 1024 bf16 with the stream's gradient 107 us, 5.0 TB/s.  Where there is a gradient of weights, a thread sums its columns over the team's rows,
+// The gradient of a row, by a team as above, bound by memory: 65536 x 1024 bf16 with the stream's gradient 103 us by
+// itself, 5.2 TB/s, and 115 behind the forward call.  Where there is a gradient of weights, a thread sums its columns over the team's rows,
 // then a workgroup's teams are added in their order; norm_weight_kernel adds the workgroups.
 template <class S, class W, int VEC, int TEAM, int K>
 __global__ __launch_bounds__(threads_of(TEAM)) void norm_backward_kernel(const GradArgs a) {
@@ -466,7 +468,7 @@ __global__ __launch_bounds__(threads_of(TEAM)) void norm_backward_kernel(const G
     }
 }
 
-// Rows that a team's registers do not hold: a row's sum and its gradient in two readings, every element by one thread (8192 x 40000 bf16: 558 us,
+// Rows that a team's registers do not hold: a row's sum and its gradient in two readings, every element by one thread (8192 x 40000 bf16: 562 us,
 // 4.7 TB/s of what is read and written once).
 template <class S, class W, int VEC>
 __global__ __launch_bounds__(kLongBlock) void norm_backward_long_kernel(const GradArgs a) {
@@ -506,7 +508,8 @@ __global__ __launch_bounds__(kLongBlock) void norm_backward_long_kernel(const Gr
 }
 
 // The weights' gradient of such rows, before grad_h is stored where grad_out may be: a thread has 4 columns of some rows.  The last
-// thread's are moved back to end with the row; the columns that it shares have the same sums in both.  8192 x 40000 bf16: some 300 us.
+// thread's are moved back to end with the row; the columns that it shares have the same sums in both.  8192 x 40000 bf16: 305 us, the third
+// reading of g and h; beside the row's second reading it was not tried.
 template <class S>
 __global__ __launch_bounds__(kBlock) void norm_columns_kernel(const GradArgs a, int64_t rows) {
     constexpr int N = 4, U = 4;
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(kBlock) void norm_columns_kernel(const GradArgs a, 
 }
 
 // grad_weight[j] = the sum of `count` partial sums.  16 columns a workgroup; 64 groups of 16 lanes take the sums in turn, eight loads
-// in flight each, and are added in a fixed order.  1024 sums of 1024 columns: 4.3 us, of which the loads' latency is most.
+// in flight each, and are added in a fixed order.  1024 sums of 1024 columns: 4.6 us, of which the loads' latency is most.
 template <class W>
 __global__ __launch_bounds__(1024) void norm_weight_kernel(const float* __restrict__ partial, int count, int D, W* grad_weight, int accumulate) {
     __shared__ float lds[16][16];

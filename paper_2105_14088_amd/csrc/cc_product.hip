@@ -6,7 +6,7 @@
 // how it is cut.  Terms beyond K are zeros that are put where a tile ends inside a row; nothing beyond a row is read.
 //
 // tile_kernel: a workgroup has a tile of the result and goes along K in steps of 128 bytes.  Both operands come to LDS in pieces of 16
-// bytes, straight from memory where all rows begin at words of 4 bytes (4096 x 4096 x 4004: 77 us, 90 through registers), through
+// bytes, straight from memory where all rows begin at words of 4 bytes (4096 x 4096 x 4004: 73 us; x 4001, through registers, 88), through
 // registers else.  In LDS a row has 8 such pieces, and piece c lies at place c ^ (row / 2 % 8): the lanes that read the same piece of 16 rows then use all 64 banks once.  Two to
 // four tiles are held: while one is multiplied, others are on their way.
 //
@@ -51,8 +51,8 @@ __device__ __forceinline__ Int4 load_short(const int8_t* row, int k, int K) {
     return __builtin_bit_cast(Int4, v);
 }
 
-// A load of 16 bytes that does not begin at a word takes far longer than one that does (8 x 50001 x 1001: 22 us, x 1004 13): such a piece is read as
-// the five words that it lies in, and `by` bytes of the first are shifted out (16 us).  At a row's ends, where a word has bytes that are not the row's, the piece is read as it lies, by = 0.
+// A load of 16 bytes that does not begin at a word takes far longer than one that does (8 x 50001 x 1001: 22 us, x 1004 12): such a piece is read as
+// the five words that it lies in, and `by` bytes of the first are shifted out (15 us).  At a row's ends, where a word has bytes that are not the row's, the piece is read as it lies, by = 0.
 struct Whole {
     Int4 v;
     __device__ __forceinline__ Int4 get() const { return v; }
@@ -145,9 +145,9 @@ __device__ __forceinline__ void tile_of(uint32_t id, int tiles_m, int tiles_n, i
 // How rows come to LDS: straight, through registers, or through registers from addresses that 32 bits do not reach from a tile's first.
 enum RowMode { kRowsDirect, kRowsHeld, kRowsFar };
 
-// Large products are bound by the matrix cores at the clock that the card's power leaves them: 8192 x 8192 x 4096 251 us, 2.19 POP/s (233 us
-// with neither loads nor LDS reads), x 16384 917 us, 2.40.  A wavefront of 128 x 128 reads a byte from LDS for 64 products; with four
-// of them a compute unit's LDS is busy half of the time.  Smaller tiles: 2048 x 2048 x 2048 16 us, 1.1 POP/s; 1024 x 1024 x 1024 6 us.
+// Large products are bound by the matrix cores at the clock that the card's power leaves them: 8192 x 8192 x 4096 257 us, 2.14 POP/s (7 %
+// less with neither loads nor LDS reads), x 16384 877 us, 2.51.  A wavefront of 128 x 128 reads a byte from LDS for 64 products; with four
+// of them a compute unit's LDS is busy half of the time.  Smaller tiles: 2048 x 2048 x 2048 16 us, 1.1 POP/s; 1024 x 1024 x 1024 8 us, the call itself.
 // RING tiles of the operands are held, so a tile has RING - 1 others' time to arrive.  With more than one workgroup to a tile (gridDim.y) each
 // has a stretch of K, and S is int32: its sums go to a matrix of their own.
 template <class S, int BM, int BN, int WM, int WN, int STEP, int RING, RowMode MODE>
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, const int32_t* 
     }
 }
 
-// Bound by memory: 8 x 50001 x 1024 12 us, 4.2 TB/s; 8 x 8192 x 8192 16 us, 4.2; with rows at any byte 8 x 50001 x 1001 16 us, 3.1.  MT * 16 rows;
+// Bound by memory: 8 x 50001 x 1024 11.7 us, 4.4 TB/s; 8 x 8192 x 8192 14.4 us, 4.7; with rows at any byte 8 x 50001 x 1001 15 us, 3.4.  MT * 16 rows;
 // NT * 16 channels to `share` wavefronts of a workgroup (8 at the most), each of which has a stretch of K.  Weights are read once, the rows
 // of x once for every NT * 16 channels.
 constexpr int kFewWaves = 8;
@@ -588,7 +588,7 @@ void launch_few(const Args& a, int64_t waves, hipStream_t s) {
     int share = 1;
     while (share < kFewWaves && places * share < waves && a.K > 512 / NT * share) share *= 2;
     // A compute unit has one workgroup of eight wavefronts or two: unless those nearly fill the card, wavefronts that share nothing go by
-    // themselves (8 x 90000 x 1024: 20 us, 25 in eights; 1 x 131072 x 1024, where eights fill it twice: 31 and 28).
+    // themselves (8 x 90000 x 1024: 18 us, 24 in eights; 1 x 131072 x 1024, where eights fill it twice: 27.7 and 27.4).
     const int64_t all = places * share, rounds = (all + kFullCard - 1) / kFullCard;
     const int64_t per = all * 10 >= rounds * kFullCard * 9 ? kFewWaves / share : 1;
     hipLaunchKernelGGL((few_kernel<S, MT, NT>), dim3((unsigned)((places + per - 1) / per)), dim3((unsigned)(per * share * 64)),
@@ -613,8 +613,8 @@ void launch_tiles(Args a, bool direct, int stretches, hipStream_t s) {
 int64_t tiles_of(int64_t M, int64_t N, int64_t side) { return ((M + side - 1) / side) * ((N + side - 1) / side); }
 
 constexpr int64_t kFewRows = 32;
-// A tile of 256 takes a compute unit, which has two of 128 at once; those take 0.6 of its time together (8192 x 8192 x 4096: 269 us in four
-// rounds of the former, 320 in eight of the latter), but leave less of a last round unused (5000 x 5000 x 1024: 46 and 41 us).
+// A tile of 256 takes a compute unit, which has two of 128 at once; those take 0.6 of its time together (8192 x 8192 x 4096: 259 us in four
+// rounds of the former, 305 in eight of the latter), but leave less of a last round unused (5000 x 5000 x 1024: 46 and 45 us).
 bool large_tiles(int64_t M, int64_t N) {
     const double small = (double)tiles_of(M, N, 128) / 512;
     return (double)((tiles_of(M, N, 256) + 255) / 256) <= 0.6 * (small < 1.0 ? 1.0 : small);
@@ -633,7 +633,7 @@ void run(const Args& a, void* workspace, hipStream_t s) {
     const bool direct = !far && !a.bytes;
     const int stretches = stretches_of(a.M, a.N, a.K);
     if (a.M <= kFewRows) {
-        // 8 x 50001 x 1024: 14.7 us with 32 channels a wavefront, 15.9 with 16; 1 x 512 x 8192: 11.2 and 7.9
+        // 8 x 50001 x 1024: 11.9 us with 32 channels a wavefront, 13.4 with 16; 1 x 512 x 8192: 10.9 and 7.5 to 8.3
         if (a.N >= 16384) a.M <= 16 ? launch_few<S, 1, 2>(a, 1536, s) : launch_few<S, 2, 2>(a, 1536, s);
         else a.M <= 16 ? launch_few<S, 1, 1>(a, 2048, s) : launch_few<S, 2, 1>(a, 2048, s);
     } else if (far) {

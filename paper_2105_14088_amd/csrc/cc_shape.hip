@@ -206,7 +206,8 @@ __device__ __forceinline__ void look_back(const int32_t* history, int n, int sta
 }
 
 // 64 lanes, K vectors each, for a row.  The next row is on its way while one is worked on.  Bound by memory where penalties only forbid: 64 x
-// 1000 x 1000 bf16 61 us, 4.2 TB/s; with counts by some 18 operations a logit (forward 70 to 75 us, gradient 92).
+// 1000 x 1000 bf16 61 us, 4.2 TB/s; with counts forward 68 us (3.8 TB/s) and gradient 90 (4.3): their 22 and 19
+// vector operations a logit keep the SIMDs busy for 36 and 31 us, and with four wavefronts on each they do not all hide behind the memory.
 template <class S, int VEC, int K, bool BACK, bool COUNT>
 __global__ __launch_bounds__(kThreads) void short_kernel(const Args a) {
     constexpr int CAP = 64 * VEC * K, WAVES = kThreads / 64;
@@ -294,7 +295,8 @@ __global__ __launch_bounds__(kThreads) void short_kernel(const Args a) {
     }
 }
 
-// A stretch of a row: 128 rows of 131072 bf16 12 us without a history (5.5 TB/s), 22 with some 2000 entries each, as unequal as words.  A
+// A stretch of a row: 128 rows of 131072 bf16 12 us without a history (5.5 TB/s), 21 with some 2000 entries each, as unequal as words.
+// Every row counts its history anew, also where it is one entry longer than the row before: 8 x 512 x 32000 bf16 157 us, 106 without a history.  A
 // vector that would end beyond the row is taken element by element.
 template <class S, int THREADS, bool BACK, bool COUNT>
 __global__ __launch_bounds__(THREADS) void long_kernel(const Args a) {
